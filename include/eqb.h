@@ -319,6 +319,160 @@ eqb_status eqb_layer_noalloc(const uint16_t* z, const float* b, int64_t T, int32
                              int32_t* hist_hi_sum, int32_t* hist_lo_sum, int32_t* dev_status, void* stream);
 
 /*
+ * ------------------------------------------------------------------------
+ * Training operators around the layer: the balance loss with its gradient,
+ * the experts' rows, and the optimizer step.  The conventions above hold for
+ * them too, except that every output is WRITTEN, not accumulated.
+ * ------------------------------------------------------------------------
+ */
+
+/* Element types of rows, gradients and the like. */
+#define EQB_DTYPE_F32        0
+#define EQB_DTYPE_BF16       1
+#define EQB_DTYPE_F16        2
+
+/* What the balance loss takes as a token's probabilities p_{t,e}. */
+#define EQB_SCORE_SIGMOID    0   /* sigmoid(z_{t,e}) / sum_e sigmoid(z_{t,e}) */
+#define EQB_SCORE_SOFTMAX    1   /* exp(z_{t,e}) / sum_e exp(z_{t,e}) */
+
+/*
+ * The auxiliary balance loss (Sec. 2, "GShard"; App. D) of each balance group,
+ * with the counts of every expert.  A group is a partition of the token batch:
+ * a rank's local batch, or one sequence.  For group p with n_p valid tokens:
+ *   f_{p,e}    = #{(t, k) : topk_idx[t,k] = e, t valid in p}
+ *   prob_{p,e} = (1/n_p) sum over valid t of p_{t,e}
+ *   loss_p     = alpha * sum_e F_{p,e} prob_{p,e},   F_{p,e} = E f_{p,e} / (K n_p)
+ * so that an even load gives alpha.  A group without valid tokens has prob = 0
+ * and loss = 0.
+ *   z [T,E] bf16 bits (16-byte aligned).  Logits of -inf (masked experts) have
+ *     probability 0; a row of nothing but -inf has p = 0 throughout.
+ *   topk_idx [T,K] int32 (nullable): entries outside [0, E) are not counted.
+ *     With NULL, `load` is an INPUT: counts that the routing gave (over the
+ *     valid tokens).
+ *   valid [T] uint8 (nullable: every token is valid): a token of 0 takes no part,
+ *     whatever its logits hold (NaN included).
+ *   load [P,E] int32 (out, or in without topk_idx); tokens [P] int32 (out: n_p);
+ *   prob [P,E] binary32 (out); loss [P] binary32 (out).
+ *   workspace: eqb_balance_workspace_size(E, P) bytes, 256-byte aligned, owned
+ *     by the caller, zeroed once after allocation; each call leaves its leading
+ *     counter zero again.  Two calls whose work may overlap need two.
+ * The probabilities of a row and the sums over up to T / 256 rows are binary32,
+ * the sums of those binary64; the result does not depend on the order in which
+ * blocks run.  T = 0 writes zeros (`load` too, with or without topk_idx).
+ */
+size_t eqb_balance_workspace_size(int32_t E, int32_t P);     /* host only; 0 for unsupported E or P */
+eqb_status eqb_balance_loss(const uint16_t* z, const int32_t* topk_idx, const uint8_t* valid, int64_t T,
+                            int32_t E, int32_t K, const int64_t* part_off, int32_t P, int32_t score, double alpha,
+                            int32_t* load, int32_t* tokens, float* prob, float* loss, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of the balance loss with respect to the logits, alone or in one
+ * pass with the router backward and the load-error injection.  The loads are not
+ * differentiated (the straight-through estimate of App. D):
+ *   grad_z[t,e] = (alpha grad_loss_p / n_p) p_{t,e} q_{t,e} (F_{p,e} - sum_e' p_{t,e'} F_{p,e'})
+ *                 + (g[t,e] + inj[p,e]) sigmoid'(z_{t,e})
+ * with q = 1 - sigmoid(z) (EQB_SCORE_SIGMOID) or 1 (EQB_SCORE_SOFTMAX) and g, inj as
+ * in eqb_lei_router_backward; a row of an invalid token is 0 throughout.
+ *   load [P,E], tokens [P] int32 (in): from eqb_balance_loss.
+ *   grad_loss [P] binary32 (in): the gradient that arrives at each loss_p.
+ *   topk_idx [T,K], grad_score [T,K] (both or neither): g; inj [P,E] (nullable).
+ *   grad_z [T,E] binary32 (out, 16-byte aligned).
+ */
+eqb_status eqb_balance_backward(const uint16_t* z, const int32_t* load, const int32_t* tokens,
+                                const float* grad_loss, const int32_t* topk_idx, const float* grad_score,
+                                const float* inj, const uint8_t* valid, int64_t T, int32_t E, int32_t K,
+                                const int64_t* part_off, int32_t P, int32_t score, double alpha, float* grad_z,
+                                void* stream);
+
+/*
+ * The order of the experts' rows (what Eq. 1's FFN_e work on): the routed pairs
+ * (t, k) sorted by expert and within an expert by t*K + k.
+ *   topk_idx [T,K] int32 (in): entries outside [0, E) are dropped pairs.
+ *   offsets [E+1] int32 (out): expert e's rows are [offsets[e], offsets[e+1]).
+ *   slot [T,K] int32 (out): the row of pair (t, k), -1 for a dropped pair.
+ *   workspace: eqb_dispatch_workspace_size(T, K, E) bytes of scratch, 16-byte
+ *     aligned (nullable where that is 0); what it holds does not matter.
+ * T*K < 2^31.  T = 0 writes offsets of zeros.
+ */
+size_t eqb_dispatch_workspace_size(int64_t T, int32_t K, int32_t E);   /* host only */
+eqb_status eqb_dispatch_plan(const int32_t* topk_idx, int64_t T, int32_t K, int32_t E, int32_t* offsets,
+                             int32_t* slot, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of `hidden` elements of type dtype (EQB_DTYPE_*), between the tokens' order
+ * and the experts'.  `rows` tells how many rows the expert-ordered buffers hold;
+ * a pair whose slot lies outside [0, rows) is dropped.  Buffers need the alignment
+ * of their elements only.  T*K < 2^31.
+ *   eqb_dispatch: expert_rows[slot[t,k]] = x[t].  Rows that no slot names are left
+ *     as they are.
+ *   eqb_combine (Eq. 1): y[t] = sum over k of weight[t,k] expert_rows[slot[t,k]], in
+ *     ascending k in binary32, rounded once.  weight = NULL stands for 1: then it is
+ *     the gradient of eqb_dispatch.  Dropped pairs add nothing.
+ *   eqb_combine_backward: grad_rows[slot[t,k]] = weight[t,k] grad_y[t] (rows that no
+ *     slot names are left as they are) and grad_weight[t,k] = <grad_y[t],
+ *     expert_rows[slot[t,k]]> (0 for a dropped pair), summed in binary32: the
+ *     grad_score of eqb_lei_router_backward and eqb_balance_backward.
+ */
+eqb_status eqb_dispatch(const void* x, const int32_t* slot, int64_t T, int32_t K, int64_t rows, int32_t hidden,
+                        int32_t dtype, void* expert_rows, void* stream);
+eqb_status eqb_combine(const void* expert_rows, const int32_t* slot, const float* weight, int64_t T, int32_t K,
+                       int64_t rows, int32_t hidden, int32_t dtype, void* y, void* stream);
+eqb_status eqb_combine_backward(const void* grad_y, const void* expert_rows, const int32_t* slot,
+                                const float* weight, int64_t T, int32_t K, int64_t rows, int32_t hidden,
+                                int32_t dtype, void* grad_rows, float* grad_weight, void* stream);
+
+/*
+ * One AdamW step over n tensors (decoupled weight decay), in place:
+ *   g = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) g
+ *   v = beta2 v + ((1 - beta2) g) g
+ *   param = param (1 - lr weight_decay)
+ *           - (m / (sqrt(v) / sqrt(1 - beta2^step) + eps)) * (lr / (1 - beta1^step))
+ * Every operation is one binary32 operation in the order written (a division by a
+ * constant is a product with its reciprocal; constants are computed in binary64 and
+ * rounded once), so the results are reproducible bit for bit.
+ *
+ * state_bits = 32: exp_avg = m and exp_avg_sq = v, binary32.
+ * state_bits = 8: 8-bit codes (E4M3: sign, 4 exponent and 3 mantissa bits, largest
+ *   448, no infinities) of m / s and sqrt(v) / s, where a scale s = max / 448 belongs to
+ *   each block of EQB_ADAMW_BLOCK elements counted from the tensor's start.  (The square
+ *   root of v needs half of v's range of exponents.)  A code is rounded up or down at
+ *   random, up with the chance that makes it right on average, by 16 bits of a hash of
+ *   seed, step, the tensor's place in the call and the element: v moves by a few
+ *   thousandths per step, far less than half a code, so that rounding to nearest would
+ *   freeze the proportions inside a block.  A sqrt(v) above 0 never becomes 0, or the
+ *   divisor would fall to eps.  Blocks whose largest value is below 2^-100 are stored
+ *   as 0.  A gradient that is no finite number spoils its block.
+ *
+ * tensors: HOST array of n descriptors, read during the call.
+ *   param: binary32 weights; copy (nullable, in all tensors or in none): bf16 bits,
+ *   receives the new weights rounded to nearest even; grad: grad_dtype (F32 or BF16);
+ *   exp_avg, exp_avg_sq: numel elements of 4 bytes or of 1; exp_avg_scale,
+ *   exp_avg_sq_scale: ceil(numel / EQB_ADAMW_BLOCK) binary32 scales (8 bits only).
+ *   Pointers need the alignment of their elements; buffers must not overlap.
+ *   numel = 0 is allowed (and its pointers may be null).
+ * step >= 1: the number of this step.  grad_scale (nullable, device binary32):
+ * a factor on every gradient (clipping, unscaling).  found_inf (nullable, device
+ * binary32): where it is not 0 the call changes nothing.
+ */
+#define EQB_ADAMW_BLOCK      256
+typedef struct eqb_adamw_tensor {
+  float* param;
+  const void* grad;
+  uint16_t* copy;
+  void* exp_avg;
+  void* exp_avg_sq;
+  float* exp_avg_scale;
+  float* exp_avg_sq_scale;
+  int64_t numel;
+  double weight_decay;
+} eqb_adamw_tensor;
+eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                          int64_t step, double lr, double beta1, double beta2, double eps, uint64_t seed,
+                          const float* grad_scale, const float* found_inf, void* stream);
+
+/*
  * Test control (host only, no HIP call): caps the number of blocks of the
  * streaming kernels (routing, the margin passes, the LEI kernels) at
  * max_blocks for the calls that follow FROM THE CALLING HOST THREAD; calls

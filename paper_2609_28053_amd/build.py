@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, f) for f in ("eqb_api.hip", "margin.hip", "select.hip", "balance.hip", "variants.hip",
-                                          "layer_noalloc.hip")]
+                                          "layer_noalloc.hip", "balance_loss.hip", "experts.hip", "adamw.hip")]
 # The routing kernels are compiled on their own (one object per expert count,
 # in parallel: every fan-out has its own unrolled kernel), without IEEE mode: their
 # float maxima and medians then need no NaN quieting, which lets the compiler

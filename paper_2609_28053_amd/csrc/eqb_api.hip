@@ -1,6 +1,7 @@
 // eqb_api.hip - the C ABI declared in include/eqb.h.  Every argument check
 // runs before anything is enqueued; the calls never synchronise the host.
 #include <atomic>
+#include <cmath>
 
 #include "eqb_internal.hpp"
 
@@ -60,6 +61,18 @@ eqb_status make_table(const int64_t* part_off, int32_t P, int64_t T, PartTable* 
   for (int p = 0; p <= P; ++p) pt->off[p] = part_off[p];
   return EQB_OK;
 }
+
+// The key of a tensor's random bits at a step: seed, step and place mixed to 32 bits.
+uint32_t adamw_key(uint64_t seed, int64_t step, int32_t i) {
+  uint64_t k = seed + (uint64_t)step * 0x9E3779B97F4A7C15ull + (uint64_t)i * 0xD1B54A32D192ED03ull;
+  k = (k ^ (k >> 32)) * 0xBF58476D1CE4E5B9ull;
+  k = (k ^ (k >> 29)) * 0x94D049BB133111EBull;
+  return (uint32_t)(k ^ (k >> 32));
+}
+
+// Elements of one tensor and blocks of one launch: blocks times 256 threads stay below 2^32.
+constexpr int64_t kAdamwMostElements = (int64_t)1 << 34;
+constexpr uint32_t kAdamwMostBlocks = 1u << 23;
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -345,6 +358,182 @@ eqb_status layer_call(const uint16_t* z, const float* b, int64_t T, int32_t E, i
 }  // namespace eqb
 
 extern "C" {
+
+// -------------------------------------------------- training operators --
+size_t eqb_balance_workspace_size(int32_t E, int32_t P) {
+  if (!supported_E(E) || P < 1 || P > EQB_MAX_PARTITIONS) return 0;
+  return balance_workspace(nullptr, E, P, nullptr);
+}
+
+eqb_status eqb_balance_loss(const uint16_t* z, const int32_t* topk_idx, const uint8_t* valid, int64_t T,
+                            int32_t E, int32_t K, const int64_t* part_off, int32_t P, int32_t score, double alpha,
+                            int32_t* load, int32_t* tokens, float* prob, float* loss, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (T < 0 || T > INT32_MAX || K < 1 || K >= E) return EQB_ERR_INVALID_ARG;
+  if (!supported_E(E)) return EQB_ERR_UNSUPPORTED;
+  if (score != EQB_SCORE_SIGMOID && score != EQB_SCORE_SOFTMAX) return EQB_ERR_INVALID_ARG;
+  if (!(alpha == alpha)) return EQB_ERR_INVALID_ARG;
+  BalanceArgs a;
+  const eqb_status st = make_table(part_off, P, T, &a.pt);
+  if (st != EQB_OK) return st;
+  if (!load || !tokens || !prob || !loss || !workspace || (T > 0 && !z)) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(z) || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return EQB_ERR_UNSUPPORTED;
+  BalanceWorkspace ws;
+  if (workspace_bytes < balance_workspace(workspace, E, a.pt.P, &ws)) return EQB_ERR_INVALID_ARG;
+  a.z = z;
+  a.idx = topk_idx;
+  a.valid = valid;
+  a.T = T;
+  a.E = E;
+  a.K = K;
+  a.softmax = score == EQB_SCORE_SOFTMAX;
+  a.alpha = alpha;
+  a.load = load;
+  a.tokens = tokens;
+  a.prob = prob;
+  a.loss = loss;
+  return launch_balance_loss(a, ws, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_balance_backward(const uint16_t* z, const int32_t* load, const int32_t* tokens,
+                                const float* grad_loss, const int32_t* topk_idx, const float* grad_score,
+                                const float* inj, const uint8_t* valid, int64_t T, int32_t E, int32_t K,
+                                const int64_t* part_off, int32_t P, int32_t score, double alpha, float* grad_z,
+                                void* stream) {
+  if (T < 0 || T > INT32_MAX || K < 1 || K >= E) return EQB_ERR_INVALID_ARG;
+  if (!supported_E(E)) return EQB_ERR_UNSUPPORTED;
+  if (score != EQB_SCORE_SIGMOID && score != EQB_SCORE_SOFTMAX) return EQB_ERR_INVALID_ARG;
+  if (!(alpha == alpha)) return EQB_ERR_INVALID_ARG;
+  BalanceArgs a;
+  const eqb_status st = make_table(part_off, P, T, &a.pt);
+  if (st != EQB_OK) return st;
+  if ((topk_idx == nullptr) != (grad_score == nullptr)) return EQB_ERR_INVALID_ARG;
+  if (T == 0) return EQB_OK;
+  if (!z || !load || !tokens || !grad_loss || !grad_z) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(z) || !aligned16(grad_z)) return EQB_ERR_UNSUPPORTED;
+  a.z = z;
+  a.idx = topk_idx;
+  a.valid = valid;
+  a.T = T;
+  a.E = E;
+  a.K = K;
+  a.softmax = score == EQB_SCORE_SOFTMAX;
+  a.alpha = alpha;
+  a.load = const_cast<int32_t*>(load);
+  a.tokens = const_cast<int32_t*>(tokens);
+  a.grad_loss = grad_loss;
+  a.grad_score = grad_score;
+  a.inj = inj;
+  a.grad_z = grad_z;
+  return launch_balance_backward(a, static_cast<hipStream_t>(stream));
+}
+
+static bool plan_shape(int64_t T, int32_t K) { return T >= 0 && K >= 1 && T <= INT32_MAX && T * K <= INT32_MAX; }
+
+size_t eqb_dispatch_workspace_size(int64_t T, int32_t K, int32_t E) {
+  if (!plan_shape(T, K) || !supported_E(E)) return 0;
+  const uint32_t blocks = dispatch_plan_blocks(T * K);
+  return blocks > 1 ? (size_t)blocks * E * sizeof(int32_t) : 0;
+}
+
+eqb_status eqb_dispatch_plan(const int32_t* topk_idx, int64_t T, int32_t K, int32_t E, int32_t* offsets,
+                             int32_t* slot, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!plan_shape(T, K) || K >= E) return EQB_ERR_INVALID_ARG;
+  if (!supported_E(E)) return EQB_ERR_UNSUPPORTED;
+  if (!offsets || (T > 0 && (!topk_idx || !slot))) return EQB_ERR_INVALID_ARG;
+  const size_t need = eqb_dispatch_workspace_size(T, K, E);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(workspace)) return EQB_ERR_UNSUPPORTED;
+  return launch_dispatch_plan(topk_idx, T * K, E, offsets, slot, static_cast<int32_t*>(workspace),
+                              static_cast<hipStream_t>(stream));
+}
+
+static eqb_status row_call(eqb_status (*launch)(const RowArgs&, hipStream_t), const RowArgs& a, bool pointers,
+                           void* stream) {
+  if (!plan_shape(a.T, a.K) || a.rows < 0 || a.rows > INT32_MAX || a.H < 1) return EQB_ERR_INVALID_ARG;
+  if (a.dtype != EQB_DTYPE_F32 && a.dtype != EQB_DTYPE_BF16 && a.dtype != EQB_DTYPE_F16) return EQB_ERR_INVALID_ARG;
+  if (a.T == 0) return EQB_OK;
+  if (!pointers) return EQB_ERR_INVALID_ARG;
+  const uintptr_t mask = a.dtype == EQB_DTYPE_F32 ? 3 : 1;
+  if ((reinterpret_cast<uintptr_t>(a.tokens) | reinterpret_cast<uintptr_t>(a.experts) |
+       reinterpret_cast<uintptr_t>(a.out)) & mask)
+    return EQB_ERR_UNSUPPORTED;
+  return launch(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_dispatch(const void* x, const int32_t* slot, int64_t T, int32_t K, int64_t rows, int32_t hidden,
+                        int32_t dtype, void* expert_rows, void* stream) {
+  const RowArgs a{x, nullptr, slot, nullptr, T, rows, K, hidden, dtype, expert_rows, nullptr};
+  return row_call(launch_dispatch, a, x && slot && (expert_rows || rows == 0), stream);
+}
+
+eqb_status eqb_combine(const void* expert_rows, const int32_t* slot, const float* weight, int64_t T, int32_t K,
+                       int64_t rows, int32_t hidden, int32_t dtype, void* y, void* stream) {
+  const RowArgs a{nullptr, expert_rows, slot, weight, T, rows, K, hidden, dtype, y, nullptr};
+  return row_call(launch_combine, a, (expert_rows || rows == 0) && slot && y, stream);
+}
+
+eqb_status eqb_combine_backward(const void* grad_y, const void* expert_rows, const int32_t* slot,
+                                const float* weight, int64_t T, int32_t K, int64_t rows, int32_t hidden,
+                                int32_t dtype, void* grad_rows, float* grad_weight, void* stream) {
+  const RowArgs a{grad_y, expert_rows, slot, weight, T, rows, K, hidden, dtype, grad_rows, grad_weight};
+  return row_call(launch_combine_backward, a,
+                  grad_y && slot && weight && grad_weight && ((expert_rows && grad_rows) || rows == 0), stream);
+}
+
+eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                          int64_t step, double lr, double beta1, double beta2, double eps, uint64_t seed,
+                          const float* grad_scale, const float* found_inf, void* stream) {
+  if (n < 0 || (n > 0 && !tensors) || step < 1) return EQB_ERR_INVALID_ARG;
+  if (grad_dtype != EQB_DTYPE_F32 && grad_dtype != EQB_DTYPE_BF16) return EQB_ERR_INVALID_ARG;
+  if (state_bits != 32 && state_bits != 8) return EQB_ERR_INVALID_ARG;
+  if (!(lr == lr) || !(eps >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+    return EQB_ERR_INVALID_ARG;
+  const bool eight = state_bits == 8, grad_bf16 = grad_dtype == EQB_DTYPE_BF16;
+  bool first = true, copies = false;
+  for (int32_t i = 0; i < n; ++i) {
+    const eqb_adamw_tensor& t = tensors[i];
+    if (t.numel < 0 || t.numel > kAdamwMostElements || !(t.weight_decay == t.weight_decay)) return EQB_ERR_INVALID_ARG;
+    if (t.numel == 0) continue;
+    if (first) copies = t.copy != nullptr;
+    first = false;
+    if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (t.copy != nullptr) != copies) return EQB_ERR_INVALID_ARG;
+    if (eight && (!t.exp_avg_scale || !t.exp_avg_sq_scale)) return EQB_ERR_INVALID_ARG;
+    uintptr_t at = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.exp_avg_scale) |
+                   reinterpret_cast<uintptr_t>(t.exp_avg_sq_scale);
+    if (!eight) at |= reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq);
+    if (!grad_bf16) at |= reinterpret_cast<uintptr_t>(t.grad);
+    if ((at & 3) || ((reinterpret_cast<uintptr_t>(t.grad) | reinterpret_cast<uintptr_t>(t.copy)) & 1))
+      return EQB_ERR_UNSUPPORTED;
+  }
+  AdamwBatch b;
+  b.n = 0;
+  b.beta1 = (float)beta1;
+  b.rest1 = (float)(1.0 - beta1);
+  b.beta2 = (float)beta2;
+  b.rest2 = (float)(1.0 - beta2);
+  b.eps = (float)eps;
+  b.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  b.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+  b.grad_scale = grad_scale;
+  b.found_inf = found_inf;
+  uint32_t blocks = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const eqb_adamw_tensor& t = tensors[i];
+    if (t.numel == 0) continue;
+    const uint32_t more = adamw_blocks(t.numel);
+    if (b.n == kAdamwTensors || (b.n > 0 && blocks + more > kAdamwMostBlocks)) {
+      const eqb_status st = launch_adamw(b, blocks, eight, grad_bf16, static_cast<hipStream_t>(stream));
+      if (st != EQB_OK) return st;
+      b.n = 0;
+      blocks = 0;
+    }
+    b.t[b.n++] = AdamwSlot{t.param, t.grad, t.copy, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale,
+                           t.numel, (float)(1.0 - lr * t.weight_decay), adamw_key(seed, step, i), blocks};
+    blocks += more;
+  }
+  return b.n > 0 ? launch_adamw(b, blocks, eight, grad_bf16, static_cast<hipStream_t>(stream)) : EQB_OK;
+}
 
 eqb_status eqb_set_max_blocks(int32_t max_blocks) {
   if (max_blocks < 0) return EQB_ERR_INVALID_ARG;

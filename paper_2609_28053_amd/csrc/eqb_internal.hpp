@@ -113,6 +113,96 @@ eqb_status launch_lei_router_backward(const uint16_t* z, const int32_t* idx, con
 eqb_status launch_lei_inject(float* grad, const float* inj, int64_t T, int E, const PartTable& pt,
                              hipStream_t s);
 
+// ------------------------------------------------- training operators --
+inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct BalanceArgs {
+  const uint16_t* z;
+  const int32_t* idx = nullptr;      // nullable
+  const uint8_t* valid = nullptr;    // nullable
+  int64_t T;
+  int E, K;
+  bool softmax;
+  double alpha;
+  int32_t* load;
+  int32_t* tokens;
+  float* prob = nullptr;             // the loss's outputs
+  float* loss = nullptr;
+  const float* grad_loss = nullptr;  // the gradient's
+  const float* grad_score = nullptr;
+  const float* inj = nullptr;
+  float* grad_z = nullptr;
+  PartTable pt;
+};
+
+// Working memory of the balance loss: a ticket per group (zero before and after a call),
+// then the blocks' pieces.  A block's rows overlap consecutive groups, so block b's piece
+// of group p has place b + p, its own alone.
+constexpr int kBalanceBlocks = 512;          // most blocks of a launch
+struct BalanceWorkspace {
+  int32_t* tickets;     // [EQB_MAX_PARTITIONS]
+  int32_t* tokens;      // [kBalanceBlocks + P]
+  uint64_t* pieces;     // [kBalanceBlocks + P, E]: binary32 sum of probabilities, count
+};
+inline size_t balance_workspace(void* base, int E, int P, BalanceWorkspace* w) {
+  const size_t pieces = (size_t)kBalanceBlocks + P;
+  const size_t tickets = align256(EQB_MAX_PARTITIONS * sizeof(int32_t)), tokens = align256(pieces * sizeof(int32_t));
+  if (base && w) {
+    char* p = static_cast<char*>(base);
+    w->tickets = reinterpret_cast<int32_t*>(p);
+    w->tokens = reinterpret_cast<int32_t*>(p + tickets);
+    w->pieces = reinterpret_cast<uint64_t*>(p + tickets + tokens);
+  }
+  return tickets + tokens + align256(pieces * E * sizeof(uint64_t));
+}
+eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s);
+eqb_status launch_balance_backward(const BalanceArgs& a, hipStream_t s);
+
+// Blocks of the expert-order plan: each reads the counts of all.
+constexpr int kPlanMaxBlocks = 256;
+uint32_t dispatch_plan_blocks(int64_t N);
+eqb_status launch_dispatch_plan(const int32_t* idx, int64_t N, int E, int32_t* offsets, int32_t* slot, int32_t* counts,
+                                hipStream_t s);
+struct RowArgs {
+  const void* tokens;     // [T,H]: x, or grad_y
+  const void* experts;    // [rows,H]
+  const int32_t* slot;
+  const float* weight;
+  int64_t T, rows;
+  int K, H, dtype;
+  void* out;
+  float* grad_weight;
+};
+eqb_status launch_dispatch(const RowArgs& a, hipStream_t s);
+eqb_status launch_combine(const RowArgs& a, hipStream_t s);
+eqb_status launch_combine_backward(const RowArgs& a, hipStream_t s);
+
+// Tensors of one AdamW launch, passed by value (kernel arguments hold 4 KiB).
+struct AdamwSlot {
+  float* param;
+  const void* grad;
+  uint16_t* copy;
+  void* exp_avg;
+  void* exp_avg_sq;
+  float* exp_avg_scale;
+  float* exp_avg_sq_scale;
+  int64_t numel;
+  float keep;             // 1 - lr * weight_decay
+  uint32_t key;           // of the random bits
+  uint32_t first_block;
+};
+constexpr int kAdamwTensors = 48;
+struct AdamwBatch {
+  int n;
+  float beta1, rest1, beta2, rest2, eps, inv_root, rate;
+  const float* grad_scale;
+  const float* found_inf;
+  AdamwSlot t[kAdamwTensors];
+};
+static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
+uint32_t adamw_blocks(int64_t numel);
+eqb_status launch_adamw(const AdamwBatch& b, uint32_t blocks, bool eight, bool grad_bf16, hipStream_t s);
+
 // Count slabs per partition in a layer's workspace: enough that about 8
 // slabs share the blocks of a launch, so no counter receives the flush
 // atomics of every block.  Only the route sweep's coarse counts use them
@@ -145,8 +235,6 @@ struct LayerWorkspace {
 // Reserved for tickets.  Far more than they take: the workspace keeps the size
 // that callers have allocated by.
 constexpr size_t kTicketBytes = 128 << 10;
-
-inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Bytes of a layer workspace, and its pieces carved from base (null base:
 // only the size is computed).  with_part = false leaves out the fine pass's

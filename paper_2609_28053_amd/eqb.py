@@ -29,6 +29,12 @@ EQB_NOALLOC_SCRATCH_BYTES = (8 << 20) + (192 << 10)
 EQB_NBINS = 256
 EQB_MAX_PARTITIONS = 256
 EQB_DEV_RANK_EXCEEDS_COUNT = 1
+EQB_DTYPE_F32 = 0
+EQB_DTYPE_BF16 = 1
+EQB_DTYPE_F16 = 2
+EQB_SCORE_SIGMOID = 0
+EQB_SCORE_SOFTMAX = 1
+EQB_ADAMW_BLOCK = 256
 
 EXPORTS = (
     "eqb_route_topk",
@@ -49,6 +55,15 @@ EXPORTS = (
     "eqb_layer_workspace_zero_bytes",
     "eqb_layer",
     "eqb_layer_noalloc",
+    "eqb_balance_workspace_size",
+    "eqb_balance_loss",
+    "eqb_balance_backward",
+    "eqb_dispatch_workspace_size",
+    "eqb_dispatch_plan",
+    "eqb_dispatch",
+    "eqb_combine",
+    "eqb_combine_backward",
+    "eqb_adamw_step",
     "eqb_set_max_blocks",
     "eqb_get_max_blocks",
     "eqb_rank",
@@ -84,6 +99,15 @@ def _load():
         "eqb_layer_workspace_zero_bytes": [i32, i32],
         "eqb_layer": [P, P, i64, i32, i32, P, i32, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P, P],
         "eqb_layer_noalloc": [P, P, i64, i32, i32, P, i32, P, P, P, P, P, P, P, P, P, P],
+        "eqb_balance_workspace_size": [i32, i32],
+        "eqb_balance_loss": [P, P, P, i64, i32, i32, P, i32, i32, ctypes.c_double, P, P, P, P, P, ctypes.c_size_t, P],
+        "eqb_balance_backward": [P, P, P, P, P, P, P, P, i64, i32, i32, P, i32, i32, ctypes.c_double, P, P],
+        "eqb_dispatch_workspace_size": [i64, i32, i32],
+        "eqb_dispatch_plan": [P, i64, i32, i32, P, P, P, ctypes.c_size_t, P],
+        "eqb_dispatch": [P, P, i64, i32, i64, i32, i32, P, P],
+        "eqb_combine": [P, P, P, i64, i32, i64, i32, i32, P, P],
+        "eqb_combine_backward": [P, P, P, P, i64, i32, i64, i32, i32, P, P, P],
+        "eqb_adamw_step": [P, i32, i32, i32, i64] + [ctypes.c_double] * 4 + [ctypes.c_uint64, P, P, P],
         "eqb_set_max_blocks": [i32],
         "eqb_get_max_blocks": [],
         "eqb_rank": [i64, i32, i32],
@@ -96,6 +120,8 @@ def _load():
     lib.eqb_rank.restype = i64
     lib.eqb_layer_workspace_size.restype = ctypes.c_size_t
     lib.eqb_layer_workspace_zero_bytes.restype = ctypes.c_size_t
+    lib.eqb_balance_workspace_size.restype = ctypes.c_size_t
+    lib.eqb_dispatch_workspace_size.restype = ctypes.c_size_t
     lib.eqb_status_string.restype = ctypes.c_char_p
     return lib
 
@@ -369,6 +395,160 @@ def eqb_layer_noalloc(z, b, K, topk_idx, topk_score, tau, load, q_bf16, b_next, 
         _ptr(hist_lo_sum, torch.int32, E * EQB_NBINS, "hist_lo_sum"),
         _ptr(dev_status, torch.int32, 1, "dev_status"), _stream(stream)))
     del keep
+
+
+def eqb_balance_workspace_size(E: int, P: int) -> int:
+    """Bytes of the balance loss's workspace (uint8, zeroed once; every call leaves its counters zero)."""
+    return int(lib.eqb_balance_workspace_size(E, P))
+
+
+def _mask(valid, T):
+    """A token mask as the uint8 bytes the library reads (a bool tensor holds such bytes)."""
+    return _ptr(valid, (torch.bool, torch.uint8), T, "valid")
+
+
+def eqb_balance_loss(z, topk_idx, K, alpha, load, tokens, prob, loss, workspace, valid=None, part_off=None,
+                     score=EQB_SCORE_SIGMOID, stream=None):
+    """Balance loss of every group (partition), its mean probabilities, its valid tokens and, counted from
+    topk_idx, its loads.  With topk_idx = None the loads are an input (the routing's own counts)."""
+    T, E = z.shape
+    po, P, keep = _offsets(part_off, T)
+    _check("eqb_balance_loss", lib.eqb_balance_loss(
+        _ptr(z, _Z, name="z"), _ptr(topk_idx, torch.int32, T * K, "topk_idx"), _mask(valid, T), T, E, K, po, P,
+        score, float(alpha), _ptr(load, torch.int32, P * E, "load"), _ptr(tokens, torch.int32, P, "tokens"),
+        _ptr(prob, torch.float32, P * E, "prob"), _ptr(loss, torch.float32, P, "loss"),
+        _ptr(workspace, torch.uint8, name="workspace"), workspace.numel(), _stream(stream)))
+    del keep
+
+
+def eqb_balance_backward(z, load, tokens, K, alpha, grad_loss, grad_z, topk_idx=None, grad_score=None, inj=None,
+                         valid=None, part_off=None, score=EQB_SCORE_SIGMOID, stream=None):
+    """Gradient of the balance losses (weighted by grad_loss) with respect to the logits; with topk_idx and
+    grad_score, and with inj, in one pass with eqb_lei_router_backward's."""
+    T, E = z.shape
+    po, P, keep = _offsets(part_off, T)
+    _check("eqb_balance_backward", lib.eqb_balance_backward(
+        _ptr(z, _Z, name="z"), _ptr(load, torch.int32, P * E, "load"), _ptr(tokens, torch.int32, P, "tokens"),
+        _ptr(grad_loss, torch.float32, P, "grad_loss"), _ptr(topk_idx, torch.int32, T * K, "topk_idx"),
+        _ptr(grad_score, torch.float32, T * K, "grad_score"), _ptr(inj, torch.float32, P * E, "inj"),
+        _mask(valid, T), T, E, K, po, P, score, float(alpha), _ptr(grad_z, torch.float32, T * E, "grad_z"),
+        _stream(stream)))
+    del keep
+
+
+def eqb_dispatch_workspace_size(T: int, K: int, E: int) -> int:
+    """Bytes of scratch that eqb_dispatch_plan needs (0 for a few thousand pairs)."""
+    return int(lib.eqb_dispatch_workspace_size(T, K, E))
+
+
+def eqb_dispatch_plan(topk_idx, E, offsets, slot, workspace=None, stream=None):
+    """The routed pairs sorted by expert, in their order within an expert: every pair's row (slot, -1 for an
+    index outside [0, E)) and the experts' first rows (offsets [E+1])."""
+    T, K = topk_idx.shape
+    _check("eqb_dispatch_plan", lib.eqb_dispatch_plan(
+        _ptr(topk_idx, torch.int32, name="topk_idx"), T, K, E, _ptr(offsets, torch.int32, E + 1, "offsets"),
+        _ptr(slot, torch.int32, T * K, "slot"), _ptr(workspace, torch.uint8, name="workspace"),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
+
+
+_ROW_TYPES = {torch.float32: EQB_DTYPE_F32, torch.bfloat16: EQB_DTYPE_BF16, torch.float16: EQB_DTYPE_F16}
+
+
+def _row_type(t, name):
+    if t.dtype not in _ROW_TYPES:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {tuple(_ROW_TYPES)}")
+    return _ROW_TYPES[t.dtype]
+
+
+def eqb_dispatch(x, slot, expert_rows, stream=None):
+    """expert_rows[slot[t, k]] = x[t]; rows that no slot names are left as they are."""
+    (T, H), K, R = x.shape, slot.shape[1], expert_rows.shape[0]
+    _check("eqb_dispatch", lib.eqb_dispatch(
+        _ptr(x, name="x"), _ptr(slot, torch.int32, T * K, "slot"), T, K, R, H, _row_type(x, "x"),
+        _ptr(expert_rows, x.dtype, R * H, "expert_rows"), _stream(stream)))
+
+
+def eqb_combine(expert_rows, slot, weight, y, stream=None):
+    """y[t] = sum_k weight[t, k] expert_rows[slot[t, k]]; without weight, the gradient of eqb_dispatch."""
+    (T, H), K, R = y.shape, slot.shape[1], expert_rows.shape[0]
+    _check("eqb_combine", lib.eqb_combine(
+        _ptr(expert_rows, y.dtype, R * H, "expert_rows"), _ptr(slot, torch.int32, T * K, "slot"),
+        _ptr(weight, torch.float32, T * K, "weight"), T, K, R, H, _row_type(y, "y"), _ptr(y, name="y"),
+        _stream(stream)))
+
+
+def eqb_combine_backward(grad_y, expert_rows, slot, weight, grad_rows, grad_weight, stream=None):
+    """Gradients of eqb_combine: grad_rows of the experts' rows, grad_weight of the mixture weights."""
+    (T, H), K, R = grad_y.shape, slot.shape[1], expert_rows.shape[0]
+    _check("eqb_combine_backward", lib.eqb_combine_backward(
+        _ptr(grad_y, name="grad_y"), _ptr(expert_rows, grad_y.dtype, R * H, "expert_rows"),
+        _ptr(slot, torch.int32, T * K, "slot"), _ptr(weight, torch.float32, T * K, "weight"), T, K, R, H,
+        _row_type(grad_y, "grad_y"), _ptr(grad_rows, grad_y.dtype, R * H, "grad_rows"),
+        _ptr(grad_weight, torch.float32, T * K, "grad_weight"), _stream(stream)))
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step, converted once for repeated calls.  It
+    keeps the tensors alive that it names; ``set_grads`` exchanges the
+    gradients.  Parameters are binary32; ``copies``, if given, are BF16
+    tensors that receive the new parameters.  Either binary32 states, or 8-bit
+    ones (torch.float8_e4m3fn) with their blocks' scales: exp_avg times
+    exp_avg_scale is the first moment, exp_avg_sq times exp_avg_sq_scale the
+    square root of the second.  weight_decay: one value, or one per tensor."""
+
+    _FIELDS = np.dtype([(n, np.uint64) for n in ("param", "grad", "copy", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                 "exp_avg_sq_scale")] + [("numel", np.int64), ("weight_decay", np.float64)])
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, copies=None, exp_avg_scale=None, exp_avg_sq_scale=None,
+                 weight_decay=0.0):
+        if (exp_avg_scale is None) != (exp_avg_sq_scale is None):
+            raise ValueError("8-bit states need the scales of both moments")
+        self.n = len(params)
+        self.state_bits = 32 if exp_avg_scale is None else 8
+        self.numel = [p.numel() for p in params]
+        self.table = np.zeros(self.n, dtype=self._FIELDS)
+        self.table["numel"] = self.numel
+        self.table["weight_decay"] = weight_decay
+        blocks = [-(-n // EQB_ADAMW_BLOCK) for n in self.numel]
+        state = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
+        self._kept = []
+        self._set("param", params, torch.float32, self.numel)
+        self._set("copy", copies, torch.bfloat16, self.numel)
+        self._set("exp_avg", exp_avg, state, self.numel)
+        self._set("exp_avg_sq", exp_avg_sq, state, self.numel)
+        self._set("exp_avg_scale", exp_avg_scale, torch.float32, blocks)
+        self._set("exp_avg_sq_scale", exp_avg_sq_scale, torch.float32, blocks)
+        self.set_grads(grads)
+
+    def _set(self, field, tensors, dtype, numel):
+        if tensors is None:
+            return
+        if len(tensors) != self.n:
+            raise ValueError(f"{len(tensors)} {field} tensors for {self.n} parameters")
+        self.table[field] = [_ptr(t, dtype, n, field).value or 0 for t, n in zip(tensors, numel)]
+        self._kept.append(list(tensors))
+
+    def set_grads(self, grads):
+        """Gradients of the next step, one per parameter, all binary32 or all BF16."""
+        dtype = grads[0].dtype if self.n else torch.float32
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"gradients have dtype {dtype}, expected torch.float32 or torch.bfloat16")
+        if len(grads) != self.n:
+            raise ValueError(f"{len(grads)} gradients for {self.n} parameters")
+        self.table["grad"] = [_ptr(g, dtype, n, "grad").value or 0 for g, n in zip(grads, self.numel)]
+        self.grads = list(grads)
+        self.grad_dtype = _ROW_TYPES[dtype]
+
+
+def eqb_adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.95, eps=1e-8, seed=0, grad_scale=None,
+                   found_inf=None, stream=None):
+    """One AdamW step, in place, over all the tensors.  step counts from 1; seed draws the 8-bit states'
+    rounding; grad_scale and found_inf are device scalars (a factor on the gradients; skip the step)."""
+    _check("eqb_adamw_step", lib.eqb_adamw_step(
+        tensors.table.ctypes.data, tensors.n, tensors.grad_dtype, tensors.state_bits, int(step), float(lr),
+        float(beta1), float(beta2), float(eps), int(seed) & (2**64 - 1),
+        _ptr(grad_scale, torch.float32, 1, "grad_scale"), _ptr(found_inf, torch.float32, 1, "found_inf"),
+        _stream(stream)))
 
 
 def eqb_set_max_blocks(max_blocks: int) -> None:

@@ -1,0 +1,235 @@
+"""GPU AdamW against the stated binary32 operations, done one by one by numpy: bit for bit
+with binary32 states and for weights and scales with 8-bit ones.  A code is allowed to be
+its neighbour where the random number decides it by a hair: the scaled value is off by 3
+roundings (3 2^-24 relatively, against steps of 2^-4 to 2^-3 of it in 2^16 parts each), so
+for about 2^-24 3 16 = 3e-6 of the elements; up to 1e-4, and one in small tensors, passes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train_oracle as O
+from test_gpu_balance import eqb, say  # noqa: F401 (eqb is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.98, eps=1e-8)
+
+
+def views(flat, sizes, shift):
+    """The tensors back to back in a flat buffer that starts `shift` elements past an aligned address."""
+    buf = torch.empty(len(flat) + shift, dtype=flat.dtype, device="cuda")
+    buf[shift:].copy_(flat)
+    return list(buf[shift:].split(sizes))
+
+
+class Model:
+    def __init__(self, seed, sizes, bits, grads, copy, shift=0, spread=1e-3):
+        rng = np.random.default_rng(seed)
+        self.sizes, self.bits = sizes, bits
+        n = sum(sizes)
+        big = np.exp(rng.normal(size=n) * 1.5) * spread
+        self.w = [a.astype(np.float32) for a in np.split(rng.normal(size=n), np.cumsum(sizes)[:-1])]
+        g = (rng.normal(size=n) * big).astype(np.float32)
+        g[rng.random(n) < 0.05] = 0.0
+        gt = torch.from_numpy(g).to(torch.bfloat16 if grads == "bf16" else torch.float32)
+        self.g = [a.to(torch.float32).numpy() for a in gt.split(sizes)]
+        m = (rng.normal(size=n) * big * 0.3).astype(np.float32)
+        r = ((np.abs(rng.normal(size=n)) + 0.05) * big).astype(np.float32)
+        cut = np.cumsum(sizes)[:-1]
+        self.m, self.r = np.split(m, cut), np.split(r, cut)
+        self.decay = [0.1 if i % 2 == 0 else 0.0 for i in range(len(sizes))]
+        self.tw = views(torch.from_numpy(np.concatenate(self.w)), sizes, shift)
+        self.tg = views(gt, sizes, shift)
+        self.tc = views(torch.zeros(n, dtype=torch.bfloat16), sizes, shift) if copy else None
+        if bits == 32:
+            self.v = [a * a for a in self.r]
+            self.tm = views(torch.from_numpy(m), sizes, shift)
+            self.tv = views(torch.from_numpy(np.concatenate(self.v)), sizes, shift)
+            self.sm = self.sv = None
+            return
+        zero = np.zeros(max(sizes), dtype=np.int64)
+        self.cm, self.cv, self.sm0, self.sv0 = [], [], [], []
+        for a, b in zip(self.m, self.r):
+            c, s = O.quantise(a.astype(np.float64), zero[:len(a)] + 32768, False)
+            d, q = O.quantise(b.astype(np.float64), zero[:len(b)] + 32768, True)
+            self.cm.append(c), self.cv.append(d), self.sm0.append(s.astype(np.float32)), self.sv0.append(q.astype(np.float32))
+        blocks = [len(s) for s in self.sm0]
+        code = lambda cs: torch.from_numpy(np.concatenate(cs).astype(np.uint8)).view(torch.float8_e4m3fn)  # noqa: E731
+        self.tm, self.tv = ([t.view(torch.float8_e4m3fn) for t in views(code(c).view(torch.uint8), sizes, shift)] for c in (self.cm, self.cv))
+        self.sm, self.sv = (views(torch.from_numpy(np.concatenate(s)), blocks, shift) for s in (self.sm0, self.sv0))
+
+    def table(self, eqb):  # noqa: F811
+        return eqb.AdamwTensors(self.tw, self.tg, self.tm, self.tv, copies=self.tc, exp_avg_scale=self.sm,
+                                exp_avg_sq_scale=self.sv, weight_decay=self.decay)
+
+    def want(self, i, step, scale, hyper):
+        f = np.float32
+        if self.bits == 32:
+            m, v = self.m[i], self.v[i]
+        else:
+            at = np.arange(self.sizes[i]) // O.BLOCK
+            m = O.E4M3[self.cm[i]].astype(f) * self.sm0[i][at]
+            r = O.E4M3[self.cv[i]].astype(f) * self.sv0[i][at]
+            v = r * r
+        return O.adamw32(self.w[i], self.g[i], m, v, step, weight_decay=self.decay[i], grad_scale=scale, **hyper)
+
+
+def bits_of(t):
+    return t.cpu().view(torch.int32 if t.dtype == torch.float32 else torch.int16 if t.dtype == torch.bfloat16 else torch.uint8).numpy()
+
+
+def check(m, step, seed, scale=1.0, hyper=HYPER):
+    far = 0
+    for i, n in enumerate(m.sizes):
+        w, mm, v, r = m.want(i, step, scale, hyper)
+        assert np.array_equal(bits_of(m.tw[i]), w.view(np.int32)), (i, "weight")
+        if m.tc:
+            assert np.array_equal(bits_of(m.tc[i]), bits_of(torch.from_numpy(w).to(torch.bfloat16))), (i, "copy")
+        if m.bits == 32:
+            assert np.array_equal(bits_of(m.tm[i]), mm.view(np.int32)) and np.array_equal(bits_of(m.tv[i]), v.view(np.int32))
+            continue
+        rnd = O.random32(n, O.tensor_key(seed, step, i))
+        for t, s, x, bits, nonzero in ((m.tm[i], m.sm[i], mm, rnd & 0xFFFF, False), (m.tv[i], m.sv[i], r, rnd >> 16, True)):
+            full = np.zeros(-(-n // O.BLOCK) * O.BLOCK, dtype=np.float32)
+            full[:n] = np.abs(x)
+            top = full.reshape(-1, O.BLOCK).max(1)
+            scale32 = np.where(top < np.float32(2.0 ** -100), np.float32(0), top * np.float32(1 / 448))
+            assert np.array_equal(bits_of(s), scale32.view(np.int32)), (i, "scale")
+            codes, _ = O.quantise(x.astype(np.float64), bits, nonzero)
+            got = bits_of(t).astype(np.int64)
+            assert np.array_equal(got >> 7, codes >> 7) and np.abs(got - codes).max() <= 1
+            far += int((got != codes).sum())
+    assert far <= max(2, 1e-4 * sum(m.sizes)), far
+
+
+SIZES = [[1], [3, 1, 5], [255, 256, 257, 511], [1000, 4096, 4097, 2, 16385, 100], [70000, 1, 9, 300],
+         [17] * 60 + [1024] * 60 + [5000] * 7]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grads", ["f32", "bf16"])
+@pytest.mark.parametrize("copy", [False, True])
+@pytest.mark.parametrize("which", range(len(SIZES)))
+@pytest.mark.parametrize("shift", [0, 1])
+def test_step(eqb, bits, grads, copy, which, shift):  # noqa: F811
+    sizes = SIZES[which]
+    say(f"adamw {bits} bits, {grads} gradients, copy={copy}, {len(sizes)} tensors, shift={shift}")
+    m = Model(which * 10 + shift, sizes, bits, grads, copy, shift)
+    eqb.eqb_adamw_step(m.table(eqb), 7, seed=123456789012345, **HYPER)
+    check(m, 7, 123456789012345)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_scalars(eqb, bits):  # noqa: F811
+    """The first step, other coefficients, a factor on the gradients, and a step that is skipped."""
+    sizes = [300, 2000]
+    one = torch.ones(1, device="cuda")
+    for step, scale, hyper in ((1, 1.0, HYPER), (1, 0.37, dict(lr=1.0, beta1=0.0, beta2=0.0, eps=0.5)),
+                               (100000, 3.0, dict(lr=1e-4, beta1=0.95, beta2=0.999, eps=1e-15))):
+        m = Model(step, sizes, bits, "f32", True)
+        say(f"adamw {bits} bits, step {step}, scale {scale}")
+        eqb.eqb_adamw_step(m.table(eqb), step, seed=9, grad_scale=one * scale, found_inf=one * 0, **hyper)
+        check(m, step, 9, np.float32(scale), hyper)
+    m = Model(5, sizes, bits, "f32", True)
+    before = [bits_of(t).copy() for t in m.tw + m.tc + m.tm + m.tv]
+    eqb.eqb_adamw_step(m.table(eqb), 3, found_inf=one, **HYPER)
+    assert all(np.array_equal(a, bits_of(t)) for a, t in zip(before, m.tw + m.tc + m.tm + m.tv))
+
+
+def test_new_gradients_and_empty_tensors(eqb):  # noqa: F811
+    m = Model(1, [0, 40, 0, 600], 32, "bf16", False)
+    t = m.table(eqb)
+    t.set_grads([g.clone() for g in m.tg])
+    eqb.eqb_adamw_step(t, 2, **HYPER)
+    check(m, 2, 0)
+    with pytest.raises(ValueError):
+        t.set_grads(m.tg[:1])
+    with pytest.raises(TypeError):
+        t.set_grads([g.to(torch.float16) for g in m.tg])
+    with pytest.raises(ValueError):
+        eqb.AdamwTensors(m.tw, m.tg, m.tm, [v[:1] for v in m.tv])
+    with pytest.raises(ValueError):
+        eqb.AdamwTensors([torch.zeros((4, 4), device="cuda").t()[:2]], [torch.zeros(8, device="cuda")],
+                         [torch.zeros(8, device="cuda")], [torch.zeros(8, device="cuda")])
+
+
+def test_blocks_of_zeros_and_tiny_values(eqb):  # noqa: F811
+    """8 bits: blocks without gradients stay 0; blocks below 2^-100 are stored as 0; subnormal and huge values."""
+    for spread in (0.0, 1e-38, 1e-33, 1e-20, 1e15):
+        m = Model(3, [256 * 3 + 10], 8, "f32", False, spread=spread)
+        say(f"adamw 8 bits, values about {spread}")
+        eqb.eqb_adamw_step(m.table(eqb), 4, seed=1, **HYPER)
+        check(m, 4, 1)
+
+
+def test_a_gradient_that_is_no_number_spoils_its_block_alone(eqb):  # noqa: F811
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        m, o = Model(6, [1000], 8, "f32", False), Model(6, [1000], 8, "f32", False)
+        m.tg[0][300] = bad
+        for k in (m, o):
+            eqb.eqb_adamw_step(k.table(eqb), 4, seed=1, **HYPER)
+        keep = np.ones(1000, dtype=bool)
+        keep[256:512] = False
+        for a, b in ((m.tw, o.tw), (m.tm, o.tm), (m.tv, o.tv)):
+            assert np.array_equal(bits_of(a[0])[keep], bits_of(b[0])[keep])
+        value = m.tm[0].to(torch.float32) * m.sm[0].repeat_interleave(256)[:1000]
+        assert not torch.isfinite(value[300]) and not torch.isfinite(m.tw[0][300])
+
+
+def test_states_of_8_bits_follow_those_of_32(eqb):  # noqa: F811
+    """On average the codes neither freeze nor drift: after 400 steps of gradients of constant size the mean of the
+    second moment is that of the exact one (both moments' means within five standard errors of rounding by steps of an
+    eighth, sqrt(1/12)/8 an element a step over the window 1/(1 - beta2) of the average)."""
+    n, steps = 1 << 16, 400
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    d = dict(device="cuda")
+    sizes = torch.exp(torch.randn(n, generator=g, **d))
+    w8, w32 = torch.zeros(n, **d), torch.zeros(n, **d)
+    m8, v8 = (torch.zeros(n, dtype=torch.uint8, **d).view(torch.float8_e4m3fn) for _ in range(2))
+    s8, q8 = torch.zeros(n // 256, **d), torch.zeros(n // 256, **d)
+    m32, v32, grad = torch.zeros(n, **d), torch.zeros(n, **d), torch.empty(n, **d)
+    eight = eqb.AdamwTensors([w8], [grad], [m8], [v8], exp_avg_scale=[s8], exp_avg_sq_scale=[q8])
+    full = eqb.AdamwTensors([w32], [grad], [m32], [v32])
+    say("adamw, 400 steps")
+    for step in range(1, steps + 1):
+        grad.copy_(torch.randn(n, generator=g, **d) * sizes)
+        eqb.eqb_adamw_step(eight, step, 1e-3, 0.9, 0.99, 1e-8, seed=5)
+        eqb.eqb_adamw_step(full, step, 1e-3, 0.9, 0.99, 1e-8)
+    r8 = v8.to(torch.float32) * q8.repeat_interleave(256)
+    ratio = (r8 * r8 / v32).double()
+    # a step's rounding of sqrt(v) has deviation 1/8/sqrt(12) or less; v keeps 1/(1 - 0.99) of them, squared
+    # doubles them: 0.072 sqrt(100/2) = 0.51 an element at most, and its square adds to the mean of v
+    sd = 2 * 0.036 * (1 / (1 - 0.99 ** 2)) ** 0.5
+    assert abs(float(ratio.mean()) - 1) < sd * sd + 5 * sd / n ** 0.5
+    # the weights, driven by the ratio of the moments, end where the exact ones do
+    assert float((w8 - w32).norm() / w32.norm()) < 2 * sd
+
+
+def test_elements_past_2_to_the_32(eqb):  # noqa: F811
+    """A tensor of more than 2^32 elements: its last ones against the formula, with their own random numbers."""
+    n, tail = (1 << 32) + 777, 777 + 256 * 3
+    say("adamw, 2^32 elements")
+    d = dict(device="cuda")
+    w = torch.zeros(n, **d)
+    grad = torch.zeros(n, dtype=torch.bfloat16, **d)
+    m, v = (torch.zeros(n, dtype=torch.uint8, **d).view(torch.float8_e4m3fn) for _ in range(2))
+    blocks = -(-n // 256)
+    sm, sv = torch.zeros(blocks, **d), torch.zeros(blocks, **d)
+    rng = np.random.default_rng(2)
+    g = torch.from_numpy(rng.normal(size=tail).astype(np.float32)).to(torch.bfloat16)
+    grad[-tail:] = g.cuda()
+    w[-tail:] = 1.0
+    eqb.eqb_adamw_step(eqb.AdamwTensors([w], [grad], [m], [v], exp_avg_scale=[sm], exp_avg_sq_scale=[sv],
+                                        weight_decay=0.1), 1, seed=77, **HYPER)
+    zero = np.zeros(tail, dtype=np.float32)
+    ww, mm, _, r = O.adamw32(zero + 1, g.to(torch.float32).numpy(), zero, zero, 1, weight_decay=0.1, **HYPER)
+    assert np.array_equal(bits_of(w[-tail:]), ww.view(np.int32)) and not w[:4096].any()
+    rnd = O.random32(tail, O.tensor_key(77, 1, 0), n - tail)
+    far = 0
+    for t, x, bits, nz in ((m, mm, rnd & 0xFFFF, False), (v, r, rnd >> 16, True)):
+        codes, _ = O.quantise(x.astype(np.float64), bits, nz)
+        got = t.view(torch.uint8)[-tail:].cpu().numpy().astype(np.int64)
+        assert np.abs(got - codes).max() <= 1
+        far += int((got != codes).sum())
+    assert far <= 2
