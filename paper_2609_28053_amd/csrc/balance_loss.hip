@@ -5,18 +5,45 @@
 
 namespace eqb {
 
-// Sum (maximum) over aligned groups of G lanes, the same in every lane of the group.
-template <int G>
-__device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-  for (int off = 1; off < G; off <<= 1) x += __shfl_xor(x, off);
+// Sum (maximum) over aligned groups of G lanes, the same in every lane of the group: DPP
+// up to 16 lanes, then swaps of 16 and of 32 lanes between two copies.
+template <int G, class F>
+__device__ __forceinline__ float group_fold(float x, F f) {
+  auto dpp = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  if constexpr (G >= 2) x = f(x, dpp(std::integral_constant<int, 0xB1>{}));
+  if constexpr (G >= 4) x = f(x, dpp(std::integral_constant<int, 0x4E>{}));
+  if constexpr (G >= 8) x = f(x, dpp(std::integral_constant<int, 0x141>{}));
+  if constexpr (G >= 16) x = f(x, dpp(std::integral_constant<int, 0x140>{}));
+  if constexpr (G >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (G >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   return x;
 }
 template <int G>
+__device__ __forceinline__ float group_sum(float x) {
+  return group_fold<G>(x, [](float a, float b) { return a + b; });
+}
+template <int G>
 __device__ __forceinline__ float group_max(float x) {
-#pragma unroll
-  for (int off = 1; off < G; off <<= 1) x = fmaxf(x, __shfl_xor(x, off));
-  return x;
+  return group_fold<G>(x, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The partition that holds row t.
+__device__ __forceinline__ int partition_of(const PartTable& pt, int64_t t) {
+  int lo = 0, hi = pt.P - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (pt.off[mid + 1] <= t) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -24,119 +51,157 @@ constexpr float kLog2e = 1.4426950408889634f;
 // lost digits to underflow: the row's probabilities are then those of a softmax.
 constexpr float kTinySum = 0x1p-100f;
 
-// A row's exponentials exp(x - max) over the group's lanes, whole rows of -inf giving 0;
-// returns their sum.
+// A row's exponentials exp(x - max) over the group's lanes, whole rows of -inf giving 0, and
+// their sum; where a row does not take part its terms w and sum d stay as they are.
 template <int G, int N>
-__device__ __forceinline__ float softmax_terms(const float (&x)[N], float (&w)[N]) {
+__device__ __forceinline__ float softmax_where(bool part, const float (&x)[N], float (&w)[N], float d) {
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
-  m = group_max<G>(m);
-  m = fmaxf(m, -3.0e38f);
-  float d = 0.0f;
+  m = fmaxf(group_max<G>(m), -3.0e38f);
+  float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    w[i] = __builtin_amdgcn_exp2f((x[i] - m) * kLog2e);
-    d += w[i];
+    const float v = __builtin_amdgcn_exp2f((x[i] - m) * kLog2e);
+    w[i] = part ? v : w[i];
+    sum += v;
   }
-  return group_sum<G>(d);
+  sum = group_sum<G>(sum);
+  return part ? sum : d;
+}
+template <int G, int N>
+__device__ __forceinline__ float softmax_terms(const float (&x)[N], float (&w)[N]) {
+  return softmax_where<G>(true, x, w, 0.0f);
 }
 
 // ------------------------------------------------------------- the loss --
 // G = E/8 lanes hold a row, 8 experts each.  A lane sums the probabilities of its
 // experts over its rows in binary32; at the end of a block's piece of a group the block
-// adds its lanes' sums, and stores them with its counts.  The block that completes a
-// group (by the group's ticket) adds the pieces in their order in binary64, writes the
-// group's results and sets the ticket back to 0.  Blocks sit on XCDs with an L2 each:
-// pieces pass between them in agent-scope stores and loads, complete (vmcnt) before the
-// ticket is drawn.
-constexpr int kLossThreads = 1024, kLossWaves = kLossThreads / 64;
-constexpr int kLossU = 4;          // rows per lane and step
+// adds its lanes' sums in binary64.  If the group has rows in other blocks too, the blocks
+// hand their pieces over (in binary32) through the workspace: the last of a bunch of
+// neighbours to come, by a ticket, adds theirs, and the last of those adds the sums, each in
+// a fixed order in binary64, and writes the group's results.  Who completes a count sets
+// its ticket back to 0.  Blocks sit on XCDs with an L2 each: pieces pass between them in
+// agent-scope stores and loads, complete (vmcnt) before the ticket is drawn.
+constexpr int kLossThreads = 768, kLossWaves = kLossThreads / 64;
+constexpr int kLossU = 2;          // rows per lane and step
 
 __device__ __forceinline__ uint64_t pack_piece(float prob, int count) {
   return (uint64_t)__float_as_uint(prob) | ((uint64_t)(uint32_t)count << 32);
 }
 
-template <int E, bool kSoftmax>
-__global__ __launch_bounds__(kLossThreads) void balance_loss_kernel(
+template <int E, bool kSoftmax, bool kMask>
+__global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     const uint16_t* __restrict__ z, const int32_t* __restrict__ idx, const uint8_t* __restrict__ valid, int64_t T,
-    int K, const PartTable pt, int64_t rows_per_block, double alpha, const BalanceWorkspace ws, int32_t* load,
+    int K, const PartTable pt, int64_t rows_per_block, int bunch_bits, double alpha, const BalanceWorkspace ws, int32_t* load,
     int32_t* __restrict__ tokens, float* __restrict__ prob, float* __restrict__ loss) {
-  constexpr int G = E / 8, R = 64 / G, ROWS = kLossWaves * R * kLossU;
+  constexpr int G = E / 8, R = 64 / G;
+  constexpr uint32_t ROWS = kLossWaves * R * kLossU;
   __shared__ float sh_sum[kLossWaves][E];
-  __shared__ int32_t sh_cnt[E];
+  // counts in 256/E copies, a lane adding to copy lane % copies: with one, the 64 lanes of
+  // a wave queue on the few counters of a small E
+  __shared__ int32_t sh_cnt[kNBins / E][E];
   __shared__ int32_t sh_tokens, sh_ticket;
   __shared__ double sh_d[kLossThreads];
   __shared__ int64_t sh_c[kLossThreads];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane % G, rr = lane / G;
   if (blockIdx.x == 0) {           // groups without tokens
-    for (int p = 0; p < pt.P; ++p) {
-      if (pt.off[p + 1] > pt.off[p]) continue;
-      if (tid < E) {
-        prob[p * E + tid] = 0.0f;
-        if (idx || T == 0) load[p * E + tid] = 0;
+    for (int q = tid >> 6; q < pt.P; q += kLossWaves) {
+      if (pt.off[q + 1] > pt.off[q]) continue;
+      for (int e = lane; e < E; e += 64) {
+        prob[q * E + e] = 0.0f;
+        if (idx || T == 0) load[q * E + e] = 0;
       }
-      if (tid == 0) {
-        tokens[p] = 0;
-        loss[p] = 0.0f;
+      if (lane == 0) {
+        tokens[q] = 0;
+        loss[q] = 0.0f;
       }
     }
   }
-  if (tid < E) sh_cnt[tid] = 0;
+  if (tid < kNBins) (&sh_cnt[0][0])[tid] = 0;
   if (tid == 0) sh_tokens = 0;
   int64_t r0, r1;
   block_rows(T, rows_per_block, &r0, &r1);
-  int p = 0;
   for (int64_t s0 = r0; s0 < r1;) {
-    while (p < pt.P - 1 && pt.off[p + 1] <= s0) ++p;
+    const int p = partition_of(pt, s0);
     const int64_t s1 = pt.off[p + 1] < r1 ? pt.off[p + 1] : r1;
     __syncthreads();
-    if (idx) {
-      for (int64_t i = s0 * K + tid; i < s1 * K; i += kLossThreads) {
-        const int e = idx[i];
-        if (e >= 0 && e < E && (!valid || valid[i / K])) atomicAdd(&sh_cnt[e], 1);
-      }
-    }
     float acc[8] = {};
     int n = 0;
-    for (int64_t base = s0; base < s1; base += ROWS) {
-      uint4 zw[kLossU];
-      bool on[kLossU];
+    // pieces of at most kSegMax rows: 32-bit offsets from their bases
+    for (int64_t c0 = s0; c0 < s1; c0 += kSegMax) {
+      const int64_t cu = wave_uniform(c0);
+      const uint16_t* zc = z + cu * E;
+      const uint8_t* vc = kMask ? valid + cu : nullptr;
+      const uint32_t rows = (uint32_t)(s1 - c0 < kSegMax ? s1 - c0 : kSegMax);
+      // rows past the last one read the last one, and count as 0
+      auto row_of = [&](uint32_t base, int u) { return base + (uint32_t)((u * kLossWaves + wave) * R + rr); };
+      auto fetch = [&](uint32_t base, uint4 (&zw)[kLossU], bool (&on)[kLossU]) {
 #pragma unroll
-      for (int u = 0; u < kLossU; ++u) {
-        const int64_t t = base + (u * kLossWaves + wave) * R + rr;
-        on[u] = t < s1 && (!valid || valid[t]);
-        zw[u] = make_uint4(0, 0, 0, 0);
-        if (on[u]) zw[u] = *reinterpret_cast<const uint4*>(z + t * E + 8 * g);
-      }
-#pragma unroll
-      for (int u = 0; u < kLossU; ++u) {
-        const float x[8] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y),
-                            bf16_lo(zw[u].z), bf16_hi(zw[u].z), bf16_lo(zw[u].w), bf16_hi(zw[u].w)};
-        float w[8], d = 0.0f;
-        if (kSoftmax) {
-          d = softmax_terms<G>(x, w);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            w[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * -kLog2e));
-            d += w[i];
-          }
-          d = group_sum<G>(d);
-          const bool tiny = on[u] && d < kTinySum;
-          if (__any(tiny)) {
-            float ws_[8];
-            const float ds = softmax_terms<G>(x, ws_);
-            d = tiny ? ds : d;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = tiny ? ws_[i] : w[i];
-          }
+        for (int u = 0; u < kLossU; ++u) {
+          const uint32_t t = row_of(base, u), tc = t < rows ? t : rows - 1;
+          zw[u] = at<const uint4>(zc, (tc * E + 8 * g) * 2u);
+          on[u] = t < rows && (!kMask || at<const uint8_t>(vc, tc) != 0);
         }
-        const float inv = on[u] && d != 0.0f ? 1.0f / d : 0.0f;
+      };
+      uint4 zn[kLossU];
+      bool next[kLossU];
+      fetch(0, zn, next);
+      if (idx) {
+        const int32_t* ic = idx + cu * K;
+        const uint32_t pairs = rows * (uint32_t)K;
+        for (uint32_t i = tid; i < pairs; i += 4 * kLossThreads) {
+          int e[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(w[i], inv, acc[i]);
-        n += on[u] && g == 0;
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t k = i + j * kLossThreads;
+            e[j] = -1;
+            if (k < pairs && (!kMask || vc[k / (uint32_t)K])) e[j] = ic[k];
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (e[j] >= 0 && e[j] < E) atomicAdd(&sh_cnt[lane % (kNBins / E)][e[j]], 1);
+        }
+      }
+      for (uint32_t base = 0; base < rows; base += ROWS) {
+        uint4 zw[kLossU];
+        bool on[kLossU];
+#pragma unroll
+        for (int u = 0; u < kLossU; ++u) {
+          zw[u] = zn[u];
+          on[u] = next[u];
+        }
+        fetch(base + ROWS, zn, next);
+#pragma unroll
+        for (int u = 0; u < kLossU; ++u) {
+          if (kMask && !on[u]) zw[u] = make_uint4(0, 0, 0, 0);      // whatever a masked token holds
+          const float x[8] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y),
+                              bf16_lo(zw[u].z), bf16_hi(zw[u].z), bf16_lo(zw[u].w), bf16_hi(zw[u].w)};
+          float w[8], d = 0.0f;
+          if (kSoftmax) {
+            d = softmax_terms<G>(x, w);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              w[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * -kLog2e));
+              d += w[i];
+            }
+            d = group_sum<G>(d);
+            const bool tiny = d < kTinySum;
+            if (__any(tiny)) {
+              // the logits unpacked again, rather than kept for this in registers
+              asm volatile("" : "+v"(zw[u].x), "+v"(zw[u].y), "+v"(zw[u].z), "+v"(zw[u].w));
+              const float y[8] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y),
+                                  bf16_lo(zw[u].z), bf16_hi(zw[u].z), bf16_lo(zw[u].w), bf16_hi(zw[u].w)};
+              d = softmax_where<G>(tiny, y, w, d);
+            }
+          }
+          const float inv = on[u] && d != 0.0f ? __builtin_amdgcn_rcpf(d) : 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(w[i], inv, acc[i]);
+          if (kMask) n += on[u] && g == 0;
+        }
       }
     }
     // the block's sums: over the rows of a wave, then over the waves
@@ -146,92 +211,147 @@ __global__ __launch_bounds__(kLossThreads) void balance_loss_kernel(
       for (int off = G; off < 64; off <<= 1) acc[i] += __shfl_xor(acc[i], off);
       if (lane < G) sh_sum[wave][8 * g + i] = acc[i];
     }
-    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
-    if (lane == 0 && n) atomicAdd(&sh_tokens, n);
-    __syncthreads();
-    const int64_t piece = (int64_t)blockIdx.x + p;
-    if (tid < E) {
-      double s = 0.0;
-      for (int w = 0; w < kLossWaves; ++w) s += (double)sh_sum[w][tid];
-      __hip_atomic_store(ws.pieces + piece * E + tid, pack_piece((float)s, sh_cnt[tid]), __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
-      sh_cnt[tid] = 0;
+    if (kMask) {
+      for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
+      if (lane == 0 && n) atomicAdd(&sh_tokens, n);
     }
-    if (tid == 0) {
-      __hip_atomic_store(ws.tokens + piece, sh_tokens, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      sh_tokens = 0;
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const int first = (int)(pt.off[p] / rows_per_block), last = (int)((pt.off[p + 1] - 1) / rows_per_block);
-    if (tid == 0) sh_ticket = __hip_atomic_fetch_add(ws.tickets + p, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (sh_ticket == last - first) {
-      // every piece of the group is there
-      constexpr int J = kLossThreads / E;
-      const int e = tid % E, j = tid / E;
-      double s = 0.0;
-      int64_t c = 0;
-      for (int b = first + j; b <= last; b += J) {
-        const uint64_t v = __hip_atomic_load(ws.pieces + (int64_t)(b + p) * E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s += (double)__uint_as_float((uint32_t)v);
-        c += (int)(v >> 32);
+    double sum = 0.0;
+    int64_t count = 0, nv = pt.off[p + 1] - pt.off[p];
+    if (tid < E) {
+      for (int w = 0; w < kLossWaves; ++w) sum += (double)sh_sum[w][tid];
+      for (int c = 0; c < kNBins / E; ++c) {
+        count += sh_cnt[c][tid];
+        sh_cnt[c][tid] = 0;
       }
-      sh_d[tid] = s;
-      sh_c[tid] = c;
-      int64_t nv = 0;
-      if (valid) {
-        for (int b = first + lane; b <= last; b += 64)
-          nv += __hip_atomic_load(ws.tokens + b + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        for (int off = 32; off > 0; off >>= 1) nv += (int64_t)__shfl_xor((unsigned long long)nv, off);
-      } else {
-        nv = pt.off[p + 1] - pt.off[p];
+    }
+    if (kMask) nv = sh_tokens;
+    bool whole = true;             // sum, count and nv are the group's
+    if (first < last) {
+      // Pieces of a bunch of neighbouring blocks are summed by the last of these to come, and
+      // the bunches' sums by the last to bring one.  A bunch of a group has place bunch + p:
+      // both only grow from piece to piece.
+      const int piece = (int)blockIdx.x + p, bunch = piece >> bunch_bits;
+      const int bunch0 = (first + p) >> bunch_bits, bunch1 = (last + p) >> bunch_bits;
+      const int i0 = bunch == bunch0 ? first + p : bunch << bunch_bits;
+      const int i1 = bunch == bunch1 ? last + p : ((bunch + 1) << bunch_bits) - 1;
+      auto hand_over = [&](uint64_t* to, int32_t* to_tokens, int at, int32_t* ticket, int others) {
+        if (tid < E)
+          __hip_atomic_store(to + (int64_t)at * E + tid, pack_piece((float)sum, (int)count), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
+        if (kMask && tid == 0)
+          __hip_atomic_store(to_tokens + at, (int)nv, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+          const int before = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (before == others) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          sh_ticket = before;
+        }
+        __syncthreads();
+        return sh_ticket == others;
+      };
+      auto collect = [&](const uint64_t* from, const int32_t* from_tokens, int lo, int hi) {
+        constexpr int J = kLossThreads / E;
+        const int e = tid % E, j = tid / E;
+        sum = 0.0;
+        count = 0;
+        for (int b0 = lo + j; b0 <= hi; b0 += 8 * J) {
+          uint64_t v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            v[i] = b0 + i * J <= hi ? __hip_atomic_load(from + (int64_t)(b0 + i * J) * E + e, __ATOMIC_RELAXED,
+                                                        __HIP_MEMORY_SCOPE_AGENT) : 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            sum += (double)__uint_as_float((uint32_t)v[i]);
+            count += (int)(v[i] >> 32);
+          }
+        }
+        sh_d[tid] = sum;
+        sh_c[tid] = count;
+        if (kMask) {
+          nv = 0;
+          for (int b = lo + lane; b <= hi; b += 64)
+            nv += __hip_atomic_load(from_tokens + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          for (int off = 32; off > 0; off >>= 1) nv += (int64_t)__shfl_xor((unsigned long long)nv, off);
+        }
+        __syncthreads();
+        if (tid < E) {
+#pragma unroll 2
+          for (int q = 1; q < J; ++q) {
+            sum += sh_d[q * E + tid];
+            count += sh_c[q * E + tid];
+          }
+        }
+        __syncthreads();
+      };
+      whole = hand_over(ws.pieces, ws.tokens, piece, ws.bunch_tickets + bunch + p, i1 - i0);
+      if (whole) {
+        collect(ws.pieces, ws.tokens, i0, i1);
+        if (bunch0 < bunch1) {
+          whole = hand_over(ws.bunches, ws.bunch_tokens, bunch + p, ws.tickets + p, bunch1 - bunch0);
+          if (whole) collect(ws.bunches, ws.bunch_tokens, bunch0 + p, bunch1 + p);
+        }
       }
-      __syncthreads();
+    }
+    if (whole) {
       double part = 0.0;
       if (tid < E) {
-        for (int q = 1; q < J; ++q) {
-          s += sh_d[q * E + tid];
-          c += sh_c[q * E + tid];
-        }
-        if (!idx) c = load[(int64_t)p * E + tid];
-        const double mean = nv > 0 ? s / (double)nv : 0.0;
+        if (!idx) count = load[(int64_t)p * E + tid];
+        else load[(int64_t)p * E + tid] = (int32_t)count;
+        const double mean = nv > 0 ? sum / (double)nv : 0.0;
         prob[(int64_t)p * E + tid] = (float)mean;
-        if (idx) load[(int64_t)p * E + tid] = (int32_t)c;
-        part = nv > 0 ? (double)c * E / ((double)K * (double)nv) * mean : 0.0;
+        part = nv > 0 ? (double)count * E / ((double)K * (double)nv) * mean : 0.0;
+        sh_d[tid] = part;
       }
-      __syncthreads();
-      sh_d[tid] = part;
       __syncthreads();
       if (tid < 64) {
-        for (int q = tid + 64; q < E; q += 64) part += sh_d[q];
+        part = lane < E ? part : 0.0;
+        for (int q = lane + 64; q < E; q += 64) part += sh_d[q];
         for (int off = 32; off > 0; off >>= 1) part += __shfl_xor(part, off);
-        if (tid == 0) {
+        if (lane == 0) {
           loss[p] = (float)(alpha * part);
           tokens[p] = (int32_t)nv;
-          __hip_atomic_store(ws.tickets + p, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          sh_tokens = 0;
         }
       }
+    } else if (tid == 0) {
+      sh_tokens = 0;
     }
     s0 = s1;
   }
 }
 
-template <int E>
-static void launch_loss_e(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {
+template <int E, bool kSoftmax, bool kMask>
+static void launch_loss_as(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {
   int blocks;
   int64_t rpb;
-  grid_for(a.T, kLossWaves * (512 / E) * kLossU, 1, &blocks, &rpb);
+  // One block for 32,768 logits, blocks of at least 16,384 beyond: 4,096 rows of E = 8 take
+  // 8.8 us in one block and 12.4 in two, 16,384 rows of E = 64 8.7 in 64 and 9.4 in 32.
+  grid_for(a.T, a.T * E <= 32768 ? 32768 / E : 16384 / E, 2, &blocks, &rpb);
   if (blocks > kBalanceBlocks) {
     rpb = (a.T + kBalanceBlocks - 1) / kBalanceBlocks;
     blocks = (int)((a.T + rpb - 1) / rpb);
   }
-  if (a.softmax)
-    balance_loss_kernel<E, true><<<blocks, kLossThreads, 0, s>>>(a.z, a.idx, a.valid, a.T, a.K, a.pt, rpb, a.alpha, ws,
-                                                                a.load, a.tokens, a.prob, a.loss);
-  else
-    balance_loss_kernel<E, false><<<blocks, kLossThreads, 0, s>>>(a.z, a.idx, a.valid, a.T, a.K, a.pt, rpb, a.alpha,
-                                                                 ws, a.load, a.tokens, a.prob, a.loss);
+  // Bunches pay where one block would read more than 256 KiB of pieces: 147,456 rows of E =
+  // 256 in 512 blocks take 39.5 us without and 23.8 with them, 1,000,003 rows of E = 8 20.1
+  // without and 23.7 with.  (10 bits: all blocks are one bunch.)
+  const int bunch_bits = (int64_t)blocks * E * (int64_t)sizeof(uint64_t) > (256 << 10) ? kBunchBits : 10;
+  static_assert(kBalanceBlocks + EQB_MAX_PARTITIONS <= 1 << 10, "one bunch");
+  balance_loss_kernel<E, kSoftmax, kMask><<<blocks, kLossThreads, 0, s>>>(
+      a.z, a.idx, a.valid, a.T, a.K, a.pt, rpb, bunch_bits, a.alpha, ws, a.load, a.tokens, a.prob, a.loss);
+}
+template <int E>
+static void launch_loss_e(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {
+  if (a.softmax) {
+    if (a.valid) launch_loss_as<E, true, true>(a, ws, s);
+    else launch_loss_as<E, true, false>(a, ws, s);
+  } else {
+    if (a.valid) launch_loss_as<E, false, true>(a, ws, s);
+    else launch_loss_as<E, false, false>(a, ws, s);
+  }
 }
 
 eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {
@@ -253,111 +373,180 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // are scattered into a per-wave LDS row of zeros, read back 4 at a time, and their
 // places zeroed again.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;
+constexpr int kGradU = 3;          // rows per lane and step
+constexpr int kGradWavesPerSimd = 6;
+constexpr int kGradBlocksPerCu = kGradWavesPerSimd * 256 / kGradThreads;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-template <int E, bool kSoftmax, bool kRouter>
-__global__ __launch_bounds__(kGradThreads) void balance_backward_kernel(
+// What goes with the loss's gradient: nothing, the router backward where a lane of a
+// row's group holds at most one of its K pairs, or the router backward with any K (and
+// the injection without pairs).
+enum { kAlone, kOnePair, kAnyPairs };
+
+template <int E, bool kSoftmax, int kRouter>
+__global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backward_kernel(
     const uint16_t* __restrict__ z, const int32_t* __restrict__ load, const int32_t* __restrict__ tokens,
     const float* __restrict__ grad_loss, const int32_t* __restrict__ idx, const float* __restrict__ gs,
     const float* __restrict__ inj, const uint8_t* __restrict__ valid, int64_t T, int K, const PartTable pt,
     int64_t rows_per_block, double alpha, float* __restrict__ grad_z) {
-  constexpr int G = E / 4, R = 64 / G, ROWS = kGradWaves * R;
-  __shared__ __align__(16) float sh_g[kGradWaves][R][E];
+  constexpr int G = E / 4, R = 64 / G;
+  constexpr uint32_t ROWS = kGradWaves * R * kGradU;
+  __shared__ __align__(16) float sh_g[kRouter == kAlone ? 1 : kGradWaves][kGradU][R][E];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane % G, rr = lane / G;
-  float* my = &sh_g[wave][rr][0];
-  if (kRouter && idx) {
+  float* my = &sh_g[kRouter == kAlone ? 0 : wave][0][rr][0];      // row u of this lane: my + u * R * E
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  auto place = [&](int u) -> f32x4& { return *reinterpret_cast<f32x4*>(my + u * R * E + 4 * g); };
+  if (kRouter != kAlone) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) my[4 * g + i] = 0.0f;
+    for (int u = 0; u < kGradU; ++u) place(u) = zero;
     lds_wave_sync();
   }
   int64_t r0, r1;
   block_rows(T, rows_per_block, &r0, &r1);
-  for_each_segment(r0, r1, pt, [&](int p, int64_t s0, int64_t s1) {
+  for (int64_t s0 = r0, s1; s0 < r1; s0 = s1) {
+    const int p = partition_of(pt, s0);
+    s1 = pt.off[p + 1] < r1 ? pt.off[p + 1] : r1;
+    if (s1 - s0 > kSegMax) s1 = s0 + kSegMax;
+    // a segment holds at most kSegMax rows: 32-bit byte offsets from its bases
+    const int64_t su = wave_uniform(s0);
+    const uint16_t* seg_z = z + su * E;
+    const int32_t* seg_idx = idx + su * K;
+    const float* seg_gs = gs + su * K;
+    const uint8_t* seg_valid = valid + su;
+    float* seg_gz = grad_z + su * E;
+    const uint32_t n = (uint32_t)(s1 - s0);
     const int nv = tokens[p];
     const double c0 = nv > 0 ? alpha * (double)grad_loss[p] * E / ((double)K * (double)nv * (double)nv) : 0.0;
-    float C[4], d0[4];
+    f32x4 C, d0 = zero;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       C[i] = (float)(c0 * (double)load[(int64_t)p * E + 4 * g + i]);
-      d0[i] = kRouter && inj ? inj[(int64_t)p * E + 4 * g + i] : 0.0f;
+      if (kRouter != kAlone && inj) d0[i] = inj[(int64_t)p * E + 4 * g + i];
     }
-    for (int64_t base = s0; base < s1; base += ROWS) {
-      const int64_t t = base + wave * R + rr;
-      const bool in = t < s1, on = in && (!valid || valid[t]);
-      uint2 zw = make_uint2(0, 0);
-      if (on) zw = *reinterpret_cast<const uint2*>(z + t * E + 4 * g);
-      const float x[4] = {bf16_lo(zw.x), bf16_hi(zw.x), bf16_lo(zw.y), bf16_hi(zw.y)};
-      if (kRouter && idx) {
-        if (on)
-          for (int k = g; k < K; k += G) {
-            const int e = idx[t * K + k];
-            if (e >= 0 && e < E) my[e] = gs[t * K + k];
+    auto row_of = [&](uint32_t base, int u) -> uint32_t { return base + (uint32_t)((wave * kGradU + u) * R + rr); };
+    // logits, mask and this lane's pair of its rows at step base
+    auto fetch = [&](uint32_t base, u32x2 (&zw)[kGradU], bool (&on)[kGradU], int (&e)[kGradU], float (&gv)[kGradU]) {
+#pragma unroll
+      for (int u = 0; u < kGradU; ++u) {
+        const uint32_t t = row_of(base, u);
+        zw[u] = u32x2{0, 0};
+        e[u] = -1;
+        gv[u] = 0.0f;
+        on[u] = false;
+        if (t < n) {
+          on[u] = !valid || at<const uint8_t>(seg_valid, t) != 0;
+          zw[u] = __builtin_nontemporal_load(&at<const u32x2>(seg_z, (t * E + 4 * g) * 2u));
+          if (kRouter == kOnePair && g < K) {
+            e[u] = at<const int32_t>(seg_idx, (t * K + g) * 4u);
+            gv[u] = at<const float>(seg_gs, (t * K + g) * 4u);
           }
+        }
+      }
+    };
+    u32x2 zn[kGradU];
+    bool onn[kGradU];
+    int en[kGradU];
+    float gn[kGradU];
+    fetch(0, zn, onn, en, gn);
+    for (uint32_t base = 0; base < n; base += ROWS) {
+      u32x2 zw[kGradU];
+      bool on[kGradU];
+      int ec[kGradU];
+      float gc[kGradU];
+#pragma unroll
+      for (int u = 0; u < kGradU; ++u) {
+        on[u] = onn[u];
+        // whatever a masked token holds
+        zw[u] = on[u] ? zn[u] : u32x2{0, 0};
+        ec[u] = on[u] ? en[u] : -1;
+        gc[u] = gn[u];
+      }
+      if (base + ROWS < n) fetch(base + ROWS, zn, onn, en, gn);
+      // scatter the rows' mixture gradients
+      if (kRouter != kAlone) {
+#pragma unroll
+        for (int u = 0; u < kGradU; ++u) {
+          if (kRouter == kOnePair) {
+            if (ec[u] >= 0 && ec[u] < E) my[u * R * E + ec[u]] = gc[u];
+          } else if (idx && on[u]) {
+            const uint32_t t = row_of(base, u);
+            for (int k = g; k < K; k += G) {
+              const int e = at<const int32_t>(seg_idx, (t * K + k) * 4u);
+              if (e >= 0 && e < E) my[u * R * E + e] = at<const float>(seg_gs, (t * K + k) * 4u);
+            }
+          }
+        }
         lds_wave_sync();
       }
-      float w[4], q[4], sd[4], d;
-      if (!kSoftmax || kRouter) {
+#pragma unroll
+      for (int u = 0; u < kGradU; ++u) {
+        const uint32_t t = row_of(base, u);
+        const float x[4] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y)};
+        float w[4], q[4], sd[4], d;
+        if (!kSoftmax || kRouter != kAlone) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fabsf(x[i]) * -kLog2e);
+            const float r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+            w[i] = x[i] >= 0.0f ? r : er;
+            q[i] = x[i] >= 0.0f ? er : r;
+            sd[i] = er * r;
+          }
+        }
+        if (kSoftmax) {
+          d = softmax_terms<G>(x, w);
+        } else {
+          d = group_sum<G>(w[0] + w[1] + (w[2] + w[3]));
+          const bool tiny = d < kTinySum;
+          if (__any(tiny)) d = softmax_where<G>(tiny, x, w, d);
+        }
+        const float inv = d != 0.0f ? __builtin_amdgcn_rcpf(d) : 0.0f;
+        float c = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(fabsf(x[i]) * -kLog2e);
-          const float r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
-          w[i] = x[i] >= 0.0f ? r : er;
-          q[i] = x[i] >= 0.0f ? er : r;
-          sd[i] = er * r;
+          w[i] *= inv;
+          c = __builtin_fmaf(w[i], C[i], c);
         }
-      }
-      if (kSoftmax) {
-        d = softmax_terms<G>(x, w);
-      } else {
-        d = group_sum<G>(w[0] + w[1] + (w[2] + w[3]));
-        const bool tiny = on && d < kTinySum;
-        if (__any(tiny)) {
-          float v[4];
-          const float dv = softmax_terms<G>(x, v);
-          d = tiny ? dv : d;
+        c = group_sum<G>(c);
+        const f32x4 gm = kRouter != kAlone ? place(u) + d0 : zero;
+        f32x4 o;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = tiny ? v[i] : w[i];
+        for (int i = 0; i < 4; ++i) {
+          float a = w[i] * (C[i] - c);
+          if (!kSoftmax) a *= q[i];
+          if (kRouter != kAlone) a = __builtin_fmaf(gm[i], sd[i], a);
+          o[i] = on[u] ? a : 0.0f;
         }
+        if (t < n) __builtin_nontemporal_store(o, &at<f32x4>(seg_gz, (t * E + 4 * g) * 4u));
       }
-      const float inv = d != 0.0f ? 1.0f / d : 0.0f;
-      float c = 0.0f;
+      if (kRouter != kAlone) {
+        lds_wave_sync();          // every place has been read
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] *= inv;
-        c = __builtin_fmaf(w[i], C[i], c);
-      }
-      c = group_sum<G>(c);
-      float4 o;
-      float* po = &o.x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a = w[i] * (C[i] - c);
-        if (!kSoftmax) a *= q[i];
-        if (kRouter) a = __builtin_fmaf((idx ? my[4 * g + i] : 0.0f) + d0[i], sd[i], a);
-        po[i] = on ? a : 0.0f;
-      }
-      if (in) *reinterpret_cast<float4*>(grad_z + t * E + 4 * g) = o;
-      if (kRouter && idx) {
-        lds_wave_sync();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) my[4 * g + i] = 0.0f;
-        lds_wave_sync();
+        for (int u = 0; u < kGradU; ++u) {
+          if (kRouter == kAnyPairs) place(u) = zero;
+          else if (ec[u] >= 0 && ec[u] < E) my[u * R * E + ec[u]] = 0.0f;
+        }
+        lds_wave_sync();          // the next step scatters into zeros
       }
     }
-  });
+  }
 }
 
-template <int E, bool kSoftmax>
-static void launch_backward_es(const BalanceArgs& a, hipStream_t s) {
+template <int E, bool kSoftmax, int kRouter>
+static void launch_backward_as(const BalanceArgs& a, hipStream_t s) {
   int blocks;
   int64_t rpb;
-  grid_for(a.T, kGradWaves * (256 / E), 4, &blocks, &rpb);
-  if (a.idx || a.inj)
-    balance_backward_kernel<E, kSoftmax, true><<<blocks, kGradThreads, 0, s>>>(
-        a.z, a.load, a.tokens, a.grad_loss, a.idx, a.grad_score, a.inj, a.valid, a.T, a.K, a.pt, rpb, a.alpha, a.grad_z);
-  else
-    balance_backward_kernel<E, kSoftmax, false><<<blocks, kGradThreads, 0, s>>>(
-        a.z, a.load, a.tokens, a.grad_loss, a.idx, a.grad_score, a.inj, a.valid, a.T, a.K, a.pt, rpb, a.alpha, a.grad_z);
+  grid_for(a.T, kGradWaves * (256 / E) * kGradU, kGradBlocksPerCu, &blocks, &rpb);
+  balance_backward_kernel<E, kSoftmax, kRouter><<<blocks, kGradThreads, 0, s>>>(
+      a.z, a.load, a.tokens, a.grad_loss, a.idx, a.grad_score, a.inj, a.valid, a.T, a.K, a.pt, rpb, a.alpha, a.grad_z);
+}
+template <int E, bool kSoftmax>
+static void launch_backward_es(const BalanceArgs& a, hipStream_t s) {
+  if (!a.idx && !a.inj) launch_backward_as<E, kSoftmax, kAlone>(a, s);
+  else if (a.idx && a.K <= E / 4) launch_backward_as<E, kSoftmax, kOnePair>(a, s);
+  else launch_backward_as<E, kSoftmax, kAnyPairs>(a, s);
 }
 template <int E>
 static void launch_backward_e(const BalanceArgs& a, hipStream_t s) {

@@ -135,25 +135,34 @@ struct BalanceArgs {
   PartTable pt;
 };
 
-// Working memory of the balance loss: a ticket per group (zero before and after a call),
-// then the blocks' pieces.  A block's rows overlap consecutive groups, so block b's piece
-// of group p has place b + p, its own alone.
+// Working memory of the balance loss: the tickets (zero before and after a call), then the
+// blocks' pieces and the sums of bunches of them.  A block's rows overlap consecutive
+// groups, so block b's piece of group p has place b + p, its own alone.
 constexpr int kBalanceBlocks = 512;          // most blocks of a launch
+constexpr int kBunchBits = 4;                // 16 pieces
 struct BalanceWorkspace {
-  int32_t* tickets;     // [EQB_MAX_PARTITIONS]
-  int32_t* tokens;      // [kBalanceBlocks + P]
-  uint64_t* pieces;     // [kBalanceBlocks + P, E]: binary32 sum of probabilities, count
+  int32_t* tickets;         // [EQB_MAX_PARTITIONS]
+  int32_t* bunch_tickets;   // [bunches]
+  int32_t* tokens;          // [kBalanceBlocks + P]
+  int32_t* bunch_tokens;    // [bunches], ((kBalanceBlocks + P) >> kBunchBits) + P + 1 of them
+  uint64_t* pieces;         // [kBalanceBlocks + P, E]: binary32 sum of probabilities, count
+  uint64_t* bunches;        // [bunches, E]
 };
 inline size_t balance_workspace(void* base, int E, int P, BalanceWorkspace* w) {
-  const size_t pieces = (size_t)kBalanceBlocks + P;
-  const size_t tickets = align256(EQB_MAX_PARTITIONS * sizeof(int32_t)), tokens = align256(pieces * sizeof(int32_t));
+  const size_t pieces = (size_t)kBalanceBlocks + P, bunches = (pieces >> kBunchBits) + P + 1;
+  const size_t at1 = align256(EQB_MAX_PARTITIONS * sizeof(int32_t)), at2 = at1 + align256(bunches * sizeof(int32_t));
+  const size_t at3 = at2 + align256(pieces * sizeof(int32_t)), at4 = at3 + align256(bunches * sizeof(int32_t));
+  const size_t at5 = at4 + align256(pieces * E * sizeof(uint64_t));
   if (base && w) {
     char* p = static_cast<char*>(base);
     w->tickets = reinterpret_cast<int32_t*>(p);
-    w->tokens = reinterpret_cast<int32_t*>(p + tickets);
-    w->pieces = reinterpret_cast<uint64_t*>(p + tickets + tokens);
+    w->bunch_tickets = reinterpret_cast<int32_t*>(p + at1);
+    w->tokens = reinterpret_cast<int32_t*>(p + at2);
+    w->bunch_tokens = reinterpret_cast<int32_t*>(p + at3);
+    w->pieces = reinterpret_cast<uint64_t*>(p + at4);
+    w->bunches = reinterpret_cast<uint64_t*>(p + at5);
   }
-  return tickets + tokens + align256(pieces * E * sizeof(uint64_t));
+  return at5 + align256(bunches * E * sizeof(uint64_t));
 }
 eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s);
 eqb_status launch_balance_backward(const BalanceArgs& a, hipStream_t s);

@@ -63,12 +63,22 @@ __global__ __launch_bounds__(kPlanThreads) void dispatch_rank_kernel(const int32
     if (e >= 0 && e < E) atomicAdd(&sh_cnt[wave][e], 1);
   }
   if (counts) {
+    // eight loads in flight: one at a time their latency was 15 of the kernel's 20 us at
+    // 885,000 pairs
     int before = 0, total = 0;
     const int e = tid % E, step = kPlanThreads / E;
-    for (int b = tid / E; b < (int)gridDim.x; b += step) {
-      const int c = counts[b * E + e];
-      total += c;
-      before += b < (int)blockIdx.x ? c : 0;
+    for (int b0 = tid / E; b0 < (int)gridDim.x; b0 += 8 * step) {
+      int c[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int b = b0 + j * step;
+        c[j] = b < (int)gridDim.x ? counts[b * E + e] : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        total += c[j];
+        before += b0 + j * step < (int)blockIdx.x ? c[j] : 0;
+      }
     }
     atomicAdd(&sh_before[e], before);
     atomicAdd(&sh_total[e], total);

@@ -156,8 +156,14 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, numel=None, name="tensor"):
     return ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
+        # the current stream's handle without a torch.cuda.Stream around it (0.2 us instead of 3)
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return ctypes.c_void_p(_raw_stream(torch._C._cuda_getDevice()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
