@@ -209,6 +209,36 @@ __device__ __forceinline__ uint64_t group_max_u64(uint64_t m) {
   return m;
 }
 
+// Sum (maximum) over aligned groups of G lanes, the same in every lane of the group: DPP
+// up to 16 lanes, then swaps of 16 and of 32 lanes between two copies.
+template <int G, class F>
+__device__ __forceinline__ float group_fold(float x, F f) {
+  auto dpp = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  if constexpr (G >= 2) x = f(x, dpp(std::integral_constant<int, 0xB1>{}));
+  if constexpr (G >= 4) x = f(x, dpp(std::integral_constant<int, 0x4E>{}));
+  if constexpr (G >= 8) x = f(x, dpp(std::integral_constant<int, 0x141>{}));
+  if constexpr (G >= 16) x = f(x, dpp(std::integral_constant<int, 0x140>{}));
+  if constexpr (G >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (G >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  return x;
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float x) {
+  return group_fold<G>(x, [](float a, float b) { return a + b; });
+}
+template <int G>
+__device__ __forceinline__ float group_max(float x) {
+  return group_fold<G>(x, [](float a, float b) { return fmaxf(a, b); });
+}
+
 // ------------------------------------------------------- float keys --
 // Routing keys are binary32 bit patterns kept in int registers and ordered
 // as floats.  A key is finite or the sentinel -inf, never NaN, and the keys

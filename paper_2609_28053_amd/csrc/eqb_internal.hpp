@@ -181,6 +181,7 @@ struct RowArgs {
   int K, H, dtype;
   void* out;
   float* grad_weight;
+  bool near = false;      // neighbouring tokens on one XCD
 };
 eqb_status launch_dispatch(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine(const RowArgs& a, hipStream_t s);

@@ -63,25 +63,33 @@ __global__ __launch_bounds__(kPlanThreads) void dispatch_rank_kernel(const int32
     if (e >= 0 && e < E) atomicAdd(&sh_cnt[wave][e], 1);
   }
   if (counts) {
-    // eight loads in flight: one at a time their latency was 15 of the kernel's 20 us at
-    // 885,000 pairs
-    int before = 0, total = 0;
-    const int e = tid % E, step = kPlanThreads / E;
-    for (int b0 = tid / E; b0 < (int)gridDim.x; b0 += 8 * step) {
-      int c[8];
+    // a row of counts by E/4 threads, 16 bytes each and four rows in flight: with one
+    // count a load their latency was most of the kernel's time
+    const int q = tid % (E / 4), step = 4 * kPlanThreads / E;
+    int before[4] = {}, total[4] = {};
+    for (int b0 = tid / (E / 4); b0 < (int)gridDim.x; b0 += 4 * step) {
+      int4 c[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 4; ++j) {
         const int b = b0 + j * step;
-        c[j] = b < (int)gridDim.x ? counts[b * E + e] : 0;
+        c[j] = b < (int)gridDim.x ? *reinterpret_cast<const int4*>(counts + b * E + 4 * q) : make_int4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        total += c[j];
-        before += b0 + j * step < (int)blockIdx.x ? c[j] : 0;
+      for (int j = 0; j < 4; ++j) {
+        const int in = b0 + j * step < (int)blockIdx.x ? -1 : 0;
+        const int v[4] = {c[j].x, c[j].y, c[j].z, c[j].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          total[i] += v[i];
+          before[i] += v[i] & in;
+        }
       }
     }
-    atomicAdd(&sh_before[e], before);
-    atomicAdd(&sh_total[e], total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (before[i]) atomicAdd(&sh_before[4 * q + i], before[i]);
+      if (total[i]) atomicAdd(&sh_total[4 * q + i], total[i]);
+    }
   }
   __syncthreads();
   if (!counts && tid < E) {       // one block: its own counts are all
@@ -154,7 +162,7 @@ eqb_status launch_dispatch_plan(const int32_t* idx, int64_t N, int E, int32_t* o
 
 // ------------------------------------------------------------- the rows --
 // Rows move in pieces of 16 bytes at the alignment of one element (gfx950's global
-// loads and stores take any address), a row's last elements one at a time.
+// loads and stores take any address).  All of it is bound by memory.
 template <class T>
 struct Piece {
   static constexpr int n = 16 / sizeof(T);
@@ -165,179 +173,332 @@ struct Piece {
 struct Bf16 {
   typedef uint16_t raw;
   static __device__ __forceinline__ float to_f(raw x) { return __uint_as_float((uint32_t)x << 16); }
-  static __device__ __forceinline__ raw of_f(float x) { return (raw)bf16x2_bits(x, 0.0f); }
+  static __device__ __forceinline__ void put(Piece<raw>::vec* v, int i, float a, float b) {
+    const uint32_t w = bf16x2_bits(a, b);
+    (*v)[i] = (raw)w;
+    (*v)[i + 1] = (raw)(w >> 16);
+  }
 };
 struct F16 {
   typedef _Float16 raw;
   static __device__ __forceinline__ float to_f(raw x) { return (float)x; }
-  static __device__ __forceinline__ raw of_f(float x) { return (raw)x; }
+  static __device__ __forceinline__ void put(Piece<raw>::vec* v, int i, float a, float b) {
+    (*v)[i] = (raw)a;
+    (*v)[i + 1] = (raw)b;
+  }
 };
 struct F32 {
   typedef float raw;
   static __device__ __forceinline__ float to_f(raw x) { return x; }
-  static __device__ __forceinline__ raw of_f(float x) { return x; }
+  static __device__ __forceinline__ void put(Piece<raw>::vec* v, int i, float a, float b) {
+    (*v)[i] = a;
+    (*v)[i + 1] = b;
+  }
 };
 
+// L lanes work on a token, with NP pieces of its row each in registers: a row of up to
+// L * NP pieces in one go, longer ones by segments.  The K rows on the experts' side are
+// taken kBatch at a time, so that kBatch * NP loads are in flight before the first is used.
 constexpr int kRowThreads = 256;
 
-// A wave's work: one token and a piece of its row of 64 * 16 bytes.
-struct RowItem {
-  int64_t t;
-  int64_t c;      // first element of this lane's piece
-  int n;          // its elements, 0 .. Piece::n
-};
-template <class D>
-__device__ __forceinline__ RowItem row_item(int64_t item, int H, int segments) {
-  constexpr int V = Piece<typename D::raw>::n;
-  RowItem it;
-  it.t = item / segments;
-  it.c = ((item - it.t * segments) * 64 + (threadIdx.x & 63)) * V;
-  const int64_t left = H - it.c;
-  it.n = left <= 0 ? 0 : left < V ? (int)left : V;
-  return it;
-}
-// the wave's number and the number of waves: item, item + stride, ...
-__device__ __forceinline__ int64_t first_item() { return (int64_t)blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6); }
-__device__ __forceinline__ int64_t item_stride() { return (int64_t)gridDim.x * (kRowThreads / 64); }
-template <class D>
-__device__ __forceinline__ typename Piece<typename D::raw>::vec load_piece(const typename D::raw* p, int n) {
-  typename Piece<typename D::raw>::vec v = {};
-  if (n == Piece<typename D::raw>::n) return *reinterpret_cast<const typename Piece<typename D::raw>::any*>(p);
+template <class D, int L, int NP, bool kStream>
+struct RowPart {
+  typedef typename D::raw raw;
+  typedef typename Piece<raw>::vec vec;
+  typedef typename Piece<raw>::any any;
+  static constexpr int V = Piece<raw>::n;
+  int64_t c[NP];      // first element of each piece
+  int skip[NP];       // its leading elements that other pieces hold too
+  // A row's last piece ends with the row, over part of the one before it, and lanes past
+  // the row hold its last piece once more (all with the same values, so that stores may
+  // overlap): a row of 333 f16 elements took 347 us to combine (100,000 tokens, K = 8) with
+  // its last elements one by one, and takes 169.  Only rows shorter than a piece go by
+  // elements, in the first lane.
+  __device__ __forceinline__ RowPart(int64_t seg, int H) {
+    const int l = threadIdx.x % L;
 #pragma unroll
-  for (int i = 0; i < Piece<typename D::raw>::n; ++i)
-    if (i < n) v[i] = p[i];
-  return v;
-}
-template <class D>
-__device__ __forceinline__ void store_piece(typename D::raw* p, typename Piece<typename D::raw>::vec v, int n) {
-  if (n == Piece<typename D::raw>::n) {
-    *reinterpret_cast<typename Piece<typename D::raw>::any*>(p) = v;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < Piece<typename D::raw>::n; ++i)
-    if (i < n) p[i] = v[i];
-}
-
-template <class D>
-__global__ __launch_bounds__(kRowThreads) void dispatch_kernel(const typename D::raw* __restrict__ x,
-                                                               const int32_t* __restrict__ slot, int64_t T, int K,
-                                                               int64_t rows, int H, int segments,
-                                                               typename D::raw* __restrict__ out) {
-  for (int64_t item = first_item(); item < T * segments; item += item_stride()) {
-    const RowItem it = row_item<D>(item, H, segments);
-    const auto v = load_piece<D>(x + it.t * H + it.c, it.n);
-    for (int k = 0; k < K; ++k) {
-      const int64_t r = slot[it.t * K + k];
-      if (r >= 0 && r < rows) store_piece<D>(out + r * H + it.c, v, it.n);
+    for (int i = 0; i < NP; ++i) {
+      c[i] = ((seg * NP + i) * L + l) * V;
+      const int64_t over = c[i] + V - H;
+      skip[i] = over <= 0 || H < V ? (c[i] < H ? 0 : V) : over < V ? (int)over : V;
+      if (over > 0 && H >= V) c[i] = H - V;
     }
   }
-}
-
-template <class D>
-__global__ __launch_bounds__(kRowThreads) void combine_kernel(const typename D::raw* __restrict__ in,
-                                                              const int32_t* __restrict__ slot,
-                                                              const float* __restrict__ weight, int64_t T, int K,
-                                                              int64_t rows, int H, int segments,
-                                                              typename D::raw* __restrict__ y) {
-  constexpr int V = Piece<typename D::raw>::n;
-  for (int64_t item = first_item(); item < T * segments; item += item_stride()) {
-    const RowItem it = row_item<D>(item, H, segments);
-    float acc[V] = {};
-    for (int k = 0; k < K; ++k) {
-      const int64_t r = slot[it.t * K + k];
-      if (r < 0 || r >= rows) continue;
-      const float w = weight ? weight[it.t * K + k] : 1.0f;
-      const auto v = load_piece<D>(in + r * H + it.c, it.n);
+  template <bool kNt>
+  __device__ __forceinline__ void load(const raw* row, int H, vec (&v)[NP]) const {
+    if (H >= V) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) acc[i] += w * D::to_f(v[i]);
-    }
-    typename Piece<typename D::raw>::vec o;
+      for (int i = 0; i < NP; ++i) {
+        const any* at = reinterpret_cast<const any*>(row + c[i]);
+        v[i] = kNt && kStream ? __builtin_nontemporal_load(at) : *at;
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = D::of_f(acc[i]);
-    store_piece<D>(y + it.t * H + it.c, o, it.n);
-  }
-}
-
-// One wave per token: grad_y's row against each of its experts' rows.
-template <class D>
-__global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(
-    const typename D::raw* __restrict__ gy, const typename D::raw* __restrict__ in, const int32_t* __restrict__ slot,
-    const float* __restrict__ weight, int64_t T, int K, int64_t rows, int H, typename D::raw* __restrict__ gin,
-    float* __restrict__ gw) {
-  constexpr int V = Piece<typename D::raw>::n;
-  const int lane = threadIdx.x & 63;
-  for (int64_t t = first_item(); t < T; t += item_stride()) {
-    for (int k = 0; k < K; ++k) {
-      const int64_t r = slot[t * K + k];
-      float dot = 0.0f;
-      if (r >= 0 && r < rows) {
-        const float w = weight[t * K + k];
-        for (int64_t c = lane * V; c < H; c += 64 * V) {
-          const int n = H - c < V ? (int)(H - c) : V;
-          const auto a = load_piece<D>(gy + t * H + c, n);
-          const auto b = load_piece<D>(in + r * H + c, n);
-          typename Piece<typename D::raw>::vec o;
+      for (int i = 0; i < NP; ++i) {
+        v[i] = vec{};
+        if (skip[i] < V) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            dot += D::to_f(a[i]) * D::to_f(b[i]);
-            o[i] = D::of_f(w * D::to_f(a[i]));
-          }
-          store_piece<D>(gin + r * H + c, o, n);
+          for (int j = 0; j < V - 1; ++j)
+            if (j < H) v[i][j] = row[j];
         }
       }
-      for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
-      if (lane == 0) gw[t * K + k] = dot;
+    }
+  }
+  __device__ __forceinline__ void store(raw* row, int H, const vec (&v)[NP]) const {
+    if (H >= V) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        any* at = reinterpret_cast<any*>(row + c[i]);
+        if (kStream) __builtin_nontemporal_store((any)v[i], at);
+        else *at = v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if (skip[i] < V) {
+#pragma unroll
+          for (int j = 0; j < V - 1; ++j)
+            if (j < H) row[j] = v[i][j];
+        }
+      }
+    }
+  }
+};
+
+// Tokens: t, t + stride, ...  A whole wave's token is known to be the same in its lanes, so
+// that its slots and weights are scalar loads.  near: blocks b, b + 8, ... run on one XCD
+// and get neighbouring tokens, whose short rows share lines of its L2.
+template <int L>
+__device__ __forceinline__ int64_t first_token(bool near) {
+  const int group = L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : (int)threadIdx.x / L;
+  const uint32_t per = gridDim.y / 8;
+  uint32_t y = blockIdx.y;
+  if (near && y < per * 8) y = (y % 8) * per + y / 8;
+  return (int64_t)y * (kRowThreads / L) + group;
+}
+template <int L>
+__device__ __forceinline__ int64_t token_stride() { return (int64_t)gridDim.y * (kRowThreads / L); }
+
+template <class D, int L, int NP, bool kStream>
+__global__ __launch_bounds__(kRowThreads) void dispatch_kernel(const RowArgs a, int segments) {
+  typedef typename D::raw raw;
+  const raw* x = static_cast<const raw*>(a.tokens);
+  raw* out = static_cast<raw*>(a.out);
+  for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
+    const RowPart<D, L, NP, kStream> part(seg, a.H);
+    for (int64_t t = first_token<L>(a.near); t < a.T; t += token_stride<L>()) {
+      typename RowPart<D, L, NP, kStream>::vec v[NP];
+      part.template load<false>(x + t * a.H, a.H, v);
+      for (int k = 0; k < a.K; ++k) {
+        const int64_t r = a.slot[t * a.K + k];
+        if (r >= 0 && r < a.rows) part.store(out + r * a.H, a.H, v);
+      }
     }
   }
 }
 
-// Blocks for that many waves' items; past 2^20 blocks they walk on by the grid.
-static uint32_t row_blocks(int64_t items) {
-  const int64_t want = (items + kRowThreads / 64 - 1) / (kRowThreads / 64);
-  int64_t most = 1 << 20;
+template <class D, int L, int NP, bool kStream>
+__global__ __launch_bounds__(kRowThreads) void combine_kernel(const RowArgs a, int segments) {
+  typedef typename D::raw raw;
+  constexpr int V = Piece<raw>::n, kBatch = NP >= 4 ? 2 : 4;
+  const raw* in = static_cast<const raw*>(a.experts);
+  raw* y = static_cast<raw*>(a.out);
+  for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
+    const RowPart<D, L, NP, kStream> part(seg, a.H);
+    for (int64_t t = first_token<L>(a.near); t < a.T; t += token_stride<L>()) {
+      float acc[NP][V] = {};
+      for (int k0 = 0; k0 < a.K; k0 += kBatch) {
+        int64_t r[kBatch];
+        float w[kBatch];
+        typename RowPart<D, L, NP, kStream>::vec v[kBatch][NP];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const int64_t at = t * a.K + k0 + j;
+          r[j] = k0 + j < a.K ? a.slot[at] : -1;
+          w[j] = k0 + j < a.K && a.weight ? a.weight[at] : 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (r[j] >= 0 && r[j] < a.rows) part.template load<true>(in + r[j] * a.H, a.H, v[j]);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (r[j] >= 0 && r[j] < a.rows) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+              for (int e = 0; e < V; ++e) acc[i][e] += w[j] * D::to_f(v[j][i][e]);
+          }
+      }
+      typename RowPart<D, L, NP, kStream>::vec o[NP];
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int e = 0; e < V; e += 2) D::put(&o[i], e, acc[i][e], acc[i][e + 1]);
+      part.store(y + t * a.H, a.H, o);
+    }
+  }
+}
+
+// A token's L lanes go over all its segments: the products of grad_y's row with each of
+// its experts' rows are theirs alone.  With one segment grad_y's row stays in registers.
+template <class D, int L, int NP, bool kStream>
+__global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(const RowArgs a, int segments) {
+  typedef typename D::raw raw;
+  typedef RowPart<D, L, NP, kStream> Part;
+  constexpr int V = Piece<raw>::n, kBatch = NP >= 4 ? 2 : 4;
+  __shared__ float sh_dot[kBatch][4];
+  const raw* gy = static_cast<const raw*>(a.tokens);
+  const raw* in = static_cast<const raw*>(a.experts);
+  raw* gin = static_cast<raw*>(a.out);
+  const bool whole = a.H % (L * NP * V) == 0;
+  for (int64_t t = first_token<L>(a.near); t < a.T; t += token_stride<L>()) {
+    typename Part::vec g[NP];
+    if (segments == 1) Part(0, a.H).template load<false>(gy + t * a.H, a.H, g);
+    for (int k0 = 0; k0 < a.K; k0 += kBatch) {
+      int64_t r[kBatch];
+      float w[kBatch], dot[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int64_t at = t * a.K + k0 + j;
+        r[j] = k0 + j < a.K ? a.slot[at] : -1;
+        w[j] = k0 + j < a.K ? a.weight[at] : 0.0f;
+        dot[j] = 0.0f;
+      }
+      for (int seg = 0; seg < segments; ++seg) {
+        const Part part(seg, a.H);
+        typename Part::vec v[kBatch][NP];
+        if (segments > 1) part.template load<false>(gy + t * a.H, a.H, g);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (r[j] >= 0 && r[j] < a.rows) part.template load<true>(in + r[j] * a.H, a.H, v[j]);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (r[j] >= 0 && r[j] < a.rows) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+              float y[V];
+#pragma unroll
+              for (int e = 0; e < V; e += 2) {
+                const float x0 = D::to_f(g[i][e]), x1 = D::to_f(g[i][e + 1]);
+                y[e] = x0 * D::to_f(v[j][i][e]);
+                y[e + 1] = x1 * D::to_f(v[j][i][e + 1]);
+                D::put(&v[j][i], e, w[j] * x0, w[j] * x1);
+              }
+              if (!whole) {
+                int skip = part.skip[i];      // compared here, not in V * NP masks kept from before the loops
+                asm volatile("" : "+v"(skip));
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = e >= skip ? y[e] : 0.0f;
+              }
+#pragma unroll
+              for (int e = 0; e < V; ++e) dot[j] += y[e];
+            }
+            part.store(gin + r[j] * a.H, a.H, v[j]);
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) dot[j] = group_sum<(L < 64 ? L : 64)>(dot[j]);
+      if (L > 64) {       // over the block's waves, in their order
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (threadIdx.x % 64 == 0) sh_dot[j][threadIdx.x / 64] = dot[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) dot[j] = (sh_dot[j][0] + sh_dot[j][1]) + (sh_dot[j][2] + sh_dot[j][3]);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (k0 + j < a.K && threadIdx.x % L == 0) a.grad_weight[t * a.K + k0 + j] = dot[j];
+    }
+  }
+}
+
+// What differs between the calls when they choose their form: whether a row's segments go
+// to waves of their own, and whether the call writes the experts' rows.
+#define EQB_ROW_CALL(name, splits, writes)                                              \
+  struct name##_call {                                                                  \
+    static constexpr bool split = splits, writes_rows = writes;                         \
+    template <class D, int L, int NP, bool kStream>                                     \
+    static void launch(dim3 grid, const RowArgs& a, int segments, hipStream_t s) {      \
+      name##_kernel<D, L, NP, kStream><<<grid, kRowThreads, 0, s>>>(a, segments);       \
+    }                                                                                   \
+  };
+EQB_ROW_CALL(dispatch, true, true)
+EQB_ROW_CALL(combine, true, false)
+EQB_ROW_CALL(combine_backward, false, true)
+#undef EQB_ROW_CALL
+
+template <class Call, class D, int L, int NP, bool kStream>
+static void launch_form(const RowArgs& a, hipStream_t s) {
+  const int64_t per = (int64_t)L * NP * Piece<typename D::raw>::n;
+  const int64_t segments = (a.H + per - 1) / per;
+  int64_t y = (a.T + kRowThreads / L - 1) / (kRowThreads / L), most = 65535;
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
-  return (uint32_t)(want < most ? want : most);
-}
-template <class D>
-static int row_segments(int H) {
-  constexpr int per = 64 * Piece<typename D::raw>::n;
-  return (int)(((int64_t)H + per - 1) / per);
+  if (y > most) y = most;
+  const int64_t x = Call::split ? (segments < 1024 ? segments : 1024) : 1;
+  Call::template launch<D, L, NP, kStream>(dim3((uint32_t)x, (uint32_t)y), a, (int)segments, s);
 }
 
-template <class D>
-static void launch_dispatch_as(const RowArgs& a, hipStream_t s) {
-  typedef typename D::raw R;
-  const int seg = row_segments<D>(a.H);
-  dispatch_kernel<D><<<row_blocks(a.T * seg), kRowThreads, 0, s>>>(static_cast<const R*>(a.tokens), a.slot, a.T, a.K,
-                                                                  a.rows, a.H, seg, static_cast<R*>(a.out));
-}
-template <class D>
-static void launch_combine_as(const RowArgs& a, hipStream_t s) {
-  typedef typename D::raw R;
-  const int seg = row_segments<D>(a.H);
-  combine_kernel<D><<<row_blocks(a.T * seg), kRowThreads, 0, s>>>(static_cast<const R*>(a.experts), a.slot, a.weight,
-                                                                 a.T, a.K, a.rows, a.H, seg, static_cast<R*>(a.out));
-}
-template <class D>
-static void launch_combine_backward_as(const RowArgs& a, hipStream_t s) {
-  typedef typename D::raw R;
-  combine_backward_kernel<D><<<row_blocks(a.T), kRowThreads, 0, s>>>(
-      static_cast<const R*>(a.tokens), static_cast<const R*>(a.experts), a.slot, a.weight, a.T, a.K, a.rows, a.H,
-      static_cast<R*>(a.out), a.grad_weight);
-}
+// Lanes and pieces for a row, by the number of its pieces: the fewest lanes that hold a row
+// of up to 64 pieces, whole waves with 2 or 4 pieces each beyond.  Few tokens: split over
+// more waves, or in the backward pass over a block's (one token of 8,192 bf16, K = 8: 42 us
+// in a wave, 12.9 in a block).
+// Calls on experts' rows of kStreamBytes (the memory-side cache) and more pass by it: loads
+// of the experts' rows and all stores are non-temporal, in calls that write experts' rows
+// only where those are whole lines of 128 bytes; dispatch then splits rows over waves by the
+// piece.  16,384 tokens of 2,048 bf16, K = 6: combine 95.9 -> 80.9 us, dispatch 91.7 -> 78,
+// backward 183 -> 163; but 147,456 rows of 100 bf16: dispatch 40 -> 104, and 5,003 rows of
+// 1,001 f32 (in the cache): combine 16.5 -> 21.6.
+// Rows under kNearBytes: neighbouring tokens on one XCD.  147,456 tokens, K = 6, rows of 32
+// bytes: combine 17.6 -> 11.7 us, of 200: 47.4 -> 38.2; of 4,096: 92 -> 96 (not taken).
+// At 147,456 tokens of 1,024 bf16, K = 6: dispatch 402 us (5.3 TB/s), combine 362 (5.8),
+// backward 770 (5.1).
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
+constexpr int64_t kNearBytes = 512;
+constexpr int64_t kRowWaves = 4096;       // waves that fill the chip
 
-#define EQB_ROW_LAUNCH(name)                                      \
-  eqb_status launch_##name(const RowArgs& a, hipStream_t s) {     \
-    if (a.dtype == EQB_DTYPE_BF16) launch_##name##_as<Bf16>(a, s); \
-    else if (a.dtype == EQB_DTYPE_F16) launch_##name##_as<F16>(a, s); \
-    else launch_##name##_as<F32>(a, s);                           \
-    return launch_status();                                       \
+template <class Call, class D>
+static void launch_rows(RowArgs a, hipStream_t s) {
+  const int64_t pieces = ((int64_t)a.H + Piece<typename D::raw>::n - 1) / Piece<typename D::raw>::n;
+  const int64_t bytes = (int64_t)a.H * sizeof(typename D::raw);
+  const bool stream = a.T * a.K * bytes >= kStreamBytes && (!Call::writes_rows || bytes % 128 == 0);
+  const bool few = a.T * pieces <= 64 * kRowWaves;
+  a.near = bytes < kNearBytes;
+  if (pieces <= 4) return launch_form<Call, D, 4, 1, false>(a, s);
+  if (pieces <= 8) return launch_form<Call, D, 8, 1, false>(a, s);
+  if (pieces <= 16) return launch_form<Call, D, 16, 1, false>(a, s);
+  if (pieces <= 32) return launch_form<Call, D, 32, 1, false>(a, s);
+  if (pieces <= 64) return launch_form<Call, D, 64, 1, false>(a, s);
+  if constexpr (Call::split) {
+    if (few) return launch_form<Call, D, 64, 1, false>(a, s);
+    if constexpr (Call::writes_rows) {
+      if (stream) return launch_form<Call, D, 64, 1, true>(a, s);
+    }
+  } else {
+    if (few) return launch_form<Call, D, 256, 1, false>(a, s);
   }
-EQB_ROW_LAUNCH(dispatch)
-EQB_ROW_LAUNCH(combine)
-EQB_ROW_LAUNCH(combine_backward)
-#undef EQB_ROW_LAUNCH
+  if constexpr (!(Call::split && Call::writes_rows)) {
+    if (stream) {
+      if (pieces <= 128) return launch_form<Call, D, 64, 2, true>(a, s);
+      return launch_form<Call, D, 64, 4, true>(a, s);
+    }
+  }
+  if (pieces <= 128) return launch_form<Call, D, 64, 2, false>(a, s);
+  return launch_form<Call, D, 64, 4, false>(a, s);
+}
+
+template <class Call>
+static eqb_status launch_call(const RowArgs& a, hipStream_t s) {
+  if (a.dtype == EQB_DTYPE_BF16) launch_rows<Call, Bf16>(a, s);
+  else if (a.dtype == EQB_DTYPE_F16) launch_rows<Call, F16>(a, s);
+  else launch_rows<Call, F32>(a, s);
+  return launch_status();
+}
+
+eqb_status launch_dispatch(const RowArgs& a, hipStream_t s) { return launch_call<dispatch_call>(a, s); }
+eqb_status launch_combine(const RowArgs& a, hipStream_t s) { return launch_call<combine_call>(a, s); }
+eqb_status launch_combine_backward(const RowArgs& a, hipStream_t s) { return launch_call<combine_backward_call>(a, s); }
 
 }  // namespace eqb
