@@ -62,17 +62,7 @@ eqb_status make_table(const int64_t* part_off, int32_t P, int64_t T, PartTable* 
   return EQB_OK;
 }
 
-// The key of a tensor's random bits at a step: seed, step and place mixed to 32 bits.
-uint32_t adamw_key(uint64_t seed, int64_t step, int32_t i) {
-  uint64_t k = seed + (uint64_t)step * 0x9E3779B97F4A7C15ull + (uint64_t)i * 0xD1B54A32D192ED03ull;
-  k = (k ^ (k >> 32)) * 0xBF58476D1CE4E5B9ull;
-  k = (k ^ (k >> 29)) * 0x94D049BB133111EBull;
-  return (uint32_t)(k ^ (k >> 32));
-}
-
-// Elements of one tensor and blocks of one launch: blocks times 256 threads stay below 2^32.
-constexpr int64_t kAdamwMostElements = (int64_t)1 << 34;
-constexpr uint32_t kAdamwMostBlocks = 1u << 23;
+constexpr int64_t kAdamwMostElements = (int64_t)1 << 33;     // of one tensor: its blocks fit a launch
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -506,33 +496,17 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t gr
     if ((at & 3) || ((reinterpret_cast<uintptr_t>(t.grad) | reinterpret_cast<uintptr_t>(t.copy)) & 1))
       return EQB_ERR_UNSUPPORTED;
   }
-  AdamwBatch b;
-  b.n = 0;
-  b.beta1 = (float)beta1;
-  b.rest1 = (float)(1.0 - beta1);
-  b.beta2 = (float)beta2;
-  b.rest2 = (float)(1.0 - beta2);
-  b.eps = (float)eps;
-  b.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-  b.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-  b.grad_scale = grad_scale;
-  b.found_inf = found_inf;
-  uint32_t blocks = 0;
-  for (int32_t i = 0; i < n; ++i) {
-    const eqb_adamw_tensor& t = tensors[i];
-    if (t.numel == 0) continue;
-    const uint32_t more = adamw_blocks(t.numel);
-    if (b.n == kAdamwTensors || (b.n > 0 && blocks + more > kAdamwMostBlocks)) {
-      const eqb_status st = launch_adamw(b, blocks, eight, grad_bf16, static_cast<hipStream_t>(stream));
-      if (st != EQB_OK) return st;
-      b.n = 0;
-      blocks = 0;
-    }
-    b.t[b.n++] = AdamwSlot{t.param, t.grad, t.copy, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale,
-                           t.numel, (float)(1.0 - lr * t.weight_decay), adamw_key(seed, step, i), blocks};
-    blocks += more;
-  }
-  return b.n > 0 ? launch_adamw(b, blocks, eight, grad_bf16, static_cast<hipStream_t>(stream)) : EQB_OK;
+  AdamwScalars c;
+  c.beta1 = (float)beta1;
+  c.rest1 = (float)(1.0 - beta1);
+  c.beta2 = (float)beta2;
+  c.rest2 = (float)(1.0 - beta2);
+  c.eps = (float)eps;
+  c.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  c.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+  c.grad_scale = grad_scale;
+  c.found_inf = found_inf;
+  return launch_adamw(tensors, n, c, lr, seed, step, eight, grad_bf16, copies, static_cast<hipStream_t>(stream));
 }
 
 eqb_status eqb_set_max_blocks(int32_t max_blocks) {

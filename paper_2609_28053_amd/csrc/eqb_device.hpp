@@ -211,22 +211,25 @@ __device__ __forceinline__ uint64_t group_max_u64(uint64_t m) {
 
 // Sum (maximum) over aligned groups of G lanes, the same in every lane of the group: DPP
 // up to 16 lanes, then swaps of 16 and of 32 lanes between two copies.
-template <int G, class F>
-__device__ __forceinline__ float group_fold(float x, F f) {
+template <int G, class T, class F>
+__device__ __forceinline__ T group_fold(T x, F f) {
+  static_assert(sizeof(T) == 4, "32-bit values");
   auto dpp = [&](auto ctrl) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false));
   };
   if constexpr (G >= 2) x = f(x, dpp(std::integral_constant<int, 0xB1>{}));
   if constexpr (G >= 4) x = f(x, dpp(std::integral_constant<int, 0x4E>{}));
   if constexpr (G >= 8) x = f(x, dpp(std::integral_constant<int, 0x141>{}));
   if constexpr (G >= 16) x = f(x, dpp(std::integral_constant<int, 0x140>{}));
   if constexpr (G >= 32) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = f(__builtin_bit_cast(T, (uint32_t)r[0]), __builtin_bit_cast(T, (uint32_t)r[1]));
   }
   if constexpr (G >= 64) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = f(__builtin_bit_cast(T, (uint32_t)r[0]), __builtin_bit_cast(T, (uint32_t)r[1]));
   }
   return x;
 }

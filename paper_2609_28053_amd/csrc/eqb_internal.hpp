@@ -187,31 +187,13 @@ eqb_status launch_dispatch(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine_backward(const RowArgs& a, hipStream_t s);
 
-// Tensors of one AdamW launch, passed by value (kernel arguments hold 4 KiB).
-struct AdamwSlot {
-  float* param;
-  const void* grad;
-  uint16_t* copy;
-  void* exp_avg;
-  void* exp_avg_sq;
-  float* exp_avg_scale;
-  float* exp_avg_sq_scale;
-  int64_t numel;
-  float keep;             // 1 - lr * weight_decay
-  uint32_t key;           // of the random bits
-  uint32_t first_block;
-};
-constexpr int kAdamwTensors = 48;
-struct AdamwBatch {
-  int n;
+struct AdamwScalars {
   float beta1, rest1, beta2, rest2, eps, inv_root, rate;
   const float* grad_scale;
   const float* found_inf;
-  AdamwSlot t[kAdamwTensors];
 };
-static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
-uint32_t adamw_blocks(int64_t numel);
-eqb_status launch_adamw(const AdamwBatch& b, uint32_t blocks, bool eight, bool grad_bf16, hipStream_t s);
+eqb_status launch_adamw(const eqb_adamw_tensor* tensors, int n, const AdamwScalars& c, double lr, uint64_t seed,
+                        int64_t step, bool eight, bool grad_bf16, bool copies, hipStream_t s);
 
 // Count slabs per partition in a layer's workspace: enough that about 8
 // slabs share the blocks of a launch, so no counter receives the flush

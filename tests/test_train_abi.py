@@ -121,7 +121,7 @@ def test_adamw_refuses(lib):
     assert call(n=-1) == call(null=True) == call(dt=2) == call(bits=16) == call(step=0) == INVALID
     assert call(lr=nan) == call(b1=1.0) == call(b1=-0.1) == call(b2=1.0) == call(b2=nan) == call(eps=-1.0) == INVALID
     assert call(param=None) == call(grad=None) == call(m=None) == call(v=None) == call(wd=nan) == INVALID
-    assert call(numel=-1) == call(numel=(1 << 34) + 1) == INVALID
+    assert call(numel=-1) == call(numel=(1 << 33) + 1) == INVALID
     assert call(bits=8) == call(bits=8, ms=a) == INVALID                     # scales missing
     assert call(more=dict(copy=a)) == call(copy=a, more=dict(copy=None)) == INVALID   # copies of some only
     assert call(param=a + 2) == call(m=a + 1) == call(grad=a + 2) == call(copy=a + 1) == UNSUPPORTED
