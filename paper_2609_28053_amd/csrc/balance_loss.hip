@@ -126,8 +126,9 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t k = i + j * kLossThreads;
-            e[j] = -1;
-            if (k < pairs && (!kMask || vc[k / (uint32_t)K])) e[j] = ic[k];
+            const uint32_t kc = k < pairs ? k : pairs - 1;
+            e[j] = ic[kc];
+            if (k >= pairs || (kMask && vc[kc / (uint32_t)K] == 0)) e[j] = -1;
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -300,7 +301,10 @@ static void launch_loss_as(const BalanceArgs& a, const BalanceWorkspace& ws, hip
   int64_t rpb;
   // One block for 32,768 logits, blocks of at least 16,384 beyond: 4,096 rows of E = 8 take
   // 8.8 us in one block and 12.4 in two, 16,384 rows of E = 64 8.7 in 64 and 9.4 in 32.
-  grid_for(a.T, a.T * E <= 32768 ? 32768 / E : 16384 / E, 2, &blocks, &rpb);
+  // One block per compute unit for up to 2^26 logits (99,991 rows of E = 128 19.0 us, with
+  // two 22.4; 147,456 of E = 256 24 either way), two beyond, where they hide more latency.
+  const int64_t logits = a.T * E;
+  grid_for(a.T, logits <= 32768 ? 32768 / E : 16384 / E, logits <= 1 << 26 ? 1 : 2, &blocks, &rpb);
   if (blocks > kBalanceBlocks) {
     rpb = (a.T + kBalanceBlocks - 1) / kBalanceBlocks;
     blocks = (int)((a.T + rpb - 1) / rpb);
