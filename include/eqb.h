@@ -356,9 +356,9 @@ eqb_status eqb_layer_noalloc(const uint16_t* z, const float* b, int64_t T, int32
  *   workspace: eqb_balance_workspace_size(E, P) bytes, 256-byte aligned, owned
  *     by the caller, zeroed once after allocation; each call leaves its leading
  *     counter zero again.  Two calls whose work may overlap need two.
- * The probabilities of a row and the sums over up to T / 256 rows are binary32,
- * the sums of those binary64; the result does not depend on the order in which
- * blocks run.  T = 0 writes zeros (`load` too, with or without topk_idx).
+ * A row's probabilities and a lane's sum over its rows are binary32, the sums of
+ * those binary64 (handed from block to block in binary32); the result does not
+ * depend on the order in which blocks run.  T = 0 writes zeros (`load` too, with or without topk_idx).
  */
 size_t eqb_balance_workspace_size(int32_t E, int32_t P);     /* host only; 0 for unsupported E or P */
 eqb_status eqb_balance_loss(const uint16_t* z, const int32_t* topk_idx, const uint8_t* valid, int64_t T,
@@ -403,7 +403,7 @@ eqb_status eqb_dispatch_plan(const int32_t* topk_idx, int64_t T, int32_t K, int3
  * Rows of `hidden` elements of type dtype (EQB_DTYPE_*), between the tokens' order
  * and the experts'.  `rows` tells how many rows the expert-ordered buffers hold;
  * a pair whose slot lies outside [0, rows) is dropped.  Buffers need the alignment
- * of their elements only.  T*K < 2^31.
+ * of their elements only, and those of one call must not overlap.  T*K < 2^31.
  *   eqb_dispatch: expert_rows[slot[t,k]] = x[t].  Rows that no slot names are left
  *     as they are.
  *   eqb_combine (Eq. 1): y[t] = sum over k of weight[t,k] expert_rows[slot[t,k]], in
@@ -474,12 +474,14 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t gr
 
 /*
  * Test control (host only, no HIP call): caps the number of blocks of the
- * streaming kernels (routing, the margin passes, the LEI kernels) at
- * max_blocks for the calls that follow FROM THE CALLING HOST THREAD; calls
- * made from other threads keep their own setting (the default 0: a whole
- * number of blocks per compute unit).  Results do not depend on it; tests
- * use it to run one block, or a block count that does not divide the rows,
- * against the same oracle.  Negative values are EQB_ERR_INVALID_ARG.
+ * streaming kernels (routing, the margin passes, the LEI kernels, the balance
+ * loss and its gradient, the experts' rows) at max_blocks for the calls that
+ * follow FROM THE CALLING HOST THREAD; calls made from other threads keep their
+ * own setting (the default 0: a whole number of blocks per compute unit).
+ * Results do not depend on it, but for the last bits of the balance loss's
+ * binary32 sums; tests use it to run one block, or a block count that does not
+ * divide the rows, against the same oracle.  Negative values are
+ * EQB_ERR_INVALID_ARG.
  * eqb_get_max_blocks returns the calling thread's current cap.
  */
 eqb_status eqb_set_max_blocks(int32_t max_blocks);

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_kernel(const RowArgs a, 
 template <class D, int L, int NP, bool kStream>
 __global__ __launch_bounds__(kRowThreads) void combine_kernel(const RowArgs a, int segments) {
   typedef typename D::raw raw;
-  constexpr int V = Piece<raw>::n, kBatch = NP >= 4 ? 2 : 4;
+  constexpr int V = Piece<raw>::n, kBatch = NP == 2 ? 8 : 4;
   const raw* in = static_cast<const raw*>(a.experts);
   raw* y = static_cast<raw*>(a.out);
   for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
@@ -345,7 +345,7 @@ template <class D, int L, int NP, bool kStream>
 __global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(const RowArgs a, int segments) {
   typedef typename D::raw raw;
   typedef RowPart<D, L, NP, kStream> Part;
-  constexpr int V = Piece<raw>::n, kBatch = NP >= 4 ? 2 : 4;
+  constexpr int V = Piece<raw>::n, kBatch = 4;
   __shared__ float sh_dot[kBatch][4];
   const raw* gy = static_cast<const raw*>(a.tokens);
   const raw* in = static_cast<const raw*>(a.experts);
@@ -448,13 +448,13 @@ static void launch_form(const RowArgs& a, hipStream_t s) {
 // Calls on experts' rows of kStreamBytes (the memory-side cache) and more pass by it: loads
 // of the experts' rows and all stores are non-temporal, in calls that write experts' rows
 // only where those are whole lines of 128 bytes; dispatch then splits rows over waves by the
-// piece.  16,384 tokens of 2,048 bf16, K = 6: combine 95.9 -> 80.9 us, dispatch 91.7 -> 78,
-// backward 183 -> 163; but 147,456 rows of 100 bf16: dispatch 40 -> 104, and 5,003 rows of
+// piece.  16,384 tokens of 2,048 bf16, K = 6: combine 95.9 -> 80 us, dispatch 91.7 -> 78,
+// backward 183 -> 159; but 147,456 rows of 100 bf16: dispatch 40 -> 104, and 5,003 rows of
 // 1,001 f32 (in the cache): combine 16.5 -> 21.6.
 // Rows under kNearBytes: neighbouring tokens on one XCD.  147,456 tokens, K = 6, rows of 32
 // bytes: combine 17.6 -> 11.7 us, of 200: 47.4 -> 38.2; of 4,096: 92 -> 96 (not taken).
-// At 147,456 tokens of 1,024 bf16, K = 6: dispatch 402 us (5.3 TB/s), combine 362 (5.8),
-// backward 770 (5.1).
+// At 147,456 tokens of 1,024 bf16, K = 6: dispatch 402 us (5.3 TB/s), combine 351 (6.0),
+// backward 755 (5.2).
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 constexpr int64_t kNearBytes = 512;
 constexpr int64_t kRowWaves = 4096;       // waves that fill the chip
