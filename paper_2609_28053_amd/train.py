@@ -1,0 +1,123 @@
+"""Buffers and handles for training an MoE layer around its routing.
+
+Each class owns the buffers of one operator and makes the calls of ``eqb`` on
+them; all computation happens in the library's kernels.  Work is enqueued on
+the current stream (or ``stream``), nothing synchronises.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import eqb
+
+
+class ExpertRows:
+    """The experts' rows of T tokens (Eq. 1): the order of the routed pairs,
+    dispatch of the tokens' rows, combine of what the experts return, and the
+    gradients of both.  Expert e's rows are offsets[e] .. offsets[e + 1] - 1."""
+
+    def __init__(self, T: int, E: int, K: int, device="cuda"):
+        self.T, self.E, self.K = T, E, K
+        i32 = dict(dtype=torch.int32, device=torch.device(device))
+        self.offsets = torch.empty(E + 1, **i32)
+        self.slot = torch.empty((T, K), **i32)
+        self.workspace = torch.empty(eqb.eqb_dispatch_workspace_size(T, K, E), dtype=torch.uint8, device=i32["device"])
+
+    def plan(self, topk_idx, stream=None):
+        """Orders the pairs of topk_idx [T,K]; entries outside [0, E) are dropped."""
+        eqb.eqb_dispatch_plan(topk_idx, self.E, self.offsets, self.slot, self.workspace, stream)
+        return self
+
+    def dispatch(self, x, rows=None, stream=None):
+        """The tokens' rows x [T,H] in the experts' order [T*K,H] (rows past offsets[E] are not written)."""
+        if rows is None:
+            rows = torch.empty((self.T * self.K, x.shape[1]), dtype=x.dtype, device=x.device)
+        eqb.eqb_dispatch(x, self.slot, rows, stream)
+        return rows
+
+    def combine(self, rows, weight=None, y=None, stream=None):
+        """sum_k weight[t, k] rows[slot[t, k]] for every token; without weight, the gradient of dispatch."""
+        if y is None:
+            y = torch.empty((self.T, rows.shape[1]), dtype=rows.dtype, device=rows.device)
+        eqb.eqb_combine(rows, self.slot, weight, y, stream)
+        return y
+
+    def combine_backward(self, grad_y, rows, weight, grad_rows=None, grad_weight=None, stream=None):
+        """Gradients of combine with respect to the rows and to the weights (the router backward's grad_score)."""
+        if grad_rows is None:
+            grad_rows = torch.empty_like(rows)
+        if grad_weight is None:
+            grad_weight = torch.empty_like(weight)
+        eqb.eqb_combine_backward(grad_y, rows, self.slot, weight, grad_rows, grad_weight, stream)
+        return grad_rows, grad_weight
+
+
+class BalanceLoss:
+    """The auxiliary balance loss of P groups over T tokens, its loads, and its
+    gradient with the router backward.  score: "sigmoid" (normalised) or
+    "softmax"."""
+
+    def __init__(self, T: int, E: int, K: int, P: int = 1, alpha: float = 1e-2, score: str = "sigmoid", device="cuda"):
+        self.T, self.E, self.K, self.P, self.alpha = T, E, K, P, alpha
+        self.score = {"sigmoid": eqb.EQB_SCORE_SIGMOID, "softmax": eqb.EQB_SCORE_SOFTMAX}[score]
+        dev = torch.device(device)
+        self.load = torch.empty((P, E), dtype=torch.int32, device=dev)
+        self.tokens = torch.empty(P, dtype=torch.int32, device=dev)
+        self.prob = torch.empty((P, E), dtype=torch.float32, device=dev)
+        self.loss = torch.empty(P, dtype=torch.float32, device=dev)
+        self.workspace = torch.zeros(eqb.eqb_balance_workspace_size(E, P), dtype=torch.uint8, device=dev)
+
+    def forward(self, z, topk_idx=None, valid=None, part_off=None, load=None, stream=None):
+        """The groups' losses [P] (self.loss); counts topk_idx, or takes the routing's loads."""
+        if (topk_idx is None) == (load is None):
+            raise ValueError("give topk_idx to count, or the loads that the routing counted")
+        if load is not None:
+            self.load = load
+        eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, self.load, self.tokens, self.prob, self.loss,
+                             self.workspace, valid, part_off, self.score, stream)
+        return self.loss
+
+    def backward(self, z, grad_loss, grad_z=None, topk_idx=None, grad_score=None, inj=None, valid=None,
+                 part_off=None, stream=None):
+        """The gradient with respect to z; with topk_idx and grad_score (and inj), the whole router's."""
+        if grad_z is None:
+            grad_z = torch.empty((self.T, self.E), dtype=torch.float32, device=z.device)
+        eqb.eqb_balance_backward(z, self.load, self.tokens, self.K, self.alpha, grad_loss, grad_z, topk_idx, grad_score,
+                                 inj, valid, part_off, self.score, stream)
+        return grad_z
+
+
+class AdamW:
+    """AdamW over a list of binary32 parameters, in place, one call a step.
+    state_bits: 32, or 8 for E4M3 states with a scale per 256 elements.
+    copies: BF16 tensors that receive the new parameters.  weight_decay: one
+    value, or one per parameter."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
+                 seed=0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits is 8 or 32, not {state_bits}")
+        self.params, self.lr, self.betas, self.eps, self.seed, self.steps = list(params), lr, betas, eps, seed, 0
+        self.weight_decay, self.copies, self.state_bits = weight_decay, copies, state_bits
+        if state_bits == 8:
+            new = lambda: [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)  # noqa: E731
+                           for p in self.params]
+            scales = lambda: [torch.zeros(-(-p.numel() // eqb.EQB_ADAMW_BLOCK), device=p.device)  # noqa: E731
+                              for p in self.params]
+            self.exp_avg_scale, self.exp_avg_sq_scale = scales(), scales()
+        else:
+            new = lambda: [torch.zeros_like(p) for p in self.params]  # noqa: E731
+            self.exp_avg_scale = self.exp_avg_sq_scale = None
+        self.exp_avg, self.exp_avg_sq = new(), new()
+        self._tensors = None
+
+    def step(self, grads, lr=None, grad_scale=None, found_inf=None, stream=None):
+        """One step with these gradients, one per parameter, all binary32 or all BF16."""
+        if self._tensors is None:
+            self._tensors = eqb.AdamwTensors(self.params, grads, self.exp_avg, self.exp_avg_sq, self.copies,
+                                             self.exp_avg_scale, self.exp_avg_sq_scale, self.weight_decay)
+        else:
+            self._tensors.set_grads(grads)
+        self.steps += 1
+        eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,
+                           grad_scale, found_inf, stream)
