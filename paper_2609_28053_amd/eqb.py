@@ -149,23 +149,23 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, numel=None, name="tensor"):
         raise ValueError(f"{name} must be a GPU tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if dtype is not None and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    if dtype is not None and t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int:
     if stream is None:
         # the current stream's handle without a torch.cuda.Stream around it (0.2 us instead of 3)
         if _raw_stream is not None and torch.cuda.is_initialized():
-            return ctypes.c_void_p(_raw_stream(torch._C._cuda_getDevice()))
+            return _raw_stream(torch._C._cuda_getDevice())
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 class PartOffsets:
@@ -531,7 +531,7 @@ class AdamwTensors:
             return
         if len(tensors) != self.n:
             raise ValueError(f"{len(tensors)} {field} tensors for {self.n} parameters")
-        self.table[field] = [_ptr(t, dtype, n, field).value or 0 for t, n in zip(tensors, numel)]
+        self.table[field] = [_ptr(t, dtype, n, field) for t, n in zip(tensors, numel)]
         self._kept.append(list(tensors))
 
     def set_grads(self, grads):
@@ -541,7 +541,7 @@ class AdamwTensors:
             raise TypeError(f"gradients have dtype {dtype}, expected torch.float32 or torch.bfloat16")
         if len(grads) != self.n:
             raise ValueError(f"{len(grads)} gradients for {self.n} parameters")
-        self.table["grad"] = [_ptr(g, dtype, n, "grad").value or 0 for g, n in zip(grads, self.numel)]
+        self.table["grad"] = [_ptr(g, dtype, n, "grad") for g, n in zip(grads, self.numel)]
         self.grads = list(grads)
         self.grad_dtype = _ROW_TYPES[dtype]
 
