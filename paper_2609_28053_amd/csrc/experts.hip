@@ -443,8 +443,9 @@ static void launch_form(const RowArgs& a, hipStream_t s) {
 
 // Lanes and pieces for a row, by the number of its pieces: the fewest lanes that hold a row
 // of up to 64 pieces, whole waves with 2 or 4 pieces each beyond.  Few tokens: split over
-// more waves, or in the backward pass over a block's (one token of 8,192 bf16, K = 8: 42 us
-// in a wave, 12.9 in a block).
+// more waves (past 4,096 waves of 64 pieces that costs: 8,000 tokens of 1,024 bf16, K = 8,
+// combine 31.5 -> 38 us), or in the backward pass over a block's (one token of 8,192 bf16, K =
+// 8: 42 us in a wave, 12.9 in a block; 1,000 of 7,168: 70 and 56; 2,000 of 4,096: 63 and 68).
 // Calls on experts' rows of kStreamBytes (the memory-side cache) and more pass by it: loads
 // of the experts' rows and all stores are non-temporal, in calls that write experts' rows
 // only where those are whole lines of 128 bytes; dispatch then splits rows over waves by the
@@ -457,7 +458,8 @@ static void launch_form(const RowArgs& a, hipStream_t s) {
 // backward 755 (5.2).
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 constexpr int64_t kNearBytes = 512;
-constexpr int64_t kRowWaves = 4096;       // waves that fill the chip
+constexpr int64_t kRowWaves = 4096;
+constexpr int64_t kBlockTokens = 1024;
 
 template <class Call, class D>
 static void launch_rows(RowArgs a, hipStream_t s) {
@@ -477,7 +479,7 @@ static void launch_rows(RowArgs a, hipStream_t s) {
       if (stream) return launch_form<Call, D, 64, 1, true>(a, s);
     }
   } else {
-    if (few) return launch_form<Call, D, 256, 1, false>(a, s);
+    if (few || a.T <= kBlockTokens) return launch_form<Call, D, 256, 1, false>(a, s);
   }
   if constexpr (!(Call::split && Call::writes_rows)) {
     if (stream) {
