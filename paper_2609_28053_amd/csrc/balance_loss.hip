@@ -346,9 +346,13 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // gradient is p q (C - sum p C) + (g + inj) sigmoid'.  The K mixture gradients of a row
 // are scattered into a per-wave LDS row of zeros, read back 4 at a time, and their
 // places zeroed again.
+// Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once and
+// non-temporal.  Two rows a lane and eight waves a SIMD: 4,194,304 rows of E = 256, K = 8
+// take 1,276 us (5.3 TB/s), with three rows and six waves 1,324, four and four 1,320, one
+// and eight 1,306; 1,000,003 of E = 128 161, 175, 161, 164.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;
-constexpr int kGradU = 3;          // rows per lane and step
-constexpr int kGradWavesPerSimd = 6;
+constexpr int kGradU = 2;          // rows per lane and step
+constexpr int kGradWavesPerSimd = 8;
 constexpr int kGradBlocksPerCu = kGradWavesPerSimd * 256 / kGradThreads;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
