@@ -120,19 +120,22 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
       fetch(0, zn, next);
       if (idx) {
         const int32_t* ic = idx + cu * K;
-        const uint32_t pairs = rows * (uint32_t)K;
+        const uint32_t pairs = rows * (uint32_t)K, inv_K = 0xFFFFFFFFu / (uint32_t)K + 1, one = K == 1 ? ~0u : 0u;
         for (uint32_t i = tid; i < pairs; i += 4 * kLossThreads) {
-          int e[4];
+          // all loads first, of places in range, and no branches among them
+          int e[4], ok[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t k = i + j * kLossThreads;
-            const uint32_t kc = k < pairs ? k : pairs - 1;
-            e[j] = ic[kc];
-            if (k >= pairs || (kMask && vc[kc / (uint32_t)K] == 0)) e[j] = -1;
+            const uint32_t k = i + j * kLossThreads, kc = k < pairs ? k : pairs - 1;
+            e[j] = at<const int32_t>(ic, 4u * kc);
+            // kc / K: exact below 2^24 for K < 256 by the rounded-up reciprocal (0 for K = 1)
+            ok[j] = kMask ? at<const uint8_t>(vc, __umulhi(kc, inv_K) + (kc & one)) : 1;
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (e[j] >= 0 && e[j] < E) atomicAdd(&sh_cnt[lane % (kNBins / E)][e[j]], 1);
+          for (int j = 0; j < 4; ++j) {
+            const bool in = (i + j * kLossThreads < pairs) & (ok[j] != 0) & ((uint32_t)e[j] < (uint32_t)E);
+            if (in) atomicAdd(&sh_cnt[lane % (kNBins / E)][e[j]], 1);
+          }
         }
       }
       for (uint32_t base = 0; base < rows; base += ROWS) {
