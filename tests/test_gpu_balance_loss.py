@@ -245,3 +245,27 @@ def test_large_batch(eqb):  # noqa: F811
     for k in (0, 65, 130):
         got = gz[k * n:k * n + 64].cpu().numpy()
         assert np.all(np.abs(got - want) <= 3 * c.eps * bound + 1e-44)
+
+
+@pytest.mark.parametrize("K", [1, 2, 3, 7, 16, 100, 255])
+def test_masked_counts(eqb, K):  # noqa: F811
+    """The counts of masked batches, every fan-out: a pair's token is found by a product with K's reciprocal."""
+    T, E = 70001 if K < 16 else 9001, 256
+    g = torch.Generator(device="cuda")
+    g.manual_seed(K)
+    d = dict(device="cuda")
+    z = torch.randn((T, E), generator=g, **d).to(torch.bfloat16).view(torch.int16)
+    idx = torch.randint(-2, E + 2, (T, K), generator=g, **d).to(torch.int32)
+    valid = torch.rand(T, generator=g, **d) < 0.7
+    cuts = [0, 11, T // 3, T // 3, T]
+    load, tokens = torch.empty((4, E), dtype=torch.int32, **d), torch.empty(4, dtype=torch.int32, **d)
+    ws = torch.zeros(eqb.eqb_balance_workspace_size(E, 4), dtype=torch.uint8, **d)
+    say(f"balance, masked counts K={K}")
+    for score in (eqb.EQB_SCORE_SIGMOID, eqb.EQB_SCORE_SOFTMAX):
+        eqb.eqb_balance_loss(z, idx, K, 1.0, load.fill_(-1), tokens, torch.empty((4, E), **d), torch.empty(4, **d), ws, valid,
+                             cuts, score)
+        for p, (a, b) in enumerate(zip(cuts, cuts[1:])):
+            mine = idx[a:b][valid[a:b]]
+            mine = mine[(mine >= 0) & (mine < E)].long()
+            assert torch.equal(load[p].long(), torch.bincount(mine.reshape(-1), minlength=E)), p
+            assert int(tokens[p]) == int(valid[a:b].sum())

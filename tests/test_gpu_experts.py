@@ -267,3 +267,61 @@ def test_captured_in_a_graph(eqb):  # noqa: F811
         for k in a:
             if k not in ("ws", "bws"):
                 assert torch.equal(a[k], b[k]), (r, k)
+
+
+def test_capped_blocks(eqb):  # noqa: F811
+    """Few blocks walk over all tokens: the same bits as many."""
+    rng = np.random.default_rng(5)
+    T, K, E, H = 700, 3, 16, 200
+    _, slot = plan(eqb, picks(rng, T, K, E, 0.05), E)
+    x, out = away((T, H), torch.bfloat16, rng, 0), away((T * K, H), torch.bfloat16, rng, 0)
+    w = torch.from_numpy(rng.random((T, K)).astype(np.float32)).cuda()
+
+    def run():
+        rows, y = torch.zeros_like(out), torch.zeros_like(x)
+        gr, gw = torch.zeros_like(out), torch.zeros((T, K), device="cuda")
+        eqb.eqb_dispatch(x, slot, rows)
+        eqb.eqb_combine(out, slot, w, y)
+        eqb.eqb_combine_backward(x, out, slot, w, gr, gw)
+        return rows, y, gr, gw
+
+    want = run()
+    for cap in (1, 3, 7):
+        say(f"rows, at most {cap} blocks")
+        eqb.eqb_set_max_blocks(cap)
+        try:
+            got = run()
+        finally:
+            eqb.eqb_set_max_blocks(0)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_buffers_beyond_the_cache(eqb):  # noqa: F811
+    """Rows past 256 MiB take the streamed forms: against torch's own indexing (a combined value within the rounding of
+    the products' and sums' order, a weight's gradient within H 2^-24 of its magnitudes)."""
+    for T, H, dtype in ((70001, 1024, torch.bfloat16), (40001, 1000, torch.float32), (9001, 8200, torch.float16)):
+        K, E = 2, 8
+        g = torch.Generator(device="cuda")
+        g.manual_seed(T)
+        idx = torch.rand((T, E), generator=g, device="cuda").topk(K, dim=1).indices.to(torch.int32)
+        _, slot = plan(eqb, idx.cpu().numpy(), E)
+        at = slot.long()
+        say(f"rows beyond the cache {T} x {H} {dtype}")
+        x = torch.randn((T, H), generator=g, device="cuda", dtype=dtype)
+        rows = torch.empty((T * K, H), dtype=dtype, device="cuda")
+        eqb.eqb_dispatch(x, slot, rows)
+        assert all(torch.equal(rows[at[:, k]], x) for k in range(K))
+        out = torch.randn((T * K, H), generator=g, device="cuda", dtype=dtype)
+        w = torch.rand((T, K), generator=g, device="cuda")
+        y = torch.empty_like(x)
+        eqb.eqb_combine(out, slot, w, y)
+        parts = [w[:, k:k + 1].double() * out[at[:, k]].double() for k in range(K)]
+        want, size = parts[0] + parts[1], parts[0].abs() + parts[1].abs()
+        half = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 0.0}[dtype]
+        assert bool(((y.double() - want).abs() <= 3 * 2.0 ** -24 * size * (1 + half) + half * want.abs() + 2.0 ** -25).all())
+        gr, gw = torch.empty_like(out), torch.empty_like(w)
+        eqb.eqb_combine_backward(x, out, slot, w, gr, gw)
+        for k in range(K):
+            assert torch.equal(gr[at[:, k]], (w[:, k:k + 1] * x.float()).to(dtype))
+            dot, mag = (x.double() * out[at[:, k]].double()), H * 2.0 ** -24
+            assert bool(((gw[:, k].double() - dot.sum(1)).abs() <= mag * dot.abs().sum(1)).all())
