@@ -28,7 +28,7 @@ __device__ __forceinline__ float softmax_where(bool part, const float (&x)[N], f
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
-  m = fmaxf(group_max<G>(m), -3.0e38f);
+  m = fmaxf(group_max<G>(m), -3.402823466e38f);     // BF16's lowest value is above it
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {

@@ -269,3 +269,27 @@ def test_masked_counts(eqb, K):  # noqa: F811
             mine = mine[(mine >= 0) & (mine < E)].long()
             assert torch.equal(load[p].long(), torch.bincount(mine.reshape(-1), minlength=E)), p
             assert int(tokens[p]) == int(valid[a:b].sum())
+
+
+@pytest.mark.parametrize("softmax", [False, True])
+@pytest.mark.parametrize("E", [8, 128, 256])
+def test_masks_of_the_lowest_value(eqb, E, softmax):  # noqa: F811
+    """Experts masked by BF16's lowest value instead of -inf: 0 beside others, and a row of nothing else is a row of
+    equal logits (probabilities 1/E)."""
+    c = Case(E, 90, E, 2, 2)
+    x = c.z.to(torch.float32)
+    low = torch.finfo(torch.bfloat16).min
+    x[::3, 1::2] = low
+    x[1::5] = low
+    x[2::7, :E // 2] = -float("inf")
+    x[4] = -float("inf")
+    x[5] = low
+    x[5, 3] = -float("inf")
+    c.z = x.to(torch.bfloat16)
+    c.x = c.z.to(torch.float64).numpy()
+    # the masked entries' own rounding does not count: their weights are 0 or 1 exactly
+    c.eps = (2 * np.abs(c.x[np.abs(c.x) < 1e30]).max() + 24) * 2.0 ** -23
+    say(f"balance, lowest values E={E} softmax={softmax}")
+    got = run(eqb, c, softmax, router=False)
+    assert np.all(np.isfinite(got["gz"])) and np.all(np.isfinite(got["prob"]))
+    check(c, got, softmax, router=False)
