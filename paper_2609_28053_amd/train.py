@@ -61,7 +61,8 @@ class BalanceLoss:
         self.T, self.E, self.K, self.P, self.alpha = T, E, K, P, alpha
         self.score = {"sigmoid": eqb.EQB_SCORE_SIGMOID, "softmax": eqb.EQB_SCORE_SOFTMAX}[score]
         dev = torch.device(device)
-        self.load = torch.empty((P, E), dtype=torch.int32, device=dev)
+        self._counts = torch.empty((P, E), dtype=torch.int32, device=dev)
+        self.load = self._counts
         self.tokens = torch.empty(P, dtype=torch.int32, device=dev)
         self.prob = torch.empty((P, E), dtype=torch.float32, device=dev)
         self.loss = torch.empty(P, dtype=torch.float32, device=dev)
@@ -71,8 +72,7 @@ class BalanceLoss:
         """The groups' losses [P] (self.loss); counts topk_idx, or takes the routing's loads."""
         if (topk_idx is None) == (load is None):
             raise ValueError("give topk_idx to count, or the loads that the routing counted")
-        if load is not None:
-            self.load = load
+        self.load = self._counts if load is None else load
         eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, self.load, self.tokens, self.prob, self.loss,
                              self.workspace, valid, part_off, self.score, stream)
         return self.loss
@@ -121,3 +121,22 @@ class AdamW:
         self.steps += 1
         eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,
                            grad_scale, found_inf, stream)
+
+    def state_dict(self) -> dict:
+        """The step's number and the states (the optimizer's own tensors, not copies)."""
+        return dict(steps=self.steps, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq,
+                    exp_avg_scale=self.exp_avg_scale, exp_avg_sq_scale=self.exp_avg_sq_scale)
+
+    def load_state_dict(self, state: dict) -> None:
+        """Takes over the values of a state_dict of the same parameters and state_bits."""
+        if (state["exp_avg_scale"] is None) != (self.state_bits == 32):
+            raise ValueError(f"the state is not one of {self.state_bits} bits")
+        for name in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
+            mine, theirs = getattr(self, name), state[name]
+            if mine is None:
+                continue
+            if [t.shape for t in mine] != [t.shape for t in theirs]:
+                raise ValueError(f"{name} has other shapes")
+            for a, b in zip(mine, theirs):
+                a.copy_(b)
+        self.steps = int(state["steps"])

@@ -233,3 +233,42 @@ def test_elements_past_2_to_the_32(eqb):  # noqa: F811
         assert np.abs(got - codes).max() <= 1
         far += int((got != codes).sum())
     assert far <= 2
+
+
+def test_on_another_stream(eqb):  # noqa: F811
+    m, o = Model(8, [5000, 3], 8, "bf16", True), Model(8, [5000, 3], 8, "bf16", True)
+    eqb.eqb_adamw_step(m.table(eqb), 2, seed=3, **HYPER)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        eqb.eqb_adamw_step(o.table(eqb), 2, seed=3, **HYPER)
+    s.synchronize()
+    for a, b in zip(m.tw + m.tc + m.tm + m.tv + m.sm + m.sv, o.tw + o.tc + o.tm + o.tv + o.sm + o.sv):
+        assert np.array_equal(bits_of(a), bits_of(b))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_optimizer_resumes(eqb, bits):  # noqa: F811
+    """An optimizer that takes over another's state goes on with the same bits."""
+    from paper_2609_28053_amd import AdamW
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    new = lambda: [torch.randn(s, generator=g, device="cuda") for s in ((64, 33), (5,), (300,))]  # noqa: E731
+    a = new()
+    kw = dict(lr=1e-2, weight_decay=[0.1, 0.0, 0.1], state_bits=bits, seed=7)
+    first = AdamW(a, **kw)
+    grads = [new() for _ in range(4)]
+    for k in range(2):
+        first.step(grads[k])
+    b = [p.clone() for p in a]
+    second = AdamW(b, **kw)
+    second.load_state_dict(first.state_dict())
+    for k in range(2, 4):
+        first.step(grads[k])
+        second.step(grads[k])
+    assert first.steps == second.steps == 4
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    with pytest.raises(ValueError):
+        AdamW(b, state_bits=40 - bits).load_state_dict(first.state_dict())
+    with pytest.raises(ValueError):
+        AdamW(b, state_bits=16)
