@@ -45,16 +45,39 @@ __device__ __forceinline__ float softmax_terms(const float (&x)[N], float (&w)[N
 }
 
 // ------------------------------------------------------------- the loss --
+// Every group is cut into pieces of a block's rows.  Where blocks went on from one group's
+// last rows to the next one's first, these were the last to finish: 99,991 rows of E = 128
+// in three groups 19.0 us, in pieces 17.5; 20,000 of E = 256 in 64 groups 13.8 and 9.8.
 // G = E/8 lanes hold a row, 8 experts each.  A lane sums the probabilities of its
-// experts over its rows in binary32; at the end of a block's piece of a group the block
-// adds its lanes' sums in binary64.  If the group has rows in other blocks too, the blocks
-// hand their pieces over (in binary32) through the workspace: the last of a bunch of
-// neighbours to come, by a ticket, adds theirs, and the last of those adds the sums, each in
-// a fixed order in binary64, and writes the group's results.  Who completes a count sets
-// its ticket back to 0.  Blocks sit on XCDs with an L2 each: pieces pass between them in
-// agent-scope stores and loads, complete (vmcnt) before the ticket is drawn.
+// experts over its rows in binary32; at the end of a piece the block adds its lanes' sums,
+// the waves' in binary64.  The pieces of a group are handed over (in binary32) through the
+// workspace: the last of a bunch of neighbours to come, by a ticket, adds theirs, and the
+// last of those adds the sums, each in a fixed order in binary64, and writes the group's
+// results.  Who completes a count sets its ticket back to 0.  Blocks sit on XCDs with an L2
+// each: pieces pass between them in agent-scope stores and loads, complete (vmcnt) before
+// the ticket is drawn.
 constexpr int kLossThreads = 768, kLossWaves = kLossThreads / 64;
 constexpr int kLossU = 2;          // rows per lane and step
+
+// The pieces: `rows` rows each, but for a group's last; group p's are first[p] to
+// first[p + 1] - 1, and first is above them all past first[P].
+constexpr int kPieceChunk = 16;
+struct Pieces {
+  int32_t first[EQB_MAX_PARTITIONS + kPieceChunk];
+  int32_t rows;
+};
+
+// The group of a piece, by a count of kPieceChunk groups at a time: a search would wait for
+// each of its loads, and the arguments are far away (20,000 rows in 64 groups: 9.8 us in
+// chunks of 16, 15.0 of 4).
+__device__ __forceinline__ int group_of(const Pieces& pieces, int P, int piece) {
+  int p = -1;
+  for (int q = 0; q < P; q += kPieceChunk) {
+#pragma unroll
+    for (int i = 0; i < kPieceChunk; ++i) p += pieces.first[q + i] <= piece ? 1 : 0;
+  }
+  return p;
+}
 
 __device__ __forceinline__ uint64_t pack_piece(float prob, int count) {
   return (uint64_t)__float_as_uint(prob) | ((uint64_t)(uint32_t)count << 32);
@@ -63,7 +86,7 @@ __device__ __forceinline__ uint64_t pack_piece(float prob, int count) {
 template <int E, bool kSoftmax, bool kMask>
 __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     const uint16_t* __restrict__ z, const int32_t* __restrict__ idx, const uint8_t* __restrict__ valid, int64_t T,
-    int K, const PartTable pt, int64_t rows_per_block, int bunch_bits, double alpha, const BalanceWorkspace ws, int32_t* load,
+    int K, const PartTable pt, const Pieces pieces, int bunch_bits, double alpha, const BalanceWorkspace ws, int32_t* load,
     int32_t* __restrict__ tokens, float* __restrict__ prob, float* __restrict__ loss) {
   constexpr int G = E / 8, R = 64 / G;
   constexpr uint32_t ROWS = kLossWaves * R * kLossU;
@@ -91,11 +114,12 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
   }
   if (tid < kNBins) (&sh_cnt[0][0])[tid] = 0;
   if (tid == 0) sh_tokens = 0;
-  int64_t r0, r1;
-  block_rows(T, rows_per_block, &r0, &r1);
-  for (int64_t s0 = r0; s0 < r1;) {
-    const int p = partition_of(pt, s0);
-    const int64_t s1 = pt.off[p + 1] < r1 ? pt.off[p + 1] : r1;
+  const int all = pieces.first[pt.P];
+  for (int piece = blockIdx.x; piece < all; piece += gridDim.x) {
+    const int p = group_of(pieces, pt.P, piece);
+    const int first = pieces.first[p], last = pieces.first[p + 1] - 1;
+    const int64_t s0 = pt.off[p] + (int64_t)(piece - first) * pieces.rows;
+    const int64_t s1 = pt.off[p + 1] < s0 + pieces.rows ? pt.off[p + 1] : s0 + pieces.rows;
     __syncthreads();
     float acc[8] = {};
     int n = 0;
@@ -181,16 +205,14 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     // the block's sums: over the rows of a wave, then over the waves
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-#pragma unroll
-      for (int off = G; off < 64; off <<= 1) acc[i] += __shfl_xor(acc[i], off);
+      acc[i] = column_sum<G>(acc[i]);
       if (lane < G) sh_sum[wave][8 * g + i] = acc[i];
     }
     if (kMask) {
-      for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
+      n = group_fold<64>(n, [](int a, int b) { return a + b; });
       if (lane == 0 && n) atomicAdd(&sh_tokens, n);
     }
     __syncthreads();
-    const int first = (int)(pt.off[p] / rows_per_block), last = (int)((pt.off[p + 1] - 1) / rows_per_block);
     double sum = 0.0;
     int64_t count = 0, nv = pt.off[p + 1] - pt.off[p];
     if (tid < E) {
@@ -203,13 +225,12 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     if (kMask) nv = sh_tokens;
     bool whole = true;             // sum, count and nv are the group's
     if (first < last) {
-      // Pieces of a bunch of neighbouring blocks are summed by the last of these to come, and
-      // the bunches' sums by the last to bring one.  A bunch of a group has place bunch + p:
-      // both only grow from piece to piece.
-      const int piece = (int)blockIdx.x + p, bunch = piece >> bunch_bits;
-      const int bunch0 = (first + p) >> bunch_bits, bunch1 = (last + p) >> bunch_bits;
-      const int i0 = bunch == bunch0 ? first + p : bunch << bunch_bits;
-      const int i1 = bunch == bunch1 ? last + p : ((bunch + 1) << bunch_bits) - 1;
+      // Pieces of a bunch of neighbours are summed by the last of these to come, and the
+      // bunches' sums by the last to bring one.  A bunch of a group has place bunch + p: both
+      // only grow from piece to piece.
+      const int bunch = piece >> bunch_bits, bunch0 = first >> bunch_bits, bunch1 = last >> bunch_bits;
+      const int i0 = bunch == bunch0 ? first : bunch << bunch_bits;
+      const int i1 = bunch == bunch1 ? last : ((bunch + 1) << bunch_bits) - 1;
       auto hand_over = [&](uint64_t* to, int32_t* to_tokens, int at, int32_t* ticket, int others) {
         if (tid < E)
           __hip_atomic_store(to + (int64_t)at * E + tid, pack_piece((float)sum, (int)count), __ATOMIC_RELAXED,
@@ -227,18 +248,18 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
         return sh_ticket == others;
       };
       auto collect = [&](const uint64_t* from, const int32_t* from_tokens, int lo, int hi) {
-        constexpr int J = kLossThreads / E;
+        constexpr int J = kLossThreads / E, kAhead = 8;
         const int e = tid % E, j = tid / E;
         sum = 0.0;
         count = 0;
-        for (int b0 = lo + j; b0 <= hi; b0 += 8 * J) {
-          uint64_t v[8];
+        for (int b0 = lo + j; b0 <= hi; b0 += kAhead * J) {
+          uint64_t v[kAhead];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kAhead; ++i)
             v[i] = b0 + i * J <= hi ? __hip_atomic_load(from + (int64_t)(b0 + i * J) * E + e, __ATOMIC_RELAXED,
                                                         __HIP_MEMORY_SCOPE_AGENT) : 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < kAhead; ++i) {
             sum += (double)__uint_as_float((uint32_t)v[i]);
             count += (int)(v[i] >> 32);
           }
@@ -284,7 +305,7 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
       if (tid < 64) {
         part = lane < E ? part : 0.0;
         for (int q = lane + 64; q < E; q += 64) part += sh_d[q];
-        for (int off = 32; off > 0; off >>= 1) part += __shfl_xor(part, off);
+        part = wave_sum(part);
         if (lane == 0) {
           loss[p] = (float)(alpha * part);
           tokens[p] = (int32_t)nv;
@@ -294,31 +315,55 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     } else if (tid == 0) {
       sh_tokens = 0;
     }
-    s0 = s1;
   }
+}
+
+// Pieces of the same number of rows as far as they go: no more than `most` of them where that
+// leaves the groups several each, or else up to one more for each group.  Returns the blocks
+// to launch for them.
+static int cut_groups(const PartTable& pt, int64_t T, int64_t most, Pieces* c) {
+  int64_t rows = 1;
+  auto cut = [&](int64_t n) {
+    int64_t all = 0;
+    rows = 1;
+    for (int p = 0; p < pt.P; ++p) {
+      const int64_t own = pt.off[p + 1] - pt.off[p], parts = (own + n - 1) / n;
+      c->first[p] = (int32_t)all;
+      all += parts;
+      if (parts > 0 && (own + parts - 1) / parts > rows) rows = (own + parts - 1) / parts;
+    }
+    return all;
+  };
+  int64_t all = cut(T > most ? (T + most - 1) / most : 1);
+  if (all > most && most >= 4 * pt.P) all = cut((T + most - pt.P - 1) / (most - pt.P));
+  all = cut(rows);          // evened out: every group has as many parts as before or fewer
+  c->first[pt.P] = (int32_t)all;
+  for (int p = pt.P + 1; p < EQB_MAX_PARTITIONS + kPieceChunk; ++p) c->first[p] = INT32_MAX;
+  c->rows = (int32_t)rows;
+  const int cap = max_blocks_cap();
+  return all < 1 ? 1 : cap > 0 && cap < all ? cap : (int)all;
 }
 
 template <int E, bool kSoftmax, bool kMask>
 static void launch_loss_as(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {
-  int blocks;
-  int64_t rpb;
+  int most;
+  int64_t rows;
   // One block for 32,768 logits, blocks of at least 16,384 beyond: 4,096 rows of E = 8 take
   // 8.8 us in one block and 12.4 in two, 16,384 rows of E = 64 8.7 in 64 and 9.4 in 32.
   // One block per compute unit for up to 2^26 logits (99,991 rows of E = 128 19.0 us, with
   // two 22.4; 147,456 of E = 256 24 either way), two beyond, where they hide more latency.
   const int64_t logits = a.T * E;
-  grid_for(a.T, logits <= 32768 ? 32768 / E : 16384 / E, logits <= 1 << 26 ? 1 : 2, &blocks, &rpb);
-  if (blocks > kBalanceBlocks) {
-    rpb = (a.T + kBalanceBlocks - 1) / kBalanceBlocks;
-    blocks = (int)((a.T + rpb - 1) / rpb);
-  }
+  grid_for(a.T, logits <= 32768 ? 32768 / E : 16384 / E, logits <= 1 << 26 ? 1 : 2, &most, &rows);
+  most = most < kBalanceBlocks ? most : kBalanceBlocks;
+  Pieces pieces;
+  const int blocks = cut_groups(a.pt, a.T, most, &pieces), all = pieces.first[a.pt.P];
   // Bunches pay where one block would read more than 256 KiB of pieces: 147,456 rows of E =
   // 256 in 512 blocks take 39.5 us without and 23.8 with them, 1,000,003 rows of E = 8 20.1
   // without and 23.7 with.  (10 bits: all blocks are one bunch.)
-  const int bunch_bits = (int64_t)blocks * E * (int64_t)sizeof(uint64_t) > (256 << 10) ? kBunchBits : 10;
+  const int bunch_bits = (int64_t)all * E * (int64_t)sizeof(uint64_t) > (256 << 10) ? kBunchBits : 10;
   static_assert(kBalanceBlocks + EQB_MAX_PARTITIONS <= 1 << 10, "one bunch");
   balance_loss_kernel<E, kSoftmax, kMask><<<blocks, kLossThreads, 0, s>>>(
-      a.z, a.idx, a.valid, a.T, a.K, a.pt, rpb, bunch_bits, a.alpha, ws, a.load, a.tokens, a.prob, a.loss);
+      a.z, a.idx, a.valid, a.T, a.K, a.pt, pieces, bunch_bits, a.alpha, ws, a.load, a.tokens, a.prob, a.loss);
 }
 template <int E>
 static void launch_loss_e(const BalanceArgs& a, const BalanceWorkspace& ws, hipStream_t s) {

@@ -242,6 +242,46 @@ __device__ __forceinline__ float group_max(float x) {
   return group_fold<G>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
+// Sum over the lanes that are congruent modulo G, the same in all of them: rotations within
+// 16 lanes, then swaps of 16 and of 32 lanes between two copies.
+template <int G>
+__device__ __forceinline__ float column_sum(float x) {
+  auto rotated = [&](auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  if constexpr (G <= 8) x += rotated(std::integral_constant<int, 0x128>{});
+  if constexpr (G <= 4) x += rotated(std::integral_constant<int, 0x124>{});
+  if constexpr (G <= 2) x += rotated(std::integral_constant<int, 0x122>{});
+  if constexpr (G <= 1) x += rotated(std::integral_constant<int, 0x121>{});
+  if constexpr (G <= 16) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+  }
+  if constexpr (G <= 32) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+  }
+  return x;
+}
+
+// Sum of binary64 values over the wave, the same in every lane.
+__device__ __forceinline__ double wave_sum(double x) {
+  auto rotated = [&](auto ctrl) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, decltype(ctrl)::value, 0xF, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), decltype(ctrl)::value, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  x += rotated(std::integral_constant<int, 0x128>{});
+  x += rotated(std::integral_constant<int, 0x124>{});
+  x += rotated(std::integral_constant<int, 0x122>{});
+  x += rotated(std::integral_constant<int, 0x121>{});
+  for (int off = 16; off < 64; off <<= 1) x += __shfl_xor(x, off);
+  return x;
+}
+
 // ------------------------------------------------------- float keys --
 // Routing keys are binary32 bit patterns kept in int registers and ordered
 // as floats.  A key is finite or the sentinel -inf, never NaN, and the keys

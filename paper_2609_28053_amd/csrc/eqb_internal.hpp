@@ -136,9 +136,9 @@ struct BalanceArgs {
 };
 
 // Working memory of the balance loss: the tickets (zero before and after a call), then the
-// blocks' pieces and the sums of bunches of them.  A block's rows overlap consecutive
-// groups, so block b's piece of group p has place b + p, its own alone.
-constexpr int kBalanceBlocks = 512;          // most blocks of a launch
+// groups' pieces and the sums of bunches of them.  There are up to kBalanceBlocks pieces, and
+// up to one more for each group.
+constexpr int kBalanceBlocks = 512;
 constexpr int kBunchBits = 4;                // 16 pieces
 struct BalanceWorkspace {
   int32_t* tickets;         // [EQB_MAX_PARTITIONS]
