@@ -394,8 +394,13 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // gradient is p q (C - sum p C) + (g + inj) sigmoid'.  The K mixture gradients of a row
 // are scattered into a per-wave LDS row of zeros, read back 4 at a time, and their
 // places zeroed again.
-// Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once and
-// non-temporal.  Two rows a lane and eight waves a SIMD: 4,194,304 rows of E = 256, K = 8
+// Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once.  The
+// gradient's stores are non-temporal, and so are the logits' loads when these take more than
+// a quarter of the memory-side cache (kStream); fewer are still there from the loss or the
+// routing.  With the loss before it, 99,991 rows of E = 128 (26 MB) 35.8 us with non-temporal
+// loads, 32.0 without; 131,072 of E = 256 (64 MiB) 56.0 and 55.2; 2,000,000 of E = 32 (128
+// MB) 96 and 105; the gradient alone of 4,194,304 of E = 256 1,274 and 1,325.
+// Two rows a lane and eight waves a SIMD: 4,194,304 rows of E = 256, K = 8
 // take 1,276 us (5.3 TB/s), with three rows and six waves 1,324, four and four 1,320, one
 // and eight 1,306; 1,000,003 of E = 128 161, 175, 161, 164.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;
@@ -409,8 +414,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // row's group holds at most one of its K pairs, or the router backward with any K (and
 // the injection without pairs).
 enum { kAlone, kOnePair, kAnyPairs };
+constexpr int64_t kGradStreamBytes = (int64_t)64 << 20;
 
-template <int E, bool kSoftmax, int kRouter>
+template <int E, bool kSoftmax, int kRouter, bool kStream>
 __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backward_kernel(
     const uint16_t* __restrict__ z, const int32_t* __restrict__ load, const int32_t* __restrict__ tokens,
     const float* __restrict__ grad_loss, const int32_t* __restrict__ idx, const float* __restrict__ gs,
@@ -463,7 +469,8 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
         on[u] = false;
         if (t < n) {
           on[u] = !valid || at<const uint8_t>(seg_valid, t) != 0;
-          zw[u] = __builtin_nontemporal_load(&at<const u32x2>(seg_z, (t * E + 4 * g) * 2u));
+          const u32x2& from = at<const u32x2>(seg_z, (t * E + 4 * g) * 2u);
+          zw[u] = kStream ? __builtin_nontemporal_load(&from) : from;
           if (kRouter == kOnePair && g < K) {
             e[u] = at<const int32_t>(seg_idx, (t * K + g) * 4u);
             gv[u] = at<const float>(seg_gs, (t * K + g) * 4u);
@@ -565,7 +572,10 @@ static void launch_backward_as(const BalanceArgs& a, hipStream_t s) {
   int blocks;
   int64_t rpb;
   grid_for(a.T, kGradWaves * (256 / E) * kGradU, kGradBlocksPerCu, &blocks, &rpb);
-  balance_backward_kernel<E, kSoftmax, kRouter><<<blocks, kGradThreads, 0, s>>>(
+  const bool stream = a.T * E * (int64_t)sizeof(uint16_t) > kGradStreamBytes;
+  const auto kernel = stream ? balance_backward_kernel<E, kSoftmax, kRouter, true>
+                             : balance_backward_kernel<E, kSoftmax, kRouter, false>;
+  kernel<<<blocks, kGradThreads, 0, s>>>(
       a.z, a.load, a.tokens, a.grad_loss, a.idx, a.grad_score, a.inj, a.valid, a.T, a.K, a.pt, rpb, a.alpha, a.grad_z);
 }
 template <int E, bool kSoftmax>

@@ -293,3 +293,34 @@ def test_masks_of_the_lowest_value(eqb, E, softmax):  # noqa: F811
     got = run(eqb, c, softmax, router=False)
     assert np.all(np.isfinite(got["gz"])) and np.all(np.isfinite(got["prob"]))
     check(c, got, softmax, router=False)
+
+
+@pytest.mark.parametrize("E,K,router", [(256, 8, True), (128, 4, False), (8, 4, True)])
+@pytest.mark.parametrize("softmax", [False, True])
+def test_gradient_of_a_large_batch(eqb, E, K, router, softmax):  # noqa: F811
+    """Logits that the memory-side cache does not keep take other loads; a row's gradient is the same in a batch of
+    half the size."""
+    T = (1 << 25) // E + 777
+    g = torch.Generator(device="cuda")
+    g.manual_seed(E)
+    d = dict(device="cuda")
+    z = torch.randn((T, E), generator=g, **d).to(torch.bfloat16).view(torch.int16)
+    valid = torch.rand(T, generator=g, **d) < 0.9
+    load = torch.randint(0, T, (1, E), generator=g, **d).int()
+    tokens, one = torch.full((1,), T, dtype=torch.int32, **d), torch.ones(1, **d)
+    pairs = {}
+    if router:
+        pairs = dict(topk_idx=torch.arange(T * K, **d).view(T, K).remainder_(E).int(),
+                     grad_score=torch.randn((T, K), generator=g, **d))
+    inj = dict(inj=torch.randn((1, E), generator=g, **d)) if router else {}
+    say(f"balance gradient T={T} E={E} K={K} router={router} softmax={softmax}")
+    kw = dict(score=eqb.EQB_SCORE_SOFTMAX if softmax else eqb.EQB_SCORE_SIGMOID)
+    whole, half = torch.full((T, E), 7.0, **d), torch.empty((T // 2, E), **d)
+    eqb.eqb_balance_backward(z, load, tokens, K, 1e-2, one, whole, valid=valid, **pairs, **inj, **kw)
+    eqb.eqb_balance_backward(z[:T // 2], load, tokens, K, 1e-2, one, half, valid=valid[:T // 2],
+                             **{n: t[:T // 2] for n, t in pairs.items()}, **inj, **kw)
+    assert torch.equal(whole[:T // 2], half)
+    eqb.eqb_balance_backward(z[-(T // 2):], load, tokens, K, 1e-2, one, half, valid=valid[-(T // 2):],
+                             **{n: t[-(T // 2):] for n, t in pairs.items()}, **inj, **kw)
+    assert torch.equal(whole[-(T // 2):], half)
+    assert bool((whole[~valid] == 0).all())
