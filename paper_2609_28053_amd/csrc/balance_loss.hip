@@ -131,16 +131,16 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
       const uint32_t rows = (uint32_t)(s1 - c0 < kSegMax ? s1 - c0 : kSegMax);
       // rows past the last one read the last one, and count as 0
       auto row_of = [&](uint32_t base, int u) { return base + (uint32_t)((u * kLossWaves + wave) * R + rr); };
-      auto fetch = [&](uint32_t base, uint4 (&zw)[kLossU], bool (&on)[kLossU]) {
+      auto fetch = [&](uint32_t base, uint4 (&zw)[kLossU], uint32_t (&vb)[kLossU]) {
 #pragma unroll
         for (int u = 0; u < kLossU; ++u) {
           const uint32_t t = row_of(base, u), tc = t < rows ? t : rows - 1;
           zw[u] = at<const uint4>(zc, (tc * E + 8 * g) * 2u);
-          on[u] = t < rows && (!kMask || at<const uint8_t>(vc, tc) != 0);
+          vb[u] = kMask ? at<const uint8_t>(vc, tc) : 1u;
         }
       };
       uint4 zn[kLossU];
-      bool next[kLossU];
+      uint32_t next[kLossU];         // the mask's bytes: to compare them here would wait for them
       fetch(0, zn, next);
       if (idx) {
         const int32_t* ic = idx + cu * K;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
 #pragma unroll
         for (int u = 0; u < kLossU; ++u) {
           zw[u] = zn[u];
-          on[u] = next[u];
+          on[u] = row_of(base, u) < rows && next[u] != 0;
         }
         fetch(base + ROWS, zn, next);
 #pragma unroll
@@ -459,16 +459,16 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
     }
     auto row_of = [&](uint32_t base, int u) -> uint32_t { return base + (uint32_t)((wave * kGradU + u) * R + rr); };
     // logits, mask and this lane's pair of its rows at step base
-    auto fetch = [&](uint32_t base, u32x2 (&zw)[kGradU], bool (&on)[kGradU], int (&e)[kGradU], float (&gv)[kGradU]) {
+    auto fetch = [&](uint32_t base, u32x2 (&zw)[kGradU], uint32_t (&vb)[kGradU], int (&e)[kGradU], float (&gv)[kGradU]) {
 #pragma unroll
       for (int u = 0; u < kGradU; ++u) {
         const uint32_t t = row_of(base, u);
         zw[u] = u32x2{0, 0};
         e[u] = -1;
         gv[u] = 0.0f;
-        on[u] = false;
+        vb[u] = 0;
         if (t < n) {
-          on[u] = !valid || at<const uint8_t>(seg_valid, t) != 0;
+          vb[u] = valid ? at<const uint8_t>(seg_valid, t) : 1;
           const u32x2& from = at<const u32x2>(seg_z, (t * E + 4 * g) * 2u);
           zw[u] = kStream ? __builtin_nontemporal_load(&from) : from;
           if (kRouter == kOnePair && g < K) {
@@ -479,10 +479,10 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
       }
     };
     u32x2 zn[kGradU];
-    bool onn[kGradU];
+    uint32_t vn[kGradU];           // the mask's bytes: to compare them here would wait for them
     int en[kGradU];
     float gn[kGradU];
-    fetch(0, zn, onn, en, gn);
+    fetch(0, zn, vn, en, gn);
     for (uint32_t base = 0; base < n; base += ROWS) {
       u32x2 zw[kGradU];
       bool on[kGradU];
@@ -490,13 +490,13 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
       float gc[kGradU];
 #pragma unroll
       for (int u = 0; u < kGradU; ++u) {
-        on[u] = onn[u];
+        on[u] = vn[u] != 0;
         // whatever a masked token holds
         zw[u] = on[u] ? zn[u] : u32x2{0, 0};
         ec[u] = on[u] ? en[u] : -1;
         gc[u] = gn[u];
       }
-      if (base + ROWS < n) fetch(base + ROWS, zn, onn, en, gn);
+      if (base + ROWS < n) fetch(base + ROWS, zn, vn, en, gn);
       // scatter the rows' mixture gradients
       if (kRouter != kAlone) {
 #pragma unroll
