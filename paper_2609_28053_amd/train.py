@@ -112,7 +112,8 @@ class AdamW:
         self._tensors = None
 
     def step(self, grads, lr=None, grad_scale=None, found_inf=None, stream=None):
-        """One step with these gradients, one per parameter, all binary32 or all BF16."""
+        """One step with these gradients, one per parameter, all binary32 or all BF16.  A step that found_inf
+        skips counts in steps as well: its value is on the device, and nothing waits for it."""
         if self._tensors is None:
             self._tensors = eqb.AdamwTensors(self.params, grads, self.exp_avg, self.exp_avg_sq, self.copies,
                                              self.exp_avg_scale, self.exp_avg_sq_scale, self.weight_decay)
