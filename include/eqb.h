@@ -355,7 +355,9 @@ eqb_status eqb_layer_noalloc(const uint16_t* z, const float* b, int64_t T, int32
  *   prob [P,E] binary32 (out); loss [P] binary32 (out).
  *   workspace: eqb_balance_workspace_size(E, P) bytes, 256-byte aligned, owned
  *     by the caller, zeroed once after allocation; each call leaves its leading
- *     counters zero again.  Two calls whose work may overlap need two.
+ *     counters zero again, wherever E and P put the rest, so that one workspace of
+ *     the largest size serves calls of all sizes.  Two calls whose work may overlap
+ *     need two.
  * A row's probabilities and a lane's sum over its rows are binary32, the sums of
  * those binary64 (handed from block to block in binary32); the result does not
  * depend on the order in which blocks run.  T = 0 writes zeros (`load` too, with or without topk_idx).

@@ -137,20 +137,23 @@ struct BalanceArgs {
 
 // Working memory of the balance loss: the tickets (zero before and after a call), then the
 // groups' pieces and the sums of bunches of them.  There are up to kBalanceBlocks pieces, and
-// up to one more for each group.
+// up to one more for each group.  The tickets lie where they lie for every E and P, so that a
+// workspace that was large enough for one call serves another of other sizes.
 constexpr int kBalanceBlocks = 512;
 constexpr int kBunchBits = 4;                // 16 pieces
+constexpr int balance_bunches(int P) { return ((kBalanceBlocks + P) >> kBunchBits) + P + 1; }
 struct BalanceWorkspace {
   int32_t* tickets;         // [EQB_MAX_PARTITIONS]
-  int32_t* bunch_tickets;   // [bunches]
+  int32_t* bunch_tickets;   // [balance_bunches(EQB_MAX_PARTITIONS)]
   int32_t* tokens;          // [kBalanceBlocks + P]
-  int32_t* bunch_tokens;    // [bunches], ((kBalanceBlocks + P) >> kBunchBits) + P + 1 of them
+  int32_t* bunch_tokens;    // [balance_bunches(P)]
   uint64_t* pieces;         // [kBalanceBlocks + P, E]: binary32 sum of probabilities, count
-  uint64_t* bunches;        // [bunches, E]
+  uint64_t* bunches;        // [balance_bunches(P), E]
 };
 inline size_t balance_workspace(void* base, int E, int P, BalanceWorkspace* w) {
-  const size_t pieces = (size_t)kBalanceBlocks + P, bunches = (pieces >> kBunchBits) + P + 1;
-  const size_t at1 = align256(EQB_MAX_PARTITIONS * sizeof(int32_t)), at2 = at1 + align256(bunches * sizeof(int32_t));
+  const size_t pieces = (size_t)kBalanceBlocks + P, bunches = balance_bunches(P);
+  const size_t at1 = align256(EQB_MAX_PARTITIONS * sizeof(int32_t));
+  const size_t at2 = at1 + align256(balance_bunches(EQB_MAX_PARTITIONS) * sizeof(int32_t));
   const size_t at3 = at2 + align256(pieces * sizeof(int32_t)), at4 = at3 + align256(bunches * sizeof(int32_t));
   const size_t at5 = at4 + align256(pieces * E * sizeof(uint64_t));
   if (base && w) {
