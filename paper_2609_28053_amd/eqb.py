@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -493,9 +494,39 @@ def eqb_combine_backward(grad_y, expert_rows, slot, weight, grad_rows, grad_weig
         _ptr(grad_weight, torch.float32, T * K, "grad_weight"), _stream(stream)))
 
 
+_dtype_of, _on_gpu = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
+
+
+def _addresses(tensors):
+    return list(map(torch.Tensor.data_ptr, tensors))
+
+
+def _same(tensors, others):
+    return len(tensors) == len(others) and all(map(operator.is_, tensors, others))
+
+
+def _values(x):
+    """A number, or a list of numbers."""
+    try:
+        return list(x)
+    except TypeError:
+        return float(x)
+
+
+def _ptrs(tensors, dtype, numel, name):
+    """_ptr of each tensor of a list (217 tensors: 94 us, one by one 126)."""
+    if (all(isinstance(t, torch.Tensor) for t in tensors) and all(map(_on_gpu, tensors)) and
+            all(map(torch.Tensor.is_contiguous, tensors)) and set(map(_dtype_of, tensors)) <= {dtype} and
+            list(map(torch.Tensor.numel, tensors)) == numel):
+        return _addresses(tensors)
+    return [_ptr(t, dtype, n, name) for t, n in zip(tensors, numel)]
+
+
 class AdamwTensors:
     """The tensors of an AdamW step, converted once for repeated calls.  It
-    keeps the tensors alive that it names; ``set_grads`` exchanges the
+    stands for the memory that the tensors have when they are given, and keeps
+    that memory: a tensor that is given other memory later (``p.data = ...``,
+    as Module.to does) is followed by ``refresh``.  ``set_grads`` exchanges the
     gradients.  Parameters are binary32; ``copies``, if given, are BF16
     tensors that receive the new parameters.  Either binary32 states, or 8-bit
     ones (torch.float8_e4m3fn) with their blocks' scales: exp_avg times
@@ -514,35 +545,58 @@ class AdamwTensors:
         self.numel = [p.numel() for p in params]
         self.table = np.zeros(self.n, dtype=self._FIELDS)
         self.table["numel"] = self.numel
-        self.table["weight_decay"] = weight_decay
-        blocks = [-(-n // EQB_ADAMW_BLOCK) for n in self.numel]
+        # per field: the tensors and their memory, which so outlives the tensors' hold on it
+        self._held = {}
+        self._all, self._at, self._decay = None, None, None
+        self.refresh(params, exp_avg, exp_avg_sq, copies, exp_avg_scale, exp_avg_sq_scale, weight_decay)
+        self.set_grads(grads)
+
+    def refresh(self, params, exp_avg, exp_avg_sq, copies=None, exp_avg_scale=None, exp_avg_sq_scale=None,
+                weight_decay=0.0):
+        """Takes over the tensors' memory and the decay where they differ from the table's; sizes and types stay.
+        Returns whether any memory did."""
+        decay = weight_decay if type(weight_decay) is float else _values(weight_decay)
+        if decay != self._decay:
+            self.table["weight_decay"] = decay
+            self._decay = decay
+        tensors = [*params, *exp_avg, *exp_avg_sq, *(copies or ()), *(exp_avg_scale or ()), *(exp_avg_sq_scale or ())]
+        # the same tensors at the same addresses: their sizes and types were looked at
+        if self._all is not None and _same(tensors, self._all) and _addresses(tensors) == self._at:
+            return False
+        if ((exp_avg_scale is None) or (exp_avg_sq_scale is None)) != (self.state_bits == 32):
+            raise ValueError(f"the table is one of {self.state_bits}-bit states")
+        self._all = None
         state = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
-        self._kept = []
+        blocks = [-(-n // EQB_ADAMW_BLOCK) for n in self.numel]
         self._set("param", params, torch.float32, self.numel)
         self._set("copy", copies, torch.bfloat16, self.numel)
         self._set("exp_avg", exp_avg, state, self.numel)
         self._set("exp_avg_sq", exp_avg_sq, state, self.numel)
         self._set("exp_avg_scale", exp_avg_scale, torch.float32, blocks)
         self._set("exp_avg_sq_scale", exp_avg_sq_scale, torch.float32, blocks)
-        self.set_grads(grads)
+        self._all, self._at = tensors, _addresses(tensors)
+        return True
 
     def _set(self, field, tensors, dtype, numel):
         if tensors is None:
+            self.table[field] = 0
+            self._held.pop(field, None)
             return
         if len(tensors) != self.n:
             raise ValueError(f"{len(tensors)} {field} tensors for {self.n} parameters")
-        self.table[field] = [_ptr(t, dtype, n, field) for t, n in zip(tensors, numel)]
-        self._kept.append(list(tensors))
+        self.table[field] = _ptrs(tensors, dtype, numel, field)
+        self._held[field] = list(tensors), list(map(torch.Tensor.untyped_storage, tensors))
 
     def set_grads(self, grads):
         """Gradients of the next step, one per parameter, all binary32 or all BF16."""
-        dtype = grads[0].dtype if self.n else torch.float32
+        dtype = grads[0].dtype if self.n and len(grads) else torch.float32
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"gradients have dtype {dtype}, expected torch.float32 or torch.bfloat16")
-        if len(grads) != self.n:
-            raise ValueError(f"{len(grads)} gradients for {self.n} parameters")
-        self.table["grad"] = [_ptr(g, dtype, n, "grad") for g, n in zip(grads, self.numel)]
-        self.grads = list(grads)
+        held = self._held.get("grad")
+        if held is not None and _same(grads, held[0]) and _addresses(grads) == self._grads_at:
+            return
+        self._set("grad", grads, dtype, self.numel)
+        self._grads_at = self.table["grad"].tolist()
         self.grad_dtype = _ROW_TYPES[dtype]
 
 

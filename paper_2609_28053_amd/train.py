@@ -91,7 +91,9 @@ class AdamW:
     """AdamW over a list of binary32 parameters, in place, one call a step.
     state_bits: 32, or 8 for E4M3 states with a scale per 256 elements.
     copies: BF16 tensors that receive the new parameters.  weight_decay: one
-    value, or one per parameter."""
+    value, or one per parameter.  Every step takes the memory that parameters,
+    copies and states have then, and lr, betas, eps, weight_decay and seed as
+    they are then."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
                  seed=0):
@@ -114,10 +116,12 @@ class AdamW:
     def step(self, grads, lr=None, grad_scale=None, found_inf=None, stream=None):
         """One step with these gradients, one per parameter, all binary32 or all BF16.  A step that found_inf
         skips counts in steps as well: its value is on the device, and nothing waits for it."""
+        tensors = (self.params, self.exp_avg, self.exp_avg_sq, self.copies, self.exp_avg_scale, self.exp_avg_sq_scale,
+                   self.weight_decay)
         if self._tensors is None:
-            self._tensors = eqb.AdamwTensors(self.params, grads, self.exp_avg, self.exp_avg_sq, self.copies,
-                                             self.exp_avg_scale, self.exp_avg_sq_scale, self.weight_decay)
+            self._tensors = eqb.AdamwTensors(self.params, grads, *tensors[1:])
         else:
+            self._tensors.refresh(*tensors)
             self._tensors.set_grads(grads)
         self.steps += 1
         eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,

@@ -1,0 +1,104 @@
+"""The training handles' host side without a GPU: the library's calls are replaced by
+recorders, and tensors of the CPU pass for the GPU's."""
+import pytest
+import torch
+
+from paper_2609_28053_amd import AdamW, eqb
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The arguments of every optimizer call, with the table's columns as they were."""
+    def ptr(t, dtype=None, numel=None, name="tensor"):
+        if t is None:
+            return None
+        if not t.is_contiguous() or (numel is not None and t.numel() != numel):
+            raise ValueError(name)
+        if dtype is not None and t.dtype is not dtype:
+            raise TypeError(name)
+        return t.data_ptr()
+
+    seen = []
+
+    def step(tensors, number, lr, beta1=0.9, beta2=0.95, eps=1e-8, seed=0, grad_scale=None, found_inf=None, stream=None):
+        seen.append(dict({n: tensors.table[n].tolist() for n in tensors.table.dtype.names}, step=number, lr=lr))
+
+    monkeypatch.setattr(eqb, "_ptr", ptr)
+    monkeypatch.setattr(eqb, "eqb_adamw_step", step)
+    return seen
+
+
+def at(tensors):
+    return [t.data_ptr() for t in tensors]
+
+
+def model(bits=8):
+    params = [torch.nn.Parameter(torch.randn(s)) for s in ((4, 5), (3,), (300,))]
+    copies = [p.detach().to(torch.bfloat16) for p in params]
+    return params, copies, AdamW(params, copies=copies, state_bits=bits, weight_decay=[0.1, 0.0, 0.2])
+
+
+def grads_of(params):
+    return [torch.randn_like(p) for p in params]
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_takes_the_memory_that_the_tensors_have_then(calls, bits):
+    """Parameters, copies and states that were given other memory, or replaced in the optimizer's lists."""
+    params, copies, opt = model(bits)
+    opt.step(grads_of(params))
+    params[0].data = params[0].data.clone()
+    copies[1].data = copies[1].data.clone()
+    opt.exp_avg[2] = opt.exp_avg[2].clone()
+    opt.exp_avg_sq[0].data = opt.exp_avg_sq[0].data.clone()
+    if bits == 8:
+        opt.exp_avg_scale[1] = opt.exp_avg_scale[1].clone()
+    for _ in range(2):
+        grads = grads_of(params)
+        opt.step(grads)
+        got = calls[-1]
+        assert got["param"] == at(params) and got["copy"] == at(copies) and got["grad"] == at(grads)
+        assert got["exp_avg"] == at(opt.exp_avg) and got["exp_avg_sq"] == at(opt.exp_avg_sq)
+        if bits == 8:
+            assert got["exp_avg_scale"] == at(opt.exp_avg_scale) and got["exp_avg_sq_scale"] == at(opt.exp_avg_sq_scale)
+
+
+def test_a_tables_memory_outlives_its_tensors(calls):
+    """What a table names stays allocated while the table stands, whatever becomes of the tensors: it owns the storages
+    that its addresses lie in."""
+    params, copies, opt = model()
+    grads = grads_of(params)
+    table = eqb.AdamwTensors(params, grads, opt.exp_avg, opt.exp_avg_sq, copies, opt.exp_avg_scale, opt.exp_avg_sq_scale)
+    kept = [t.untyped_storage()._cdata for t in params + copies + grads]
+    before = table.table.copy()
+    for t in params + copies + grads:
+        t.data = torch.zeros_like(t.data)
+    held = {s._cdata for _, storages in table._held.values() for s in storages}
+    assert held.issuperset(kept) and (table.table == before).all()
+
+
+def test_the_decay_of_a_step_is_the_one_it_has_then(calls):
+    params, _, opt = model()
+    opt.step(grads_of(params))
+    opt.weight_decay[1] = 0.7
+    opt.step(grads_of(params))
+    opt.weight_decay = 0.25
+    opt.step(grads_of(params))
+    assert [c["weight_decay"] for c in calls] == [[0.1, 0.0, 0.2], [0.1, 0.7, 0.2], [0.25] * 3]
+
+
+def test_memory_of_another_kind_is_refused(calls):
+    params, copies, opt = model()
+    opt.step(grads_of(params))
+    params[2].data = torch.zeros(5)
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(4, 5), torch.zeros(3), torch.zeros(300)])
+    params[2].data = torch.zeros(300, dtype=torch.float64)
+    with pytest.raises(TypeError):
+        opt.step([torch.zeros(4, 5), torch.zeros(3), torch.zeros(300)])
+    params[2].data = torch.zeros(300)
+    copies.append(torch.zeros(2, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(4, 5), torch.zeros(3), torch.zeros(300)])
+    with pytest.raises(ValueError):
+        opt.step([])
