@@ -3,8 +3,11 @@
 Every function takes torch tensors that live on the GPU (except ``part_off``,
 a host sequence of P+1 token offsets) and passes their device pointers and the
 current HIP stream to the C ABI of the same name.  All computation happens in
-the library's kernels; torch only provides device memory and streams.  A
-missing or unloadable library raises ImportError: there is no fallback.
+the library's kernels; torch only provides device memory and streams.  With
+``stream`` the caller orders that stream behind the work that makes the
+tensors, and keeps them allocated until its work is done
+(torch.Tensor.record_stream).  A missing or unloadable library raises
+ImportError: there is no fallback.
 """
 from __future__ import annotations
 

@@ -3,15 +3,67 @@
 Each class owns the buffers of one operator and makes the calls of ``eqb`` on
 them; all computation happens in the library's kernels.  Work is enqueued on
 the current stream (or ``stream``), nothing synchronises.
+
+With ``stream`` the caller orders that stream behind the work that makes the
+arguments.  What a call returns is allocated on the stream that it is computed
+on; a handle's own buffers, which its constructor fills on the stream current
+there, and the arguments stay allocated until the work on ``stream`` is done.
+Calls of one handle on several streams are ordered by the caller.
 """
 from __future__ import annotations
+
+import contextlib
 
 import torch
 
 from . import eqb
 
 
-class ExpertRows:
+class _Handle:
+    """A handle's buffers and the streams that are behind their fills."""
+
+    _fill = None
+
+    def _filled(self, device):
+        """After the constructor's fills on the current stream."""
+        device = torch.device(device)
+        if device.type == "cuda":
+            stream = torch.cuda.current_stream(device)
+            self._fill = torch.cuda.Event()
+            self._fill.record(stream)
+            self._behind = {stream.cuda_stream}
+
+    def _buffers(self):
+        """The handle's own buffers that calls on any stream use."""
+        return ()
+
+    def _on(self, stream, *given):
+        """The context of a call on a stream: what it allocates is the stream's, and the handle's buffers (at its first
+        call there) and the given tensors are known to be used there."""
+        if self._fill is None:                # no GPU buffers: the call itself says so
+            return contextlib.nullcontext()
+        first = eqb._stream(stream) not in self._behind
+        if stream is None and not first:
+            return contextlib.nullcontext()
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+        if first:
+            with torch.cuda.stream(stream):
+                capturing = torch.cuda.is_current_stream_capturing()
+            if not capturing:                 # a capture begins behind all work, and may wait for none of it
+                stream.wait_event(self._fill)
+                self._behind.add(stream.cuda_stream)
+            for t in self._buffers():
+                t.record_stream(stream)
+        for t in given:
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
+        return torch.cuda.stream(stream)
+
+
+class ExpertRows(_Handle):
     """The experts' rows of T tokens (Eq. 1): the order of the routed pairs,
     dispatch of the tokens' rows, combine of what the experts return, and the
     gradients of both.  Expert e's rows are offsets[e] .. offsets[e + 1] - 1."""
@@ -22,37 +74,45 @@ class ExpertRows:
         self.offsets = torch.empty(E + 1, **i32)
         self.slot = torch.empty((T, K), **i32)
         self.workspace = torch.empty(eqb.eqb_dispatch_workspace_size(T, K, E), dtype=torch.uint8, device=i32["device"])
+        self._filled(device)
+
+    def _buffers(self):
+        return self.offsets, self.slot, self.workspace
 
     def plan(self, topk_idx, stream=None):
         """Orders the pairs of topk_idx [T,K]; entries outside [0, E) are dropped."""
-        eqb.eqb_dispatch_plan(topk_idx, self.E, self.offsets, self.slot, self.workspace, stream)
+        with self._on(stream, topk_idx):
+            eqb.eqb_dispatch_plan(topk_idx, self.E, self.offsets, self.slot, self.workspace)
         return self
 
     def dispatch(self, x, rows=None, stream=None):
         """The tokens' rows x [T,H] in the experts' order [T*K,H] (rows past offsets[E] are not written)."""
-        if rows is None:
-            rows = torch.empty((self.T * self.K, x.shape[1]), dtype=x.dtype, device=x.device)
-        eqb.eqb_dispatch(x, self.slot, rows, stream)
+        with self._on(stream, x, rows):
+            if rows is None:
+                rows = torch.empty((self.T * self.K, x.shape[1]), dtype=x.dtype, device=x.device)
+            eqb.eqb_dispatch(x, self.slot, rows)
         return rows
 
     def combine(self, rows, weight=None, y=None, stream=None):
         """sum_k weight[t, k] rows[slot[t, k]] for every token; without weight, the gradient of dispatch."""
-        if y is None:
-            y = torch.empty((self.T, rows.shape[1]), dtype=rows.dtype, device=rows.device)
-        eqb.eqb_combine(rows, self.slot, weight, y, stream)
+        with self._on(stream, rows, weight, y):
+            if y is None:
+                y = torch.empty((self.T, rows.shape[1]), dtype=rows.dtype, device=rows.device)
+            eqb.eqb_combine(rows, self.slot, weight, y)
         return y
 
     def combine_backward(self, grad_y, rows, weight, grad_rows=None, grad_weight=None, stream=None):
         """Gradients of combine with respect to the rows and to the weights (the router backward's grad_score)."""
-        if grad_rows is None:
-            grad_rows = torch.empty_like(rows)
-        if grad_weight is None:
-            grad_weight = torch.empty_like(weight)
-        eqb.eqb_combine_backward(grad_y, rows, self.slot, weight, grad_rows, grad_weight, stream)
+        with self._on(stream, grad_y, rows, weight, grad_rows, grad_weight):
+            if grad_rows is None:
+                grad_rows = torch.empty_like(rows)
+            if grad_weight is None:
+                grad_weight = torch.empty_like(weight)
+            eqb.eqb_combine_backward(grad_y, rows, self.slot, weight, grad_rows, grad_weight)
         return grad_rows, grad_weight
 
 
-class BalanceLoss:
+class BalanceLoss(_Handle):
     """The auxiliary balance loss of P groups over T tokens, its loads, and its
     gradient with the router backward.  score: "sigmoid" (normalised) or
     "softmax"."""
@@ -67,27 +127,33 @@ class BalanceLoss:
         self.prob = torch.empty((P, E), dtype=torch.float32, device=dev)
         self.loss = torch.empty(P, dtype=torch.float32, device=dev)
         self.workspace = torch.zeros(eqb.eqb_balance_workspace_size(E, P), dtype=torch.uint8, device=dev)
+        self._filled(dev)
+
+    def _buffers(self):
+        return self._counts, self.tokens, self.prob, self.loss, self.workspace
 
     def forward(self, z, topk_idx=None, valid=None, part_off=None, load=None, stream=None):
         """The groups' losses [P] (self.loss); counts topk_idx, or takes the routing's loads."""
         if (topk_idx is None) == (load is None):
             raise ValueError("give topk_idx to count, or the loads that the routing counted")
         self.load = self._counts if load is None else load
-        eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, self.load, self.tokens, self.prob, self.loss,
-                             self.workspace, valid, part_off, self.score, stream)
+        with self._on(stream, z, topk_idx, valid, load):
+            eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, self.load, self.tokens, self.prob, self.loss,
+                                 self.workspace, valid, part_off, self.score)
         return self.loss
 
     def backward(self, z, grad_loss, grad_z=None, topk_idx=None, grad_score=None, inj=None, valid=None,
                  part_off=None, stream=None):
         """The gradient with respect to z; with topk_idx and grad_score (and inj), the whole router's."""
-        if grad_z is None:
-            grad_z = torch.empty((self.T, self.E), dtype=torch.float32, device=z.device)
-        eqb.eqb_balance_backward(z, self.load, self.tokens, self.K, self.alpha, grad_loss, grad_z, topk_idx, grad_score,
-                                 inj, valid, part_off, self.score, stream)
+        with self._on(stream, z, grad_loss, grad_z, topk_idx, grad_score, inj, valid, self.load):
+            if grad_z is None:
+                grad_z = torch.empty((self.T, self.E), dtype=torch.float32, device=z.device)
+            eqb.eqb_balance_backward(z, self.load, self.tokens, self.K, self.alpha, grad_loss, grad_z, topk_idx, grad_score,
+                                     inj, valid, part_off, self.score)
         return grad_z
 
 
-class AdamW:
+class AdamW(_Handle):
     """AdamW over a list of binary32 parameters, in place, one call a step.
     state_bits: 32, or 8 for E4M3 states with a scale per 256 elements.
     copies: BF16 tensors that receive the new parameters.  weight_decay: one
@@ -112,6 +178,11 @@ class AdamW:
             self.exp_avg_scale = self.exp_avg_sq_scale = None
         self.exp_avg, self.exp_avg_sq = new(), new()
         self._tensors = None
+        self._filled(self.params[0].device if self.params else "cpu")
+
+    def _buffers(self):
+        return [t for ts in (self.params, self.copies, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
+                             self.exp_avg_sq_scale) for t in ts or ()]
 
     def step(self, grads, lr=None, grad_scale=None, found_inf=None, stream=None):
         """One step with these gradients, one per parameter, all binary32 or all BF16.  A step that found_inf
@@ -121,11 +192,13 @@ class AdamW:
         if self._tensors is None:
             self._tensors = eqb.AdamwTensors(self.params, grads, *tensors[1:])
         else:
-            self._tensors.refresh(*tensors)
+            if self._tensors.refresh(*tensors) and self._fill is not None:
+                self._behind.clear()          # memory that no stream is known to use
             self._tensors.set_grads(grads)
         self.steps += 1
-        eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,
-                           grad_scale, found_inf, stream)
+        with self._on(stream, grad_scale, found_inf, *grads):
+            eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,
+                               grad_scale, found_inf)
 
     def state_dict(self) -> dict:
         """The step's number and the states (the optimizer's own tensors, not copies)."""

@@ -1,8 +1,8 @@
-"""The training handles on the GPU: tensors that change their memory."""
+"""The training handles on the GPU: tensors that change their memory, and streams of their own."""
 import pytest
 import torch
 
-from paper_2609_28053_amd import AdamW
+from paper_2609_28053_amd import AdamW, BalanceLoss, ExpertRows
 from test_gpu_balance import say
 
 pytestmark = pytest.mark.gpu
@@ -35,3 +35,81 @@ def test_a_parameter_that_moves_is_followed(bits):
     b.step(second)
     assert all(torch.equal(p, q) for p, q in zip(still, moved))
     assert torch.equal(old, was) and not torch.equal(moved[0], was)
+
+
+T, E, K, H, P = 5000, 64, 4, 256, 3
+
+
+def inputs():
+    z, x, out, gy = tensors(3, (T, E), (T, H), (T * K, H), (T, H))
+    idx = z.topk(K, dim=1).indices.to(torch.int32)
+    bf = lambda t: t.to(torch.bfloat16)  # noqa: E731
+    return dict(z=bf(z).view(torch.int16), idx=idx, x=bf(x), out=bf(out), gy=bf(gy), w=torch.sigmoid(z).gather(1, idx.long()),
+                one=torch.ones(P, **D), valid=z[:, 0] < 1.0, grads=tensors(4, *SHAPES))
+
+
+def pass_of(rows, loss, opt, i, stream):
+    part = [0, 100, 3000, T]
+    got = dict(rows=rows.plan(i["idx"], stream=stream).dispatch(i["x"], stream=stream)[:int(T * K)])
+    got["y"] = rows.combine(i["out"], i["w"], stream=stream)
+    got["grad_out"], got["grad_w"] = rows.combine_backward(i["gy"], i["out"], i["w"], stream=stream)
+    got["loss"] = loss.forward(i["z"], i["idx"], i["valid"], part, stream=stream)
+    got["grad_z"] = loss.backward(i["z"], i["one"], topk_idx=i["idx"], grad_score=got["grad_w"], valid=i["valid"],
+                                  part_off=part, stream=stream)
+    opt.step(i.pop("grads"), grad_scale=i["one"][:1], stream=stream)
+    return got
+
+
+def made(params, bits):
+    return ExpertRows(T, E, K), BalanceLoss(T, E, K, P), AdamW(params, lr=1e-2, state_bits=bits)
+
+
+def busy(stream, n=40):
+    """Some milliseconds of products on the stream."""
+    with torch.cuda.stream(stream):
+        a = torch.ones((4096, 4096), dtype=torch.bfloat16, **D)
+        for _ in range(n):
+            a = (a @ a) * 2.0 ** -12
+    return a
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_a_stream_of_their_own(bits, as_handle):
+    """Calls with stream= behind a busy stream, their inputs dropped and overwritten-if-reused meanwhile: the same bits
+    as on the current stream."""
+    say(f"handles on a stream, {bits} bits")
+    p, q = tensors(0, *SHAPES), tensors(0, *SHAPES)
+    want = pass_of(*made(p, bits), inputs(), None)
+    want = {k: v.clone() for k, v in want.items()}
+    i, objects = inputs(), made(q, bits)
+    sizes = [(t.shape, t.dtype) for t in i.values() if isinstance(t, torch.Tensor)] + [(g.shape, g.dtype) for g in i["grads"]]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    busy(s)
+    got = pass_of(*objects, i, s.cuda_stream if as_handle else s)
+    del i, objects                   # nothing else holds them while the stream still works
+    for _ in range(3):
+        junk = [torch.empty(shape, dtype=dtype, **D).view(torch.uint8).fill_(0xFF) for shape, dtype in sizes]
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert len(junk) == len(sizes)
+    for k in want:
+        assert torch.equal(want[k], got[k]), k
+    assert all(torch.equal(a, b) for a, b in zip(p, q))
+
+
+def test_buffers_filled_on_a_busy_stream():
+    """A handle made on a busy stream and used on another at once: the call waits for the fills."""
+    say("handles made on a busy stream")
+    p, q = tensors(0, *SHAPES), tensors(0, *SHAPES)
+    want = {k: v.clone() for k, v in pass_of(*made(p, 8), inputs(), None).items()}
+    i = inputs()
+    torch.cuda.synchronize()
+    kept = busy(torch.cuda.current_stream())
+    objects = made(q, 8)
+    s = torch.cuda.Stream()
+    got = pass_of(*objects, i, s)
+    s.synchronize()
+    assert kept.numel() and all(torch.equal(want[k], got[k]) for k in want)
+    assert all(torch.equal(a, b) for a, b in zip(p, q))

@@ -102,3 +102,79 @@ def test_memory_of_another_kind_is_refused(calls):
         opt.step([torch.zeros(4, 5), torch.zeros(3), torch.zeros(300)])
     with pytest.raises(ValueError):
         opt.step([])
+
+
+class Stream:
+    """A stream that notes what waits on it."""
+
+    def __init__(self, number):
+        self.cuda_stream, self.waits = number, []
+
+    def wait_event(self, event):
+        self.waits.append(event)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """The stream that is current where memory is allocated and where the library is called: lists of numbers (0: the
+    current stream outside)."""
+    import contextlib
+    now, where = [0], dict(alloc=[], call=[])
+
+    @contextlib.contextmanager
+    def on(s):
+        now.append(s.cuda_stream)
+        yield
+        now.pop()
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream(now[-1]))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: None)
+    monkeypatch.setattr(eqb, "_stream", lambda s: now[-1] if s is None else s.cuda_stream)
+    for name in ("empty", "empty_like"):
+        real = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, real=real, **k: (where["alloc"].append(now[-1]), real(*a, **k))[1])
+    for name in ("eqb_dispatch_plan", "eqb_dispatch", "eqb_combine", "eqb_combine_backward", "eqb_balance_loss",
+                 "eqb_balance_backward", "eqb_adamw_step"):
+        def call(*a, **k):
+            given = [x for x in list(a) + list(k.values()) if isinstance(x, Stream)]
+            where["call"].append(given[0].cuda_stream if given else now[-1])
+        monkeypatch.setattr(eqb, name, call)
+    return where
+
+
+def handles():
+    from paper_2609_28053_amd import BalanceLoss, ExpertRows
+    T, E, K, H = 6, 8, 2, 4
+    rows, loss = ExpertRows(T, E, K, device="cpu"), BalanceLoss(T, E, K, device="cpu")
+    p = torch.zeros(3)
+    opt = AdamW([p])
+    x, r, w = torch.zeros(T, H), torch.zeros(T * K, H), torch.zeros(T, K)
+    z, idx, one = torch.zeros(T, E), torch.zeros(T, K, dtype=torch.int32), torch.ones(1)
+    return [(rows, lambda s: rows.plan(idx, stream=s)), (rows, lambda s: rows.dispatch(x, stream=s)),
+            (rows, lambda s: rows.combine(r, w, stream=s)), (rows, lambda s: rows.combine_backward(x, r, w, stream=s)),
+            (loss, lambda s: loss.forward(z, idx, stream=s)), (loss, lambda s: loss.backward(z, one, stream=s)),
+            (opt, lambda s: opt.step([p.clone()], stream=s))]
+
+
+def test_a_call_allocates_on_the_stream_that_it_works_on(calls, streams):
+    for handle, call in handles():
+        handle._fill, handle._behind = "filled", {0}
+        for number in (7, 0):
+            streams["alloc"].clear(), streams["call"].clear()
+            call(Stream(number) if number else None)
+            assert streams["call"] == [number] and set(streams["alloc"]) <= {number}
+
+
+def test_the_first_call_on_a_stream_waits_for_the_fills(calls, streams):
+    for handle, call in handles():
+        handle._fill, handle._behind = "filled", {0}
+        s = Stream(7)
+        call(s)
+        assert s.waits == ["filled"]
+        call(s)
+        assert s.waits == ["filled"]
+        here = Stream(0)
+        call(here)
+        assert here.waits == []
