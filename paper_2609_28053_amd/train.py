@@ -195,10 +195,10 @@ class AdamW(_Handle):
             if self._tensors.refresh(*tensors) and self._fill is not None:
                 self._behind.clear()          # memory that no stream is known to use
             self._tensors.set_grads(grads)
-        self.steps += 1
         with self._on(stream, grad_scale, found_inf, *grads):
-            eqb.eqb_adamw_step(self._tensors, self.steps, self.lr if lr is None else lr, *self.betas, self.eps, self.seed,
-                               grad_scale, found_inf)
+            eqb.eqb_adamw_step(self._tensors, self.steps + 1, self.lr if lr is None else lr, *self.betas, self.eps,
+                               self.seed, grad_scale, found_inf)
+        self.steps += 1
 
     def state_dict(self) -> dict:
         """The step's number and the states (the optimizer's own tensors, not copies)."""

@@ -104,6 +104,22 @@ def test_memory_of_another_kind_is_refused(calls):
         opt.step([])
 
 
+def test_a_refused_step_does_not_count(calls, monkeypatch):
+    params, _, opt = model()
+    opt.step(grads_of(params))
+    taken = eqb.eqb_adamw_step
+
+    def refuse(*a, **k):
+        raise eqb.EqbError("eqb_adamw_step", eqb.EQB_ERR_INVALID_ARG)
+
+    monkeypatch.setattr(eqb, "eqb_adamw_step", refuse)
+    with pytest.raises(eqb.EqbError):
+        opt.step(grads_of(params), lr=float("nan"))
+    monkeypatch.setattr(eqb, "eqb_adamw_step", taken)
+    opt.step(grads_of(params))
+    assert [c["step"] for c in calls] == [1, 2] and opt.steps == 2
+
+
 class Stream:
     """A stream that notes what waits on it."""
 
