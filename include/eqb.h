@@ -456,9 +456,17 @@ eqb_status eqb_combine_backward(const void* grad_y, const void* expert_rows, con
  *   numel = 0 is allowed (and its pointers may be null).
  * step >= 1: the number of this step.  grad_scale (nullable, device binary32):
  * a factor on every gradient (clipping, unscaling).  found_inf (nullable, device
- * binary32): where it is not 0 the call changes nothing.
+ * binary32): where it is not 0 the call changes nothing.  The number of the next
+ * step then stays the same, which the host does not know without waiting:
+ * eqb_adamw_step_counted keeps it on the device, also for steps that are captured
+ * in a graph and replayed.  counter: EQB_ADAMW_COUNTER_BYTES of device memory,
+ * 8-byte aligned; its first 8 bytes are the steps taken so far (int64: zeroed once,
+ * or set to go on from a saved state), the rest is scratch.  A call that is not
+ * skipped adds one and is the step of that number; a skipped one changes nothing
+ * there either.  Its constants are computed on the device, in binary64 as well.
  */
 #define EQB_ADAMW_BLOCK      256
+#define EQB_ADAMW_COUNTER_BYTES 64
 typedef struct eqb_adamw_tensor {
   float* param;
   const void* grad;
@@ -473,6 +481,9 @@ typedef struct eqb_adamw_tensor {
 eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
                           int64_t step, double lr, double beta1, double beta2, double eps, uint64_t seed,
                           const float* grad_scale, const float* found_inf, void* stream);
+eqb_status eqb_adamw_step_counted(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                                  void* counter, double lr, double beta1, double beta2, double eps, uint64_t seed,
+                                  const float* grad_scale, const float* found_inf, void* stream);
 
 /*
  * Test control (host only, no HIP call): caps the number of blocks of the

@@ -16,7 +16,7 @@ constexpr int kAdamwThreads = 256, kAdamwWaves = kAdamwThreads / 64;
 struct AdamwScales {
   float* exp_avg;
   float* exp_avg_sq;
-  uint32_t key;           // of the random bits
+  uint32_t key;           // of the random bits; with a counter the tensor's place
 };
 struct AdamwCopy {
   uint16_t* copy;
@@ -76,8 +76,11 @@ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
 }
 
 // The key of a tensor's random bits at a step: seed, step and place mixed to 32 bits.
-static uint32_t adamw_key(uint64_t seed, int64_t step, int32_t i) {
-  uint64_t k = seed + (uint64_t)step * 0x9E3779B97F4A7C15ull + (uint64_t)i * 0xD1B54A32D192ED03ull;
+__host__ __device__ inline uint64_t adamw_base(uint64_t seed, int64_t step) {
+  return seed + (uint64_t)step * 0x9E3779B97F4A7C15ull;
+}
+__host__ __device__ inline uint32_t adamw_key(uint64_t base, uint32_t i) {
+  uint64_t k = base + (uint64_t)i * 0xD1B54A32D192ED03ull;
   k = (k ^ (k >> 32)) * 0xBF58476D1CE4E5B9ull;
   k = (k ^ (k >> 29)) * 0x94D049BB133111EBull;
   return (uint32_t)(k ^ (k >> 32));
@@ -89,6 +92,18 @@ constexpr int64_t kAdamwMostBlocks = 1 << 23;
 // Maximum of values from 0 on over the wave (their patterns order like them).
 __device__ __forceinline__ float wave_max(float x) {
   return __uint_as_float(group_fold<64>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+}
+
+// One more step, unless found_inf skips it, and what it takes from its number.  The blocks of
+// the step itself run behind this and only read it.
+__global__ void adamw_count_kernel(AdamwCounter* c, const float* __restrict__ found_inf, double lr, double beta1,
+                                   double beta2, uint64_t seed) {
+  if (threadIdx.x != 0 || (found_inf && *found_inf != 0.0f)) return;
+  const int64_t step = c->steps + 1;
+  c->steps = step;
+  c->base = adamw_base(seed, step);
+  c->inv_root = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
+  c->rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
 }
 
 template <bool kStream, class T>
@@ -121,6 +136,7 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(const AdamwBatch<k
   }
   const AdamwSlot<k8, kCopy>& t = batch.t[lo];
   const float scale = c.grad_scale ? *c.grad_scale : 1.0f;
+  const float inv_root = c.counter ? c.counter->inv_root : c.inv_root, rate = c.counter ? c.counter->rate : c.rate;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // at most 2^33 elements: block numbers have 25 bits
   const int qb = (int)(blockIdx.x - t.first_block) * kAdamwWaves + wave;
@@ -185,8 +201,8 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(const AdamwBatch<k
     m[i] = m[i] * c.beta1 + gi * c.rest1;
     v[i] = v[i] * c.beta2 + (gi * c.rest2) * gi;
     r[i] = sqrtf(v[i]);
-    const float d = r[i] * c.inv_root + c.eps;
-    w[i] = w[i] * t.keep - (m[i] / d) * c.rate;
+    const float d = r[i] * inv_root + c.eps;
+    w[i] = w[i] * t.keep - (m[i] / d) * rate;
   }
   if constexpr (k8) {
     // lanes past the tensor's end hold zeros
@@ -197,7 +213,8 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(const AdamwBatch<k
     const float nv = tv < 0x1p-100f ? 0.0f : tv * (float)(1.0 / 448.0);
     const float im = nm > 0.0f ? 1.0f / nm : 0.0f, iv = nv > 0.0f ? 1.0f / nv : 0.0f;
     // a block of 256 elements does not cross a multiple of 2^32
-    const uint32_t high = (uint32_t)((uint64_t)base >> 32) * 0x9E3779B1u, low = (uint32_t)(uint64_t)base + q.key;
+    const uint32_t key = c.counter ? adamw_key(c.counter->base, q.key) : q.key;
+    const uint32_t high = (uint32_t)((uint64_t)base >> 32) * 0x9E3779B1u, low = (uint32_t)(uint64_t)base + key;
     uint32_t bm[4], bv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -297,7 +314,7 @@ static eqb_status launch_adamw_as(const eqb_adamw_tensor* tensors, int n, const 
       AdamwScales& q = o;
       q.exp_avg = t.exp_avg_scale;
       q.exp_avg_sq = t.exp_avg_sq_scale;
-      q.key = adamw_key(seed, step, i);
+      q.key = c.counter ? (uint32_t)i : adamw_key(adamw_base(seed, step), (uint32_t)i);
     }
     if constexpr (kCopy) o.copy = t.copy;
     blocks += more;
@@ -305,8 +322,14 @@ static eqb_status launch_adamw_as(const eqb_adamw_tensor* tensors, int n, const 
   return launch();
 }
 
-eqb_status launch_adamw(const eqb_adamw_tensor* tensors, int n, const AdamwScalars& c, double lr, uint64_t seed,
-                        int64_t step, bool eight, bool grad_bf16, bool copies, hipStream_t s) {
+eqb_status launch_adamw(const eqb_adamw_tensor* tensors, int n, const AdamwScalars& c, double lr, double beta1,
+                        double beta2, uint64_t seed, int64_t step, AdamwCounter* counter, bool eight, bool grad_bf16,
+                        bool copies, hipStream_t s) {
+  if (counter) {
+    adamw_count_kernel<<<1, 64, 0, s>>>(counter, c.found_inf, lr, beta1, beta2, seed);
+    const eqb_status st = launch_status();
+    if (st != EQB_OK) return st;
+  }
   const auto launch = eight ? grad_bf16 ? copies ? launch_adamw_as<true, true, true> : launch_adamw_as<true, true, false>
                                         : copies ? launch_adamw_as<true, false, true> : launch_adamw_as<true, false, false>
                             : grad_bf16 ? copies ? launch_adamw_as<false, true, true> : launch_adamw_as<false, true, false>

@@ -471,9 +471,9 @@ eqb_status eqb_combine_backward(const void* grad_y, const void* expert_rows, con
                   grad_y && slot && weight && grad_weight && ((expert_rows && grad_rows) || rows == 0), stream);
 }
 
-eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
-                          int64_t step, double lr, double beta1, double beta2, double eps, uint64_t seed,
-                          const float* grad_scale, const float* found_inf, void* stream) {
+static eqb_status adamw_call(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                             int64_t step, AdamwCounter* counter, double lr, double beta1, double beta2, double eps,
+                             uint64_t seed, const float* grad_scale, const float* found_inf, void* stream) {
   if (n < 0 || (n > 0 && !tensors) || step < 1) return EQB_ERR_INVALID_ARG;
   if (grad_dtype != EQB_DTYPE_F32 && grad_dtype != EQB_DTYPE_BF16) return EQB_ERR_INVALID_ARG;
   if (state_bits != 32 && state_bits != 8) return EQB_ERR_INVALID_ARG;
@@ -506,7 +506,25 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t gr
   c.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
   c.grad_scale = grad_scale;
   c.found_inf = found_inf;
-  return launch_adamw(tensors, n, c, lr, seed, step, eight, grad_bf16, copies, static_cast<hipStream_t>(stream));
+  c.counter = counter;
+  return launch_adamw(tensors, n, c, lr, beta1, beta2, seed, step, counter, eight, grad_bf16, copies,
+                      static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                          int64_t step, double lr, double beta1, double beta2, double eps, uint64_t seed,
+                          const float* grad_scale, const float* found_inf, void* stream) {
+  return adamw_call(tensors, n, grad_dtype, state_bits, step, nullptr, lr, beta1, beta2, eps, seed, grad_scale,
+                    found_inf, stream);
+}
+
+eqb_status eqb_adamw_step_counted(const eqb_adamw_tensor* tensors, int32_t n, int32_t grad_dtype, int32_t state_bits,
+                                  void* counter, double lr, double beta1, double beta2, double eps, uint64_t seed,
+                                  const float* grad_scale, const float* found_inf, void* stream) {
+  if (!counter) return EQB_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(counter) % 8 != 0) return EQB_ERR_UNSUPPORTED;
+  return adamw_call(tensors, n, grad_dtype, state_bits, 1, static_cast<AdamwCounter*>(counter), lr, beta1, beta2, eps,
+                    seed, grad_scale, found_inf, stream);
 }
 
 eqb_status eqb_set_max_blocks(int32_t max_blocks) {

@@ -190,13 +190,23 @@ eqb_status launch_dispatch(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine_backward(const RowArgs& a, hipStream_t s);
 
+// The number of steps kept on the device, and what the step at hand takes from it.
+struct AdamwCounter {
+  int64_t steps;
+  uint64_t base;          // seed and step: what the tensors' random keys come from
+  float inv_root, rate;
+};
+static_assert(sizeof(AdamwCounter) <= EQB_ADAMW_COUNTER_BYTES, "the counter");
 struct AdamwScalars {
   float beta1, rest1, beta2, rest2, eps, inv_root, rate;
   const float* grad_scale;
   const float* found_inf;
+  const AdamwCounter* counter;       // nullable: then inv_root and rate hold
 };
-eqb_status launch_adamw(const eqb_adamw_tensor* tensors, int n, const AdamwScalars& c, double lr, uint64_t seed,
-                        int64_t step, bool eight, bool grad_bf16, bool copies, hipStream_t s);
+// counter, if not null: the number of steps is there, and step does not matter.
+eqb_status launch_adamw(const eqb_adamw_tensor* tensors, int n, const AdamwScalars& c, double lr, double beta1,
+                        double beta2, uint64_t seed, int64_t step, AdamwCounter* counter, bool eight, bool grad_bf16,
+                        bool copies, hipStream_t s);
 
 // Count slabs per partition in a layer's workspace: enough that about 8
 // slabs share the blocks of a launch, so no counter receives the flush

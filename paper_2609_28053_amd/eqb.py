@@ -39,6 +39,7 @@ EQB_DTYPE_F16 = 2
 EQB_SCORE_SIGMOID = 0
 EQB_SCORE_SOFTMAX = 1
 EQB_ADAMW_BLOCK = 256
+EQB_ADAMW_COUNTER_BYTES = 64
 
 EXPORTS = (
     "eqb_route_topk",
@@ -68,6 +69,7 @@ EXPORTS = (
     "eqb_combine",
     "eqb_combine_backward",
     "eqb_adamw_step",
+    "eqb_adamw_step_counted",
     "eqb_set_max_blocks",
     "eqb_get_max_blocks",
     "eqb_rank",
@@ -112,6 +114,7 @@ def _load():
         "eqb_combine": [P, P, P, i64, i32, i64, i32, i32, P, P],
         "eqb_combine_backward": [P, P, P, P, i64, i32, i64, i32, i32, P, P, P],
         "eqb_adamw_step": [P, i32, i32, i32, i64] + [ctypes.c_double] * 4 + [ctypes.c_uint64, P, P, P],
+        "eqb_adamw_step_counted": [P, i32, i32, i32, P] + [ctypes.c_double] * 4 + [ctypes.c_uint64, P, P, P],
         "eqb_set_max_blocks": [i32],
         "eqb_get_max_blocks": [],
         "eqb_rank": [i64, i32, i32],
@@ -605,13 +608,24 @@ class AdamwTensors:
 
 def eqb_adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.95, eps=1e-8, seed=0, grad_scale=None,
                    found_inf=None, stream=None):
-    """One AdamW step, in place, over all the tensors.  step counts from 1; seed draws the 8-bit states'
-    rounding; grad_scale and found_inf are device scalars (a factor on the gradients; skip the step)."""
+    """One AdamW step, in place, over all the tensors.  step counts from 1 the steps that were taken; seed draws the
+    8-bit states' rounding; grad_scale and found_inf are device scalars (a factor on the gradients; skip the step)."""
     _check("eqb_adamw_step", lib.eqb_adamw_step(
         tensors.table.ctypes.data, tensors.n, tensors.grad_dtype, tensors.state_bits, int(step), float(lr),
         float(beta1), float(beta2), float(eps), int(seed) & (2**64 - 1),
         _ptr(grad_scale, torch.float32, 1, "grad_scale"), _ptr(found_inf, torch.float32, 1, "found_inf"),
         _stream(stream)))
+
+
+def eqb_adamw_step_counted(tensors: AdamwTensors, counter, lr, beta1=0.9, beta2=0.95, eps=1e-8, seed=0, grad_scale=None,
+                           found_inf=None, stream=None):
+    """The same with the number of steps taken on the device: counter [8] int64, its first element the steps so far.
+    A step that found_inf skips does not count."""
+    _check("eqb_adamw_step_counted", lib.eqb_adamw_step_counted(
+        tensors.table.ctypes.data, tensors.n, tensors.grad_dtype, tensors.state_bits,
+        _ptr(counter, torch.int64, EQB_ADAMW_COUNTER_BYTES // 8, "counter"), float(lr), float(beta1), float(beta2),
+        float(eps), int(seed) & (2**64 - 1), _ptr(grad_scale, torch.float32, 1, "grad_scale"),
+        _ptr(found_inf, torch.float32, 1, "found_inf"), _stream(stream)))
 
 
 def eqb_set_max_blocks(max_blocks: int) -> None:

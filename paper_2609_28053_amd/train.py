@@ -159,13 +159,17 @@ class AdamW(_Handle):
     copies: BF16 tensors that receive the new parameters.  weight_decay: one
     value, or one per parameter.  Every step takes the memory that parameters,
     copies and states have then, and lr, betas, eps, weight_decay and seed as
-    they are then."""
+    they are then.  device_steps: the number of steps taken is kept on the
+    device from the start, as steps that are captured in a graph need; else it
+    moves there with the first found_inf, which may skip steps without the host
+    knowing.  Reading ``steps`` then waits for the device."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
-                 seed=0):
+                 seed=0, device_steps=False):
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits is 8 or 32, not {state_bits}")
-        self.params, self.lr, self.betas, self.eps, self.seed, self.steps = list(params), lr, betas, eps, seed, 0
+        self.params, self.lr, self.betas, self.eps, self.seed = list(params), lr, betas, eps, seed
+        self._counter, self.steps = None, 0
         self.weight_decay, self.copies, self.state_bits = weight_decay, copies, state_bits
         if state_bits == 8:
             new = lambda: [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)  # noqa: E731
@@ -178,15 +182,35 @@ class AdamW(_Handle):
             self.exp_avg_scale = self.exp_avg_sq_scale = None
         self.exp_avg, self.exp_avg_sq = new(), new()
         self._tensors = None
+        if device_steps:
+            self._count_on_device()
         self._filled(self.params[0].device if self.params else "cpu")
 
     def _buffers(self):
         return [t for ts in (self.params, self.copies, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
-                             self.exp_avg_sq_scale) for t in ts or ()]
+                             self.exp_avg_sq_scale, None if self._counter is None else [self._counter]) for t in ts or ()]
+
+    @property
+    def steps(self) -> int:
+        """The steps taken: those that found_inf skipped are none."""
+        return self._steps if self._counter is None else int(self._counter[0])
+
+    @steps.setter
+    def steps(self, n):
+        if self._counter is None:
+            self._steps = int(n)
+        else:
+            self._counter[0].fill_(int(n))
+
+    def _count_on_device(self):
+        counter = torch.zeros(eqb.EQB_ADAMW_COUNTER_BYTES // 8, dtype=torch.int64,
+                              device=self.params[0].device if self.params else "cpu")
+        counter[0].fill_(self._steps)
+        self._counter = counter
 
     def step(self, grads, lr=None, grad_scale=None, found_inf=None, stream=None):
-        """One step with these gradients, one per parameter, all binary32 or all BF16.  A step that found_inf
-        skips counts in steps as well: its value is on the device, and nothing waits for it."""
+        """One step with these gradients, one per parameter, all binary32 or all BF16.  Where the device scalar
+        found_inf is not 0 nothing changes, the number of steps included."""
         tensors = (self.params, self.exp_avg, self.exp_avg_sq, self.copies, self.exp_avg_scale, self.exp_avg_sq_scale,
                    self.weight_decay)
         if self._tensors is None:
@@ -196,12 +220,20 @@ class AdamW(_Handle):
                 self._behind.clear()          # memory that no stream is known to use
             self._tensors.set_grads(grads)
         with self._on(stream, grad_scale, found_inf, *grads):
-            eqb.eqb_adamw_step(self._tensors, self.steps + 1, self.lr if lr is None else lr, *self.betas, self.eps,
-                               self.seed, grad_scale, found_inf)
-        self.steps += 1
+            if self._counter is None and torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a captured step needs AdamW(device_steps=True): replays would repeat one step's number")
+            if self._counter is None and found_inf is not None:
+                self._count_on_device()
+                self._behind.clear()
+            numbers = (self.lr if lr is None else lr, *self.betas, self.eps, self.seed, grad_scale, found_inf)
+            if self._counter is None:
+                eqb.eqb_adamw_step(self._tensors, self._steps + 1, *numbers)
+                self._steps += 1
+            else:
+                eqb.eqb_adamw_step_counted(self._tensors, self._counter, *numbers)
 
     def state_dict(self) -> dict:
-        """The step's number and the states (the optimizer's own tensors, not copies)."""
+        """The number of steps taken and the states (the optimizer's own tensors, not copies)."""
         return dict(steps=self.steps, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq,
                     exp_avg_scale=self.exp_avg_scale, exp_avg_sq_scale=self.exp_avg_sq_scale)
 

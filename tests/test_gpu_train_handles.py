@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from paper_2609_28053_amd import AdamW, BalanceLoss, ExpertRows
+from paper_2609_28053_amd import AdamW, BalanceLoss, ExpertRows, eqb
+from test_gpu_adamw import HYPER, Model, bits_of, check
 from test_gpu_balance import say
 
 pytestmark = pytest.mark.gpu
@@ -113,3 +114,95 @@ def test_buffers_filled_on_a_busy_stream():
     s.synchronize()
     assert kept.numel() and all(torch.equal(want[k], got[k]) for k in want)
     assert all(torch.equal(a, b) for a, b in zip(p, q))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_counted_step_is_the_step_of_its_number(bits):
+    """Bit for bit the step that a number given by the host makes, at the first steps and far on; a skipped one changes
+    nothing, the counter included."""
+    for taken in (0, 1, 6, 99999):
+        say(f"adamw {bits} bits, counted step {taken + 1}")
+        m = Model(taken, [1, 300, 2000, 255], bits, "bf16", True)
+        counter = torch.zeros(8, dtype=torch.int64, **D)
+        counter[0] = taken
+        one = torch.ones(1, **D)
+        before = [bits_of(t).copy() for t in m.tw + m.tc + m.tm + m.tv]
+        eqb.eqb_adamw_step_counted(m.table(eqb), counter, seed=11, found_inf=one, **HYPER)
+        assert all((a == bits_of(t)).all() for a, t in zip(before, m.tw + m.tc + m.tm + m.tv))
+        assert int(counter[0]) == taken
+        eqb.eqb_adamw_step_counted(m.table(eqb), counter, seed=11, found_inf=one * 0, **HYPER)
+        check(m, taken + 1, 11)
+        assert int(counter[0]) == taken + 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("on_device", [False, True])
+def test_skipped_steps_do_not_count(bits, on_device):
+    """Steps that found_inf skips, first ones and later ones, between steps that are taken: parameters and states end
+    where those of an optimizer that made the taken steps alone end."""
+    say(f"adamw {bits} bits, skipped steps")
+    p, q = tensors(0, *SHAPES), tensors(0, *SHAPES)
+    kw = dict(lr=1e-2, weight_decay=0.1, state_bits=bits, seed=3)
+    alone, skipping = AdamW(p, **kw), AdamW(q, device_steps=on_device, **kw)
+    zero, inf = torch.zeros(1, **D), torch.ones(1, **D)
+    taken = 0
+    for step, skip in enumerate((1, 1, 1, 0, 0, 1, 0)):
+        grads = tensors(50 + step, *SHAPES)
+        skipping.step(grads, found_inf=inf if skip else zero)
+        if not skip:
+            alone.step(grads)
+            taken += 1
+        assert skipping.steps == alone.steps == taken
+    skipping.step(tensors(70, *SHAPES))               # without found_inf: counted as well
+    alone.step(tensors(70, *SHAPES))
+    assert skipping.steps == alone.steps == 4
+    for a, b in zip(p + alone.exp_avg + alone.exp_avg_sq, q + skipping.exp_avg + skipping.exp_avg_sq):
+        assert (bits_of(a) == bits_of(b)).all()
+    third = AdamW([x.clone() for x in q], **kw)
+    third.load_state_dict(skipping.state_dict())
+    assert third.steps == 4
+    third.step(tensors(71, *SHAPES))
+    skipping.step(tensors(71, *SHAPES))
+    assert all(torch.equal(a, b) for a, b in zip(third.params, q))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_in_a_graph(bits):
+    """A captured step, replayed with eager work between the replays and one of them skipped: each replay is the next
+    step.  Without device_steps the capture is refused."""
+    say(f"adamw {bits} bits, steps in a graph")
+    p, q = tensors(0, *SHAPES), tensors(0, *SHAPES)
+    kw = dict(lr=1e-2, weight_decay=0.1, state_bits=bits, seed=3)
+    eager, held = AdamW(p, **kw), AdamW(q, device_steps=True, **kw)
+    grads, found = [torch.zeros(s, **D) for s in SHAPES], torch.zeros(1, **D)
+    for g, x in zip(grads, tensors(50, *SHAPES)):
+        g.copy_(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        held.step(grads, found_inf=found)
+    s.synchronize()
+    eager.step(grads)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        held.step(grads, found_inf=found)
+    for replay in range(5):
+        for g, x in zip(grads, tensors(60 + replay, *SHAPES)):
+            g.copy_(x)
+        found.fill_(float(replay == 2))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        if replay != 2:
+            eager.step(grads)
+        assert all(torch.equal(a, b) for a, b in zip(p, q)), replay
+        assert held.steps == eager.steps
+    other = AdamW(p, **kw)
+    other.step(grads)
+    torch.cuda.synchronize()
+    refused = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="device_steps"):
+        with torch.cuda.graph(refused, stream=s):
+            grads[0].add_(0.0)
+            other.step(grads)
+    torch.cuda.synchronize()

@@ -24,7 +24,11 @@ def calls(monkeypatch):
         seen.append(dict({n: tensors.table[n].tolist() for n in tensors.table.dtype.names}, step=number, lr=lr))
 
     monkeypatch.setattr(eqb, "_ptr", ptr)
+    def counted(tensors, counter, *a, **k):
+        step(tensors, counter, *a, **k)
+
     monkeypatch.setattr(eqb, "eqb_adamw_step", step)
+    monkeypatch.setattr(eqb, "eqb_adamw_step_counted", counted)
     return seen
 
 
@@ -118,6 +122,23 @@ def test_a_refused_step_does_not_count(calls, monkeypatch):
     monkeypatch.setattr(eqb, "eqb_adamw_step", taken)
     opt.step(grads_of(params))
     assert [c["step"] for c in calls] == [1, 2] and opt.steps == 2
+
+
+def test_steps_that_may_be_skipped_are_counted_on_the_device(calls):
+    """From the first found_inf on the call gets the counter, which begins with the steps taken by then."""
+    params, _, opt = model()
+    opt._behind = set()
+    opt.step(grads_of(params))
+    opt.step(grads_of(params), found_inf=torch.zeros(1))
+    opt.step(grads_of(params))
+    assert calls[0]["step"] == 1
+    assert all(c["step"] is opt._counter and c["step"].shape == (8,) for c in calls[1:])
+    assert opt._counter.tolist() == [1] + [0] * 7 and opt.steps == 1          # the recorder does not count
+    opt.load_state_dict(dict(opt.state_dict(), steps=40))
+    assert opt.steps == 40 and opt._counter[0] == 40
+    on = AdamW(params, device_steps=True)
+    on.step(grads_of(params))
+    assert calls[-1]["step"] is on._counter and on.steps == 0
 
 
 class Stream:
