@@ -66,90 +66,118 @@ class _Handle:
 class ExpertRows(_Handle):
     """The experts' rows of T tokens (Eq. 1): the order of the routed pairs,
     dispatch of the tokens' rows, combine of what the experts return, and the
-    gradients of both.  Expert e's rows are offsets[e] .. offsets[e + 1] - 1."""
+    gradients of both.  Expert e's rows are offsets[e] .. offsets[e + 1] - 1.
+
+    A plan writes new ``offsets`` and ``slot``; the calls take the newest
+    ``slot`` unless they are given one, so that with several batches in flight
+    (gradient accumulation) each keeps its own."""
 
     def __init__(self, T: int, E: int, K: int, device="cuda"):
         self.T, self.E, self.K = T, E, K
-        i32 = dict(dtype=torch.int32, device=torch.device(device))
-        self.offsets = torch.empty(E + 1, **i32)
-        self.slot = torch.empty((T, K), **i32)
-        self.workspace = torch.empty(eqb.eqb_dispatch_workspace_size(T, K, E), dtype=torch.uint8, device=i32["device"])
+        self.offsets = self.slot = None
+        self.workspace = torch.empty(eqb.eqb_dispatch_workspace_size(T, K, E), dtype=torch.uint8,
+                                     device=torch.device(device))
         self._filled(device)
 
     def _buffers(self):
-        return self.offsets, self.slot, self.workspace
+        return (self.workspace,)
+
+    def _slot(self, slot):
+        if slot is None and self.slot is None:
+            raise ValueError("no plan has been made")
+        return self.slot if slot is None else slot
 
     def plan(self, topk_idx, stream=None):
         """Orders the pairs of topk_idx [T,K]; entries outside [0, E) are dropped."""
         with self._on(stream, topk_idx):
-            eqb.eqb_dispatch_plan(topk_idx, self.E, self.offsets, self.slot, self.workspace)
+            i32 = dict(dtype=torch.int32, device=self.workspace.device)
+            offsets, slot = torch.empty(self.E + 1, **i32), torch.empty((self.T, self.K), **i32)
+            eqb.eqb_dispatch_plan(topk_idx, self.E, offsets, slot, self.workspace)
+        self.offsets, self.slot = offsets, slot
         return self
 
-    def dispatch(self, x, rows=None, stream=None):
+    def dispatch(self, x, rows=None, stream=None, slot=None):
         """The tokens' rows x [T,H] in the experts' order [T*K,H] (rows past offsets[E] are not written)."""
-        with self._on(stream, x, rows):
+        slot = self._slot(slot)
+        with self._on(stream, x, rows, slot):
             if rows is None:
                 rows = torch.empty((self.T * self.K, x.shape[1]), dtype=x.dtype, device=x.device)
-            eqb.eqb_dispatch(x, self.slot, rows)
+            eqb.eqb_dispatch(x, slot, rows)
         return rows
 
-    def combine(self, rows, weight=None, y=None, stream=None):
+    def combine(self, rows, weight=None, y=None, stream=None, slot=None):
         """sum_k weight[t, k] rows[slot[t, k]] for every token; without weight, the gradient of dispatch."""
-        with self._on(stream, rows, weight, y):
+        slot = self._slot(slot)
+        with self._on(stream, rows, weight, y, slot):
             if y is None:
                 y = torch.empty((self.T, rows.shape[1]), dtype=rows.dtype, device=rows.device)
-            eqb.eqb_combine(rows, self.slot, weight, y)
+            eqb.eqb_combine(rows, slot, weight, y)
         return y
 
-    def combine_backward(self, grad_y, rows, weight, grad_rows=None, grad_weight=None, stream=None):
+    def combine_backward(self, grad_y, rows, weight, grad_rows=None, grad_weight=None, stream=None, slot=None):
         """Gradients of combine with respect to the rows and to the weights (the router backward's grad_score)."""
-        with self._on(stream, grad_y, rows, weight, grad_rows, grad_weight):
+        slot = self._slot(slot)
+        with self._on(stream, grad_y, rows, weight, grad_rows, grad_weight, slot):
             if grad_rows is None:
                 grad_rows = torch.empty_like(rows)
             if grad_weight is None:
                 grad_weight = torch.empty_like(weight)
-            eqb.eqb_combine_backward(grad_y, rows, self.slot, weight, grad_rows, grad_weight)
+            eqb.eqb_combine_backward(grad_y, rows, slot, weight, grad_rows, grad_weight)
         return grad_rows, grad_weight
 
 
 class BalanceLoss(_Handle):
     """The auxiliary balance loss of P groups over T tokens, its loads, and its
     gradient with the router backward.  score: "sigmoid" (normalised) or
-    "softmax"."""
+    "softmax".
+
+    Every forward writes new ``load``, ``tokens``, ``prob`` and ``loss``, and
+    leaves in ``saved`` what its gradient takes of them.  backward takes the
+    newest unless it is given one: with several batches in flight (gradient
+    accumulation) each keeps its own."""
 
     def __init__(self, T: int, E: int, K: int, P: int = 1, alpha: float = 1e-2, score: str = "sigmoid", device="cuda"):
         self.T, self.E, self.K, self.P, self.alpha = T, E, K, P, alpha
         self.score = {"sigmoid": eqb.EQB_SCORE_SIGMOID, "softmax": eqb.EQB_SCORE_SOFTMAX}[score]
         dev = torch.device(device)
-        self._counts = torch.empty((P, E), dtype=torch.int32, device=dev)
-        self.load = self._counts
-        self.tokens = torch.empty(P, dtype=torch.int32, device=dev)
-        self.prob = torch.empty((P, E), dtype=torch.float32, device=dev)
-        self.loss = torch.empty(P, dtype=torch.float32, device=dev)
+        self.load = self.tokens = self.prob = self.loss = self.saved = None
         self.workspace = torch.zeros(eqb.eqb_balance_workspace_size(E, P), dtype=torch.uint8, device=dev)
         self._filled(dev)
 
     def _buffers(self):
-        return self._counts, self.tokens, self.prob, self.loss, self.workspace
+        return (self.workspace,)
 
     def forward(self, z, topk_idx=None, valid=None, part_off=None, load=None, stream=None):
-        """The groups' losses [P] (self.loss); counts topk_idx, or takes the routing's loads."""
+        """The groups' losses [P] (self.loss); counts topk_idx, or takes a copy of the routing's loads (their buffer may
+        be the next routing's before the gradient is computed)."""
         if (topk_idx is None) == (load is None):
             raise ValueError("give topk_idx to count, or the loads that the routing counted")
-        self.load = self._counts if load is None else load
         with self._on(stream, z, topk_idx, valid, load):
-            eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, self.load, self.tokens, self.prob, self.loss,
-                                 self.workspace, valid, part_off, self.score)
-        return self.loss
+            new = dict(device=self.workspace.device)
+            if load is None:
+                load = torch.empty((self.P, self.E), dtype=torch.int32, **new)
+            else:
+                eqb._ptr(load, torch.int32, self.P * self.E, "load")
+                load = load.clone()
+            tokens = torch.empty(self.P, dtype=torch.int32, **new)
+            prob = torch.empty((self.P, self.E), dtype=torch.float32, **new)
+            loss = torch.empty(self.P, dtype=torch.float32, **new)
+            eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, load, tokens, prob, loss, self.workspace, valid, part_off,
+                                 self.score)
+        self.load, self.tokens, self.prob, self.loss, self.saved = load, tokens, prob, loss, (load, tokens)
+        return loss
 
     def backward(self, z, grad_loss, grad_z=None, topk_idx=None, grad_score=None, inj=None, valid=None,
-                 part_off=None, stream=None):
+                 part_off=None, stream=None, saved=None):
         """The gradient with respect to z; with topk_idx and grad_score (and inj), the whole router's."""
-        with self._on(stream, z, grad_loss, grad_z, topk_idx, grad_score, inj, valid, self.load):
+        if saved is None and self.saved is None:
+            raise ValueError("no forward has been made")
+        load, tokens = self.saved if saved is None else saved
+        with self._on(stream, z, grad_loss, grad_z, topk_idx, grad_score, inj, valid, load, tokens):
             if grad_z is None:
                 grad_z = torch.empty((self.T, self.E), dtype=torch.float32, device=z.device)
-            eqb.eqb_balance_backward(z, self.load, self.tokens, self.K, self.alpha, grad_loss, grad_z, topk_idx, grad_score,
-                                     inj, valid, part_off, self.score)
+            eqb.eqb_balance_backward(z, load, tokens, self.K, self.alpha, grad_loss, grad_z, topk_idx, grad_score, inj, valid,
+                                     part_off, self.score)
         return grad_z
 
 

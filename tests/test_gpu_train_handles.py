@@ -206,3 +206,33 @@ def test_steps_in_a_graph(bits):
             grads[0].add_(0.0)
             other.step(grads)
     torch.cuda.synchronize()
+
+
+def test_batches_in_flight():
+    """Two forward passes before the first backward pass, the routing's loads in one buffer that both write: the
+    gradients are those of handles that serve one batch each."""
+    say("two batches in flight")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    batches = []
+    for _ in range(2):
+        z = torch.randn((T, E), generator=g, **D).to(torch.bfloat16)
+        idx = (z.float() + torch.randn(E, generator=g, **D)).topk(K, dim=1).indices.to(torch.int32)
+        batches.append((z.view(torch.int16), idx, torch.randn((T, H), generator=g, **D), torch.randn((T * K, H), generator=g, **D),
+                        torch.rand((T, K), generator=g, **D)))
+    one = torch.ones(1, **D)
+    load_of = lambda idx: torch.bincount(idx.view(-1).long(), minlength=E).to(torch.int32).view(1, E)  # noqa: E731
+    want = []
+    for z, idx, gy, out, w in batches:
+        rows, loss = ExpertRows(T, E, K), BalanceLoss(T, E, K)
+        loss.forward(z, load=load_of(idx))
+        want.append([*rows.plan(idx).combine_backward(gy, out, w), loss.backward(z, one)])
+    rows, loss, load, kept = ExpertRows(T, E, K), BalanceLoss(T, E, K), torch.empty((1, E), dtype=torch.int32, **D), []
+    for z, idx, gy, out, w in batches:
+        load.copy_(load_of(idx))
+        loss.forward(z, load=load)
+        kept.append((rows.plan(idx).slot, loss.saved))
+    load.fill_(0)
+    for (z, idx, gy, out, w), (slot, saved), expected in zip(batches, kept, want):
+        got = [*rows.combine_backward(gy, out, w, slot=slot), loss.backward(z, one, saved=saved)]
+        assert all(torch.equal(a, b) for a, b in zip(got, expected))

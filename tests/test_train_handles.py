@@ -185,6 +185,8 @@ def handles():
     from paper_2609_28053_amd import BalanceLoss, ExpertRows
     T, E, K, H = 6, 8, 2, 4
     rows, loss = ExpertRows(T, E, K, device="cpu"), BalanceLoss(T, E, K, device="cpu")
+    rows.slot = torch.zeros((T, K), dtype=torch.int32)
+    loss.saved = torch.zeros((1, E), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     p = torch.zeros(3)
     opt = AdamW([p])
     x, r, w = torch.zeros(T, H), torch.zeros(T * K, H), torch.zeros(T, K)
@@ -215,3 +217,57 @@ def test_the_first_call_on_a_stream_waits_for_the_fills(calls, streams):
         here = Stream(0)
         call(here)
         assert here.waits == []
+
+
+@pytest.fixture
+def numbers(monkeypatch, calls):
+    """The library's calls as recorders that write their number into what they compute."""
+    seen = []
+
+    def fill(name, *outputs):
+        seen.append(name)
+        for t in outputs:
+            t.fill_(len(seen))
+
+    monkeypatch.setattr(eqb, "eqb_dispatch_plan", lambda idx, E, offsets, slot, ws=None, stream=None: fill("plan", offsets, slot))
+    monkeypatch.setattr(eqb, "eqb_combine", lambda rows, slot, w, y, stream=None: fill(int(slot[0, 0]), y))
+    monkeypatch.setattr(eqb, "eqb_dispatch", lambda x, slot, rows, stream=None: fill(int(slot[0, 0]), rows))
+    monkeypatch.setattr(eqb, "eqb_combine_backward", lambda gy, r, slot, w, gr, gw, stream=None: fill(int(slot[0, 0]), gr, gw))
+    monkeypatch.setattr(eqb, "eqb_balance_loss", lambda z, idx, K, a, load, tokens, prob, loss, *r, **k: fill(
+        "loss", tokens, prob, loss, *([load] if idx is not None else [])))
+    monkeypatch.setattr(eqb, "eqb_balance_backward", lambda z, load, tokens, *r, **k: seen.append(
+        (int(load[0, 0]), int(tokens[0]))))
+    return seen
+
+
+def test_two_batches_in_flight_keep_their_plans(numbers):
+    from paper_2609_28053_amd import ExpertRows
+    rows = ExpertRows(6, 8, 2, device="cpu")
+    idx, x, r, w = torch.zeros((6, 2), dtype=torch.int32), torch.zeros(6, 4), torch.zeros(12, 4), torch.zeros(6, 2)
+    with pytest.raises(ValueError):
+        rows.dispatch(x)
+    first = rows.plan(idx).slot
+    second = rows.plan(idx).slot
+    rows.dispatch(x, slot=first), rows.combine(r, slot=first), rows.combine_backward(x, r, w, slot=first)
+    rows.dispatch(x), rows.combine(r), rows.combine_backward(x, r, w)
+    assert numbers == ["plan", "plan", 1, 1, 1, 2, 2, 2] and second is rows.slot
+
+
+def test_two_batches_in_flight_keep_their_loads(numbers):
+    """Counted loads and given ones, whose buffer the next routing fills again."""
+    from paper_2609_28053_amd import BalanceLoss
+    loss = BalanceLoss(6, 8, 2, device="cpu")
+    z, idx, one = torch.zeros(6, 8), torch.zeros((6, 2), dtype=torch.int32), torch.ones(1)
+    with pytest.raises(ValueError):
+        loss.backward(z, one)
+    a = loss.forward(z, idx)
+    first = loss.saved
+    routed = torch.full((1, 8), 50, dtype=torch.int32)
+    b = loss.forward(z, load=routed)
+    second = loss.saved
+    routed.fill_(60)
+    c = loss.forward(z, load=routed)
+    routed.fill_(70)
+    loss.backward(z, one, saved=first), loss.backward(z, one, saved=second), loss.backward(z, one)
+    assert numbers == ["loss"] * 3 + [(1, 1), (50, 2), (60, 3)]
+    assert (float(a), float(b), float(c)) == (1.0, 2.0, 3.0)
