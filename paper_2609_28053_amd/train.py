@@ -266,15 +266,21 @@ class AdamW(_Handle):
                     exp_avg_scale=self.exp_avg_scale, exp_avg_sq_scale=self.exp_avg_sq_scale)
 
     def load_state_dict(self, state: dict) -> None:
-        """Takes over the values of a state_dict of the same parameters and state_bits."""
-        if (state["exp_avg_scale"] is None) != (self.state_bits == 32):
-            raise ValueError(f"the state is not one of {self.state_bits} bits")
-        for name in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
+        """Takes over the values of a state_dict of the same parameters and state_bits; one that does not fit changes
+        nothing."""
+        names = ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")
+        steps = int(state["steps"])
+        for name in names:
             mine, theirs = getattr(self, name), state[name]
+            if (mine is None) != (theirs is None):
+                raise ValueError(f"the state is not one of {self.state_bits} bits")
             if mine is None:
                 continue
-            if [t.shape for t in mine] != [t.shape for t in theirs]:
-                raise ValueError(f"{name} has other shapes")
-            for a, b in zip(mine, theirs):
+            fits = [t.shape == u.shape and (t.dtype is u.dtype or (t.dtype is torch.float32 and u.is_floating_point()))
+                    for t, u in zip(mine, theirs)]
+            if len(mine) != len(theirs) or not all(fits):
+                raise ValueError(f"{name} has other shapes or types")
+        for name in names:
+            for a, b in zip(getattr(self, name) or (), state[name] or ()):
                 a.copy_(b)
-        self.steps = int(state["steps"])
+        self.steps = steps

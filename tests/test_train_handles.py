@@ -141,6 +141,30 @@ def test_steps_that_may_be_skipped_are_counted_on_the_device(calls):
     assert calls[-1]["step"] is on._counter and on.steps == 0
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_state_that_does_not_fit_changes_nothing(bits):
+    params, _, opt = model(bits)
+    _, _, other = model(bits)
+    for t in other.exp_avg + other.exp_avg_sq:
+        t.view(torch.uint8).fill_(1)
+    before = [t.clone() for t in opt.exp_avg + opt.exp_avg_sq]
+    good = dict(other.state_dict(), steps=5)
+    short = list(good["exp_avg_sq"])
+    short[2] = short[2][:7]
+    whole = [t.to(torch.float32).to(torch.int32) for t in good["exp_avg_sq"]]
+    scale = dict(exp_avg_sq_scale=None if bits == 8 else good["exp_avg"])
+    for bad in (dict(exp_avg_sq=short), dict(exp_avg_sq=whole), dict(exp_avg_sq=good["exp_avg_sq"][:2]), scale):
+        with pytest.raises(ValueError):
+            opt.load_state_dict(dict(good, **bad))
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(opt.exp_avg + opt.exp_avg_sq, before))
+        assert opt.steps == 0
+    with pytest.raises(KeyError):
+        opt.load_state_dict({k: v for k, v in good.items() if k != "steps"})
+    assert opt.steps == 0 and not opt.exp_avg[0].view(torch.uint8).any()
+    opt.load_state_dict(good)
+    assert opt.steps == 5 and all((t.view(torch.uint8) == 1).all() for t in opt.exp_avg + opt.exp_avg_sq)
+
+
 class Stream:
     """A stream that notes what waits on it."""
 
