@@ -259,6 +259,8 @@ class AdamW(_Handle):
                 self._steps += 1
             else:
                 eqb.eqb_adamw_step_counted(self._tensors, self._counter, *numbers)
+        # autograd sees that what it kept of them for a backward pass has changed
+        torch.autograd.graph.increment_version([*self.params, *(self.copies or ())])
 
     def state_dict(self) -> dict:
         """The number of steps taken and the states (the optimizer's own tensors, not copies)."""

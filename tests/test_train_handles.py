@@ -165,6 +165,20 @@ def test_a_state_that_does_not_fit_changes_nothing(bits):
     assert opt.steps == 5 and all((t.view(torch.uint8) == 1).all() for t in opt.exp_avg + opt.exp_avg_sq)
 
 
+def test_autograd_notices_a_step_between_forward_and_backward(calls):
+    """A parameter or copy that autograd kept for a backward pass and that a step has overwritten is refused there, as
+    with any change in place."""
+    params, copies, opt = model()
+    x = torch.randn(3, requires_grad=True)
+    for weight in (params[1], copies[1]):
+        y = (x * weight).sum()
+        y.backward()
+        y = (x * weight).sum()
+        opt.step(grads_of(params))
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+
 class Stream:
     """A stream that notes what waits on it."""
 
