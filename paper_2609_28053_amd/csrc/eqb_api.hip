@@ -65,6 +65,9 @@ eqb_status make_table(const int64_t* part_off, int32_t P, int64_t T, PartTable* 
 constexpr int64_t kAdamwMostElements = (int64_t)1 << 33;     // of one tensor: its blocks fit a launch
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+// Whether all pointers have the alignment of their 32-bit elements.
+template <class... P>
+bool aligned4(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0; }
 
 }  // namespace
 }  // namespace eqb
@@ -368,6 +371,7 @@ eqb_status eqb_balance_loss(const uint16_t* z, const int32_t* topk_idx, const ui
   if (st != EQB_OK) return st;
   if (!load || !tokens || !prob || !loss || !workspace || (T > 0 && !z)) return EQB_ERR_INVALID_ARG;
   if (!aligned16(z) || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return EQB_ERR_UNSUPPORTED;
+  if (!aligned4(topk_idx, load, tokens, prob, loss)) return EQB_ERR_UNSUPPORTED;
   BalanceWorkspace ws;
   if (workspace_bytes < balance_workspace(workspace, E, a.pt.P, &ws)) return EQB_ERR_INVALID_ARG;
   a.z = z;
@@ -401,6 +405,7 @@ eqb_status eqb_balance_backward(const uint16_t* z, const int32_t* load, const in
   if (T == 0) return EQB_OK;
   if (!z || !load || !tokens || !grad_loss || !grad_z) return EQB_ERR_INVALID_ARG;
   if (!aligned16(z) || !aligned16(grad_z)) return EQB_ERR_UNSUPPORTED;
+  if (!aligned4(load, tokens, grad_loss, topk_idx, grad_score, inj)) return EQB_ERR_UNSUPPORTED;
   a.z = z;
   a.idx = topk_idx;
   a.valid = valid;
@@ -433,7 +438,7 @@ eqb_status eqb_dispatch_plan(const int32_t* topk_idx, int64_t T, int32_t K, int3
   if (!offsets || (T > 0 && (!topk_idx || !slot))) return EQB_ERR_INVALID_ARG;
   const size_t need = eqb_dispatch_workspace_size(T, K, E);
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQB_ERR_INVALID_ARG;
-  if (!aligned16(workspace)) return EQB_ERR_UNSUPPORTED;
+  if (!aligned16(workspace) || !aligned4(topk_idx, offsets, slot)) return EQB_ERR_UNSUPPORTED;
   return launch_dispatch_plan(topk_idx, T * K, E, offsets, slot, static_cast<int32_t*>(workspace),
                               static_cast<hipStream_t>(stream));
 }
@@ -448,6 +453,8 @@ static eqb_status row_call(eqb_status (*launch)(const RowArgs&, hipStream_t), co
   if ((reinterpret_cast<uintptr_t>(a.tokens) | reinterpret_cast<uintptr_t>(a.experts) |
        reinterpret_cast<uintptr_t>(a.out)) & mask)
     return EQB_ERR_UNSUPPORTED;
+  // slots and weights are scalar loads, which drop an address's last two bits
+  if (!aligned4(a.slot, a.weight, a.grad_weight)) return EQB_ERR_UNSUPPORTED;
   return launch(a, static_cast<hipStream_t>(stream));
 }
 
@@ -479,6 +486,7 @@ static eqb_status adamw_call(const eqb_adamw_tensor* tensors, int32_t n, int32_t
   if (state_bits != 32 && state_bits != 8) return EQB_ERR_INVALID_ARG;
   if (!(lr == lr) || !(eps >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
     return EQB_ERR_INVALID_ARG;
+  if (!aligned4(grad_scale, found_inf)) return EQB_ERR_UNSUPPORTED;
   const bool eight = state_bits == 8, grad_bf16 = grad_dtype == EQB_DTYPE_BF16;
   bool first = true, copies = false;
   for (int32_t i = 0; i < n; ++i) {
