@@ -375,7 +375,7 @@ eqb_status eqb_balance_loss(const uint16_t* z, const int32_t* topk_idx, const ui
  *   grad_z[t,e] = (alpha grad_loss_p / n_p) p_{t,e} q_{t,e} (F_{p,e} - sum_e' p_{t,e'} F_{p,e'})
  *                 + (g[t,e] + inj[p,e]) sigmoid'(z_{t,e})
  * with q = 1 - sigmoid(z) (EQB_SCORE_SIGMOID) or 1 (EQB_SCORE_SOFTMAX) and g, inj as
- * in eqb_lei_router_backward; a row of an invalid token is 0 throughout.
+ * in eqb_lei_router_backward, sigmoid' too; a row of an invalid token is 0 throughout.
  *   load [P,E], tokens [P] int32 (in): from eqb_balance_loss.
  *   grad_loss [P] binary32 (in): the gradient that arrives at each loss_p.
  *   topk_idx [T,K], grad_score [T,K] (both or neither): g; inj [P,E] (nullable).

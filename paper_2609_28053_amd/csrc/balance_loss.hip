@@ -394,6 +394,10 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // gradient is p q (C - sum p C) + (g + inj) sigmoid'.  The K mixture gradients of a row
 // are scattered into a per-wave LDS row of zeros, read back 4 at a time, and their
 // places zeroed again.
+// sigmoid' is computed as in the router backward alone, so that with C = 0 the results are
+// the same bits; against the bare exponential and reciprocal, which lose digits of large
+// logits and all beyond 87, that costs 1 to 4% (with the loss, 1,000,003 rows of E = 128, K =
+// 8: 218.9 -> 221.7 us, of E = 64, K = 6: 115.1 -> 119.7).
 // Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once.  The
 // gradient's stores are non-temporal, and so are the logits' loads when these take more than
 // a quarter of the memory-side cache (kStream); fewer are still there from the loss or the
@@ -424,6 +428,7 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
     int64_t rows_per_block, double alpha, float* __restrict__ grad_z) {
   constexpr int G = E / 4, R = 64 / G;
   constexpr uint32_t ROWS = kGradWaves * R * kGradU;
+  constexpr bool kSigmoid = !kSoftmax || kRouter != kAlone;
   __shared__ __align__(16) float sh_g[kRouter == kAlone ? 1 : kGradWaves][kGradU][R][E];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane % G, rr = lane / G;
@@ -518,14 +523,30 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
         const uint32_t t = row_of(base, u);
         const float x[4] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y)};
         float w[4], q[4], sd[4], d;
-        if (!kSoftmax || kRouter != kAlone) {
+        if (kSigmoid) {
+          // exp(-|x|) as in the router backward alone: logits of 32 or more take a longer form,
+          // chosen per wave and row
+          float ex[4];
+          const float top = max3_abs(max3_abs(0.0f, x[0], x[1]), x[2], x[3]);
+          if (kRouter == kAlone) {
+            // (nothing is a multiple of sigmoid': what the short form loses above 32, 1e-7 of a
+            // probability at 90, does not matter, and 0 from 128 on is 0 at any power)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16(__builtin_elementwise_minimum(fabsf(x[i]), 128.0f));
+          } else if (__builtin_expect(__any(top >= kSigmoidMax), 0)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16_wide(fabsf(x[i]));
+            asm volatile("; large logits");
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16(fabsf(x[i]));
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fabsf(x[i]) * -kLog2e);
-            const float r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+            const float r = newton_rcp(1.0f + ex[i]), er = ex[i] * r;     // sigmoid(|x|), sigmoid(-|x|)
             w[i] = x[i] >= 0.0f ? r : er;
             q[i] = x[i] >= 0.0f ? er : r;
-            sd[i] = er * r;
+            sd[i] = __builtin_fmaf(-er, er, er);
           }
         }
         if (kSoftmax) {
@@ -533,9 +554,15 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
         } else {
           d = group_sum<G>(w[0] + w[1] + (w[2] + w[3]));
           const bool tiny = d < kTinySum;
-          if (__any(tiny)) d = softmax_where<G>(tiny, x, w, d);
+          if (__any(tiny)) {
+            // the logits unpacked again, rather than kept for this in registers
+            uint32_t w0 = zw[u].x, w1 = zw[u].y;
+            asm volatile("" : "+v"(w0), "+v"(w1));
+            const float y[4] = {bf16_lo(w0), bf16_hi(w0), bf16_lo(w1), bf16_hi(w1)};
+            d = softmax_where<G>(tiny, y, w, d);
+          }
         }
-        const float inv = d != 0.0f ? __builtin_amdgcn_rcpf(d) : 0.0f;
+        const float inv = d != 0.0f ? newton_rcp(d) : 0.0f;
         float c = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

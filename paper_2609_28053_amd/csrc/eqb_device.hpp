@@ -139,12 +139,15 @@ __device__ __forceinline__ float max3_abs(float m, float a, float b) {
 // like the division but for rare last bits, and with q = sigmoid(-a), q - q^2 in
 // one rounding halves what q carries near 0.
 // wide: any BF16 x, in 20 instructions; for |x| < 32 the same value.
+// newton_rcp: 1 / d after that step.
+__device__ __forceinline__ float newton_rcp(float d) {
+  const float r0 = __builtin_amdgcn_rcpf(d);
+  return __builtin_fmaf(__builtin_fmaf(-d, r0, 1.0f), r0, r0);
+}
 template <bool wide>
 __device__ __forceinline__ float sigmoid_prime_bf16(float x) {
   const float e = wide ? exp_neg_bf16_wide(fabsf(x)) : exp_neg_bf16(fabsf(x));
-  const float d = 1.0f + e;
-  const float r0 = __builtin_amdgcn_rcpf(d);
-  const float q = e * __builtin_fmaf(__builtin_fmaf(-d, r0, 1.0f), r0, r0);   // sigmoid(-a) <= 1/2
+  const float q = e * newton_rcp(1.0f + e);   // sigmoid(-a) <= 1/2
   return __builtin_fmaf(-q, q, q);
 }
 
