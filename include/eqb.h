@@ -358,8 +358,8 @@ eqb_status eqb_layer_noalloc(const uint16_t* z, const float* b, int64_t T, int32
  *     counters zero again, wherever E and P put the rest, so that one workspace of
  *     the largest size serves calls of all sizes.  Two calls whose work may overlap
  *     need two.
- * A row's probabilities and a lane's sum over its rows are binary32, the sums of
- * those binary64 (handed from block to block in binary32); the result does not
+ * A row's probabilities and a lane's sum over up to 128 of its rows are binary32, the
+ * sums of those binary64 (handed from block to block in binary32); the result does not
  * depend on the order in which blocks run.  T = 0 writes zeros (`load` too, with or without topk_idx).
  */
 size_t eqb_balance_workspace_size(int32_t E, int32_t P);     /* host only; 0 for unsupported E or P */

@@ -49,7 +49,9 @@ __device__ __forceinline__ float softmax_terms(const float (&x)[N], float (&w)[N
 // last rows to the next one's first, these were the last to finish: 99,991 rows of E = 128
 // in three groups 19.0 us, in pieces 17.5; 20,000 of E = 256 in 64 groups 13.8 and 9.8.
 // G = E/8 lanes hold a row, 8 experts each.  A lane sums the probabilities of its
-// experts over its rows in binary32; at the end of a piece the block adds its lanes' sums,
+// experts over its rows in binary32, 128 rows at most: then its wave's sums are added to
+// binary64 ones in LDS (one sum over 80,000 equal rows was off by 1.2e-3, so by 1.9e-6; a
+// step costs nothing measurable more).  At the end of a piece the block adds its lanes' sums,
 // the waves' in binary64.  The pieces of a group are handed over (in binary32) through the
 // workspace: the last of a bunch of neighbours to come, by a ticket, adds theirs, and the
 // last of those adds the sums, each in a fixed order in binary64, and writes the group's
@@ -58,6 +60,7 @@ __device__ __forceinline__ float softmax_terms(const float (&x)[N], float (&w)[N
 // the ticket is drawn.
 constexpr int kLossThreads = 768, kLossWaves = kLossThreads / 64;
 constexpr int kLossU = 2;          // rows per lane and step
+constexpr uint32_t kLossSteps = 64;     // steps of a lane's sum in binary32
 
 // The pieces: `rows` rows each, but for a group's last; group p's are first[p] to
 // first[p + 1] - 1, and first is above them all past first[P].
@@ -91,6 +94,7 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
   constexpr int G = E / 8, R = 64 / G;
   constexpr uint32_t ROWS = kLossWaves * R * kLossU;
   __shared__ float sh_sum[kLossWaves][E];
+  __shared__ double sh_long[kLossWaves][E];      // sums of the wave's earlier steps
   // counts in 256/E copies, a lane adding to copy lane % copies: with one, the 64 lanes of
   // a wave queue on the few counters of a small E
   __shared__ int32_t sh_cnt[kNBins / E][E];
@@ -123,6 +127,7 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     __syncthreads();
     float acc[8] = {};
     int n = 0;
+    uint32_t steps = 0;
     // pieces of at most kSegMax rows: 32-bit offsets from their bases
     for (int64_t c0 = s0; c0 < s1; c0 += kSegMax) {
       const int64_t cu = wave_uniform(c0);
@@ -163,6 +168,15 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
         }
       }
       for (uint32_t base = 0; base < rows; base += ROWS) {
+        if (__builtin_expect(++steps > kLossSteps && steps % kLossSteps == 1, 0)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            double& to = sh_long[wave][8 * g + i];
+            const float v = column_sum<G>(acc[i]);
+            if (lane < G) to = steps > 2 * kLossSteps ? to + (double)v : (double)v;
+            acc[i] = 0.0f;
+          }
+        }
         uint4 zw[kLossU];
         bool on[kLossU];
 #pragma unroll
@@ -217,6 +231,8 @@ __global__ __launch_bounds__(kLossThreads, 6) void balance_loss_kernel(
     int64_t count = 0, nv = pt.off[p + 1] - pt.off[p];
     if (tid < E) {
       for (int w = 0; w < kLossWaves; ++w) sum += (double)sh_sum[w][tid];
+      if (steps > kLossSteps)
+        for (int w = 0; w < kLossWaves; ++w) sum += sh_long[w][tid];
       for (int c = 0; c < kNBins / E; ++c) {
         count += sh_cnt[c][tid];
         sh_cnt[c][tid] = 0;

@@ -52,3 +52,51 @@ def test_pieces_joined_in_two_levels(eqb, softmax, cuts, E, mask):  # noqa: F811
     say(f"balance, two levels, E={E} groups={c.P} mask={mask} softmax={softmax}")
     ws = torch.zeros(eqb.eqb_balance_workspace_size(E, c.P), dtype=torch.uint8, device="cuda")
     loss_of(eqb, c, ws, softmax)
+
+
+@pytest.mark.parametrize("E,T", [(256, 48 * 63 - 1), (256, 48 * 64 - 5), (256, 48 * 65), (256, 48 * 128), (256, 48 * 129 + 1),
+                                 (128, 96 * 64), (8, 1536 * 64 + 11), (256, 70001)])
+def test_a_lanes_sums_of_whole_lengths(eqb, E, T):  # noqa: F811
+    """One block over one group, at step counts around the 64 that a lane sums before it adds to its wave's sum."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    z = (torch.randn((T, E), generator=g, device="cuda") * 1.5).to(torch.bfloat16)
+    valid = torch.rand(T, generator=g, device="cuda") < 0.8
+    p = torch.sigmoid(z.double())
+    p = (p / p.sum(1, keepdim=True))[valid].mean(0)
+    ws = torch.zeros(eqb.eqb_balance_workspace_size(E, 1), dtype=torch.uint8, device="cuda")
+    load, tokens = torch.ones((1, E), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    prob, loss = torch.empty((1, E), device="cuda"), torch.empty(1, device="cuda")
+    say(f"balance, one block, E={E} T={T}")
+    eqb.eqb_set_max_blocks(1)
+    try:
+        eqb.eqb_balance_loss(z.view(torch.int16), None, 2, 1.0, load, tokens, prob, loss, ws, valid)
+    finally:
+        eqb.eqb_set_max_blocks(0)
+    eps = (2 * float(z.float().abs().max()) + 24) * 2.0 ** -23
+    assert int(tokens) == int(valid.sum())
+    assert bool(((prob[0].double() - p).abs() <= (eps + 128 * 2.0 ** -24) * p).all())
+
+
+def test_means_of_many_equal_rows(eqb):  # noqa: F811
+    """2,000,000 copies of one row in one block: a lane adds the same number 80,000 times, so that the roundings of one
+    long binary32 sum would all go one way (1e-3 and more); a lane sums 128 rows at most, and the rest is binary64."""
+    E, T = 256, 2000000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    row = torch.randn((1, E), generator=g, device="cuda").to(torch.bfloat16)
+    z = row.expand(T, E).contiguous()
+    p = torch.softmax(row.double(), 1)[0]
+    ws = torch.zeros(eqb.eqb_balance_workspace_size(E, 1), dtype=torch.uint8, device="cuda")
+    load, tokens = torch.ones((1, E), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    prob, loss = torch.empty((1, E), device="cuda"), torch.empty(1, device="cuda")
+    say("balance, equal rows in one block")
+    eqb.eqb_set_max_blocks(1)
+    try:
+        eqb.eqb_balance_loss(z.view(torch.int16), None, 2, 1.0, load, tokens, prob, loss, ws, score=eqb.EQB_SCORE_SOFTMAX)
+    finally:
+        eqb.eqb_set_max_blocks(0)
+    eps = (2 * float(row.float().abs().max()) + 24) * 2.0 ** -23
+    far = ((prob[0].double() - p).abs() / p).max()
+    say(f"relative error {float(far):.1e}")
+    assert float(far) <= eps + 128 * 2.0 ** -24
