@@ -69,13 +69,18 @@ __device__ __forceinline__ f32x4 decode_e4m3x4(uint32_t w) {
   return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
+// 32 bits mixed by shifts and odd multipliers, those that C. Wellons published in 2018 as the
+// least biased of a search (every input bit turns every output bit half of the time).
 __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x7FEB352Du;
   x = (x ^ (x >> 15)) * 0x846CA68Bu;
   return x ^ (x >> 16);
 }
 
-// The key of a tensor's random bits at a step: seed, step and place mixed to 32 bits.
+// The key of a tensor's random bits at a step: seed, step and place mixed to 32 bits.  Steps
+// and places count in multiples that spread evenly over 2^64 (2^64 by the golden ratio, and by
+// the root of x^4 = x + 1, its like for three dimensions), the mixer's multipliers are D.
+// Stafford's (published with Steele, Lea and Flood's splittable generators, 2014).
 __host__ __device__ inline uint64_t adamw_base(uint64_t seed, int64_t step) {
   return seed + (uint64_t)step * 0x9E3779B97F4A7C15ull;
 }
