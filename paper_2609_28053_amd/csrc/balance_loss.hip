@@ -17,9 +17,10 @@ __device__ __forceinline__ int partition_of(const PartTable& pt, int64_t t) {
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
-// Below this sum the sigmoids of a row equal their exponentials to binary32, and may have
-// lost digits to underflow: the row's probabilities are then those of a softmax.
-constexpr float kTinySum = 0x1p-100f;
+// Below this sum the sigmoids of a row equal their exponentials to binary32, and they or
+// their products may have lost digits to underflow: the row's probabilities are then those of
+// a softmax.
+constexpr float kTinySum = 0x1p-60f;
 
 // A row's exponentials exp(x - max) over the group's lanes, whole rows of -inf giving 0, and
 // their sum; where a row does not take part its terms w and sum d stay as they are.
@@ -411,9 +412,10 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // are scattered into a per-wave LDS row of zeros, read back 4 at a time, and their
 // places zeroed again.
 // sigmoid' is computed as in the router backward alone, so that with C = 0 the results are
-// the same bits; against the bare exponential and reciprocal, which lose digits of large
-// logits and all beyond 87, that costs 1 to 4% (with the loss, 1,000,003 rows of E = 128, K =
-// 8: 218.9 -> 221.7 us, of E = 64, K = 6: 115.1 -> 119.7).
+// the same bits, and p q of a sigmoid row is sigmoid' / d.  Against the bare exponential and
+// reciprocal, which lose digits of large logits and all beyond 87, that costs up to 2% (the
+// gradient of 1,000,003 rows of E = 128, K = 8: 160.5 -> 163.6 us, of 131,072 of E = 256 36.0
+// and 36.2; with logits of -inf among them, which do not take the longer form, 36.1 and 36.5).
 // Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once.  The
 // gradient's stores are non-temporal, and so are the logits' loads when these take more than
 // a quarter of the memory-side cache (kStream); fewer are still there from the loss or the
@@ -429,6 +431,17 @@ constexpr int kGradWavesPerSimd = 8;
 constexpr int kGradBlocksPerCu = kGradWavesPerSimd * 256 / kGradThreads;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Whether any of four BF16 values has a magnitude from 32 to 104.  2 |x| - 2 * 32 in 16-bit
+// patterns, the sign shifted out: below 32 it wraps past all others.
+__device__ __forceinline__ bool any_from_32_to_104(uint32_t w0, uint32_t w1) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  constexpr uint16_t k32 = 0x4200, k104 = 0x42D0;
+  const u16x2 two = {2, 2}, low = {(uint16_t)(2 * k32), (uint16_t)(2 * k32)};
+  const u16x2 a = __builtin_bit_cast(u16x2, w0) * two - low, b = __builtin_bit_cast(u16x2, w1) * two - low;
+  const u16x2 m = __builtin_elementwise_min(a, b);
+  return (m.x < m.y ? m.x : m.y) <= 2 * (k104 - k32);
+}
 
 // What goes with the loss's gradient: nothing, the router backward where a lane of a
 // row's group holds at most one of its K pairs, or the router backward with any K (and
@@ -538,35 +551,33 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
       for (int u = 0; u < kGradU; ++u) {
         const uint32_t t = row_of(base, u);
         const float x[4] = {bf16_lo(zw[u].x), bf16_hi(zw[u].x), bf16_lo(zw[u].y), bf16_hi(zw[u].y)};
-        float w[4], q[4], sd[4], d;
+        // w: p without the division by d; pq: p q without it
+        float w[4], sd[4], pq[4], d;
         if (kSigmoid) {
-          // exp(-|x|) as in the router backward alone: logits of 32 or more take a longer form,
-          // chosen per wave and row
+          // exp(-|x|) as in the router backward alone: logits from 32 to 104 take a longer form,
+          // chosen per wave and row.  Beyond (masked experts) both forms give 0.  Without the router
+          // nothing is a multiple of sigmoid': what the short form loses, 1e-7 of a probability at 90,
+          // does not matter.
           float ex[4];
-          const float top = max3_abs(max3_abs(0.0f, x[0], x[1]), x[2], x[3]);
-          if (kRouter == kAlone) {
-            // (nothing is a multiple of sigmoid': what the short form loses above 32, 1e-7 of a
-            // probability at 90, does not matter, and 0 from 128 on is 0 at any power)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16(__builtin_elementwise_minimum(fabsf(x[i]), 128.0f));
-          } else if (__builtin_expect(__any(top >= kSigmoidMax), 0)) {
+          if (kRouter != kAlone && __builtin_expect(__any(any_from_32_to_104(zw[u].x, zw[u].y)), 0)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16_wide(fabsf(x[i]));
             asm volatile("; large logits");
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16(fabsf(x[i]));
+            for (int i = 0; i < 4; ++i) ex[i] = exp_neg_bf16<true>(fabsf(x[i]));
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float r = newton_rcp(1.0f + ex[i]), er = ex[i] * r;     // sigmoid(|x|), sigmoid(-|x|)
             w[i] = x[i] >= 0.0f ? r : er;
-            q[i] = x[i] >= 0.0f ? er : r;
-            sd[i] = __builtin_fmaf(-er, er, er);
+            pq[i] = sd[i] = __builtin_fmaf(-er, er, er);
           }
         }
         if (kSoftmax) {
           d = softmax_terms<G>(x, w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pq[i] = w[i];
         } else {
           d = group_sum<G>(w[0] + w[1] + (w[2] + w[3]));
           const bool tiny = d < kTinySum;
@@ -576,23 +587,21 @@ __global__ __launch_bounds__(kGradThreads, kGradWavesPerSimd) void balance_backw
             asm volatile("" : "+v"(w0), "+v"(w1));
             const float y[4] = {bf16_lo(w0), bf16_hi(w0), bf16_lo(w1), bf16_hi(w1)};
             d = softmax_where<G>(tiny, y, w, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pq[i] = tiny ? w[i] : pq[i];      // q is 1 there
           }
         }
         const float inv = d != 0.0f ? newton_rcp(d) : 0.0f;
         float c = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] *= inv;
-          c = __builtin_fmaf(w[i], C[i], c);
-        }
-        c = group_sum<G>(c);
+        for (int i = 0; i < 4; ++i) c = __builtin_fmaf(w[i], C[i], c);
+        c = group_sum<G>(c) * inv;
         const f32x4 gm = kRouter != kAlone ? place(u) + d0 : zero;
         f32x4 o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float a = w[i] * (C[i] - c);
-          if (!kSoftmax) a *= q[i];
-          if (kRouter != kAlone) a = __builtin_fmaf(gm[i], sd[i], a);
+          const float s = (C[i] - c) * inv;
+          const float a = kRouter != kAlone ? __builtin_fmaf(pq[i], s, gm[i] * sd[i]) : pq[i] * s;
           o[i] = on[u] ? a : 0.0f;
         }
         if (t < n) __builtin_nontemporal_store(o, &at<f32x4>(seg_gz, (t * E + 4 * g) * 4u));

@@ -90,12 +90,16 @@ __device__ __forceinline__ float sigmoid_f32(float x) {
 // exp(-a) of a BF16 a in [0, 32].  log2 e = kHi + kLo with kHi of 16 significant
 // bits: a of 8 bits makes a * kHi exact in binary32, so exp(-a) = 2^(-a kHi) *
 // exp(-a kLo ln 2), the second factor 1 - c to c^2/2 < 1.3e-8.
+// kAny: and of any other a >= 0, infinity included, to c^2/2 (1.3e-7 where the result is
+// least), without subnormal results; c is held below 1, a clamp that costs nothing.
 constexpr float kSigmoidMax = 32.0f;
+template <bool kAny = false>
 __device__ __forceinline__ float exp_neg_bf16(float a) {
   const float kHi = 1.44268798828125f;
   const float kLoLn2 = 4.888495368504664e-06f;
   const float e1 = __builtin_amdgcn_exp2f(-(a * kHi));
-  return __builtin_fmaf(-e1, a * kLoLn2, e1);
+  const float c = a * kLoLn2;
+  return __builtin_fmaf(-e1, kAny ? __builtin_amdgcn_fmed3f(c, 0.0f, 1.0f) : c, e1);
 }
 
 // The same of any BF16 a >= 0.  From a = 32 the second factor is 1 - c + c^2/2 (off by
