@@ -374,9 +374,11 @@ static void launch_loss_as(const BalanceArgs& a, const BalanceWorkspace& ws, hip
   most = most < kBalanceBlocks ? most : kBalanceBlocks;
   Pieces pieces;
   const int blocks = cut_groups(a.pt, a.T, most, &pieces), all = pieces.first[a.pt.P];
-  // Bunches pay where one block would read more than 256 KiB of pieces: 147,456 rows of E =
-  // 256 in 512 blocks take 39.5 us without and 23.8 with them, 1,000,003 rows of E = 8 20.1
-  // without and 23.7 with.  (10 bits: all blocks are one bunch.)
+  // Bunches pay where one block would read more than 256 KiB of pieces.  One group, without and
+  // with them: 16,384 rows of E = 256 17.7 and 12.4 us, 147,456 28.2 and 22.8, 1,000,003 of E =
+  // 128 61.2 and 55.8; of E = 64 34.2 and 34.6, of E = 16 19.0 and 22.3, of E = 8 18.8 and 24.0;
+  // at the line, 99,991 of E = 128 (254 KiB) 17.8 and 16.2, in three groups 15.1 and 15.5.  (10
+  // bits: all blocks are one bunch.)
   const int bunch_bits = (int64_t)all * E * (int64_t)sizeof(uint64_t) > (256 << 10) ? kBunchBits : 10;
   static_assert(kBalanceBlocks + EQB_MAX_PARTITIONS <= 1 << 10, "one bunch");
   balance_loss_kernel<E, kSoftmax, kMask><<<blocks, kLossThreads, 0, s>>>(

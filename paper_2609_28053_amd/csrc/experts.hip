@@ -443,9 +443,13 @@ static void launch_form(const RowArgs& a, hipStream_t s) {
 
 // Lanes and pieces for a row, by the number of its pieces: the fewest lanes that hold a row
 // of up to 64 pieces, whole waves with 2 or 4 pieces each beyond.  Few tokens: split over
-// more waves (past 4,096 waves of 64 pieces that costs: 8,000 tokens of 1,024 bf16, K = 8,
-// combine 31.5 -> 38 us), or in the backward pass over a block's (one token of 8,192 bf16, K =
-// 8: 42 us in a wave, 12.9 in a block; 1,000 of 7,168: 70 and 56; 2,000 of 4,096: 63 and 68).
+// more waves.  8 to 512 tokens of 2,048 bf16, K = 8: combine 5.2 to 6.1 us whole, 5.1 to 5.5
+// split, dispatch 4.2 to 7.1 and 4.2 to 6.3; of 7,168, 8 to 128 tokens: 5.8 to 6.2 and 5.1 to
+// 5.5, 5.0 to 7.2 and 4.3 to 6.0.  Past 4,096 waves of 64 pieces it costs: 1,000 tokens of
+// 4,096, combine 13.3 -> 17.3, 8,000 of 1,024 25.9 -> 34.0; dispatch within 3% either way.
+// In the backward pass over a block's waves: one token of 8,192 bf16, K = 8, 42 us in a wave,
+// 12.9 in a block; 64 to 1,000 tokens of 1,024 to 7,168, K = 2 and 8, a wave takes 0.85 (1,000
+// of 1,024) to 1.9 times as long as a block (64 of 7,168), 2,000 tokens 0.78 to 1.05.
 // Calls on experts' rows of kStreamBytes (the memory-side cache) and more pass by it: loads
 // of the experts' rows and all stores are non-temporal, in calls that write experts' rows
 // only where those are whole lines of 128 bytes; dispatch then splits rows over waves by the
