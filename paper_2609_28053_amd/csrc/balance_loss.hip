@@ -424,9 +424,10 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // routing.  With the loss before it, 99,991 rows of E = 128 (26 MB) 35.8 us with non-temporal
 // loads, 32.0 without; 131,072 of E = 256 (64 MiB) 56.0 and 55.2; 2,000,000 of E = 32 (128
 // MB) 96 and 105; the gradient alone of 4,194,304 of E = 256 1,274 and 1,325.
-// Two rows a lane and eight waves a SIMD: 4,194,304 rows of E = 256, K = 8
-// take 1,276 us (5.3 TB/s), with three rows and six waves 1,324, four and four 1,320, one
-// and eight 1,306; 1,000,003 of E = 128 161, 175, 161, 164.
+// Two rows a lane and eight waves a SIMD: when this was chosen, over one set of buffers,
+// 4,194,304 rows of E = 256, K = 8 took 1,276 us, with three rows and six waves 1,324, four
+// and four 1,320, one and eight 1,306; 1,000,003 of E = 128 161, 175, 161, 164.  Over buffers
+// that change they take 1,345 (5.0 TB/s) and 164.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;
 constexpr int kGradU = 2;          // rows per lane and step
 constexpr int kGradWavesPerSimd = 8;
