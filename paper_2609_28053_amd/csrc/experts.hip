@@ -390,8 +390,12 @@ __global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(const Row
 #pragma unroll
                 for (int e = 0; e < V; ++e) y[e] = e >= skip ? y[e] : 0.0f;
               }
+              // a piece's products in pairs: V times fewer roundings of the running sum
 #pragma unroll
-              for (int e = 0; e < V; ++e) dot[j] += y[e];
+              for (int n = V / 2; n > 0; n /= 2)
+#pragma unroll
+                for (int e = 0; e < n; ++e) y[e] += y[e + n];
+              dot[j] += y[0];
             }
             part.store(gin + r[j] * a.H, a.H, v[j]);
           }
