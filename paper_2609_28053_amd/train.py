@@ -190,7 +190,8 @@ class AdamW(_Handle):
     they are then.  device_steps: the number of steps taken is kept on the
     device from the start, as steps that are captured in a graph need; else it
     moves there with the first found_inf, which may skip steps without the host
-    knowing.  Reading ``steps`` then waits for the device."""
+    knowing.  Reading ``steps`` then waits for the current stream, and
+    load_state_dict copies there."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
                  seed=0, device_steps=False):
@@ -210,7 +211,7 @@ class AdamW(_Handle):
             self.exp_avg_scale = self.exp_avg_sq_scale = None
         self.exp_avg, self.exp_avg_sq = new(), new()
         self._tensors = None
-        if device_steps:
+        if device_steps and self.params:
             self._count_on_device()
         self._filled(self.params[0].device if self.params else "cpu")
 
@@ -231,8 +232,7 @@ class AdamW(_Handle):
             self._counter[0].fill_(int(n))
 
     def _count_on_device(self):
-        counter = torch.zeros(eqb.EQB_ADAMW_COUNTER_BYTES // 8, dtype=torch.int64,
-                              device=self.params[0].device if self.params else "cpu")
+        counter = torch.zeros(eqb.EQB_ADAMW_COUNTER_BYTES // 8, dtype=torch.int64, device=self.params[0].device)
         counter[0].fill_(self._steps)
         self._counter = counter
 
@@ -250,7 +250,7 @@ class AdamW(_Handle):
         with self._on(stream, grad_scale, found_inf, *grads):
             if self._counter is None and torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("a captured step needs AdamW(device_steps=True): replays would repeat one step's number")
-            if self._counter is None and found_inf is not None:
+            if self._counter is None and found_inf is not None and self.params:
                 self._count_on_device()
                 self._behind.clear()
             numbers = (self.lr if lr is None else lr, *self.betas, self.eps, self.seed, grad_scale, found_inf)

@@ -141,6 +141,15 @@ def test_steps_that_may_be_skipped_are_counted_on_the_device(calls):
     assert calls[-1]["step"] is on._counter and on.steps == 0
 
 
+def test_no_parameters(calls):
+    """An optimizer of nothing takes its steps, whatever they are given."""
+    for opt in (AdamW([]), AdamW([], state_bits=8, device_steps=True)):
+        opt.step([])
+        opt.step([], found_inf=torch.zeros(1))
+        assert opt.steps == 2
+    assert [c["step"] for c in calls] == [1, 2, 1, 2] and all(c["param"] == [] for c in calls)
+
+
 @pytest.mark.parametrize("bits", [8, 32])
 def test_a_state_that_does_not_fit_changes_nothing(bits):
     params, _, opt = model(bits)
