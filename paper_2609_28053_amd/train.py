@@ -131,16 +131,16 @@ class BalanceLoss(_Handle):
     gradient with the router backward.  score: "sigmoid" (normalised) or
     "softmax".
 
-    Every forward writes new ``load``, ``tokens``, ``prob`` and ``loss``, and
-    leaves in ``saved`` what its gradient takes of them.  backward takes the
-    newest unless it is given one: with several batches in flight (gradient
+    Every forward writes new ``load``, ``tokens``, ``prob`` and ``loss``;
+    ``saved`` is what its gradient takes of them.  backward takes the newest
+    unless it is given one: with several batches in flight (gradient
     accumulation) each keeps its own."""
 
     def __init__(self, T: int, E: int, K: int, P: int = 1, alpha: float = 1e-2, score: str = "sigmoid", device="cuda"):
         self.T, self.E, self.K, self.P, self.alpha = T, E, K, P, alpha
         self.score = {"sigmoid": eqb.EQB_SCORE_SIGMOID, "softmax": eqb.EQB_SCORE_SOFTMAX}[score]
         dev = torch.device(device)
-        self.load = self.tokens = self.prob = self.loss = self.saved = None
+        self.load = self.tokens = self.prob = self.loss = None
         self.workspace = torch.zeros(eqb.eqb_balance_workspace_size(E, P), dtype=torch.uint8, device=dev)
         self._filled(dev)
 
@@ -164,15 +164,20 @@ class BalanceLoss(_Handle):
             loss = torch.empty(self.P, dtype=torch.float32, **new)
             eqb.eqb_balance_loss(z, topk_idx, self.K, self.alpha, load, tokens, prob, loss, self.workspace, valid, part_off,
                                  self.score)
-        self.load, self.tokens, self.prob, self.loss, self.saved = load, tokens, prob, loss, (load, tokens)
+        self.load, self.tokens, self.prob, self.loss = load, tokens, prob, loss
         return loss
+
+    @property
+    def saved(self):
+        """What the gradient takes of the newest forward."""
+        return self.load, self.tokens
 
     def backward(self, z, grad_loss, grad_z=None, topk_idx=None, grad_score=None, inj=None, valid=None,
                  part_off=None, stream=None, saved=None):
         """The gradient with respect to z; with topk_idx and grad_score (and inj), the whole router's."""
-        if saved is None and self.saved is None:
-            raise ValueError("no forward has been made")
         load, tokens = self.saved if saved is None else saved
+        if load is None:
+            raise ValueError("no forward has been made")
         with self._on(stream, z, grad_loss, grad_z, topk_idx, grad_score, inj, valid, load, tokens):
             if grad_z is None:
                 grad_z = torch.empty((self.T, self.E), dtype=torch.float32, device=z.device)

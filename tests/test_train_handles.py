@@ -233,7 +233,7 @@ def handles():
     T, E, K, H = 6, 8, 2, 4
     rows, loss = ExpertRows(T, E, K, device="cpu"), BalanceLoss(T, E, K, device="cpu")
     rows.slot = torch.zeros((T, K), dtype=torch.int32)
-    loss.saved = torch.zeros((1, E), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    loss.load, loss.tokens = torch.zeros((1, E), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     p = torch.zeros(3)
     opt = AdamW([p])
     x, r, w = torch.zeros(T, H), torch.zeros(T * K, H), torch.zeros(T, K)
@@ -316,5 +316,7 @@ def test_two_batches_in_flight_keep_their_loads(numbers):
     c = loss.forward(z, load=routed)
     routed.fill_(70)
     loss.backward(z, one, saved=first), loss.backward(z, one, saved=second), loss.backward(z, one)
-    assert numbers == ["loss"] * 3 + [(1, 1), (50, 2), (60, 3)]
+    loss.load = loss.load * 2                     # loads that the program has changed (summed over ranks, say)
+    loss.backward(z, one)
+    assert numbers == ["loss"] * 3 + [(1, 1), (50, 2), (60, 3), (120, 3)]
     assert (float(a), float(b), float(c)) == (1.0, 2.0, 3.0)
