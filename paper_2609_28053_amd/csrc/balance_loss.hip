@@ -417,7 +417,8 @@ eqb_status launch_balance_loss(const BalanceArgs& a, const BalanceWorkspace& ws,
 // the same bits, and p q of a sigmoid row is sigmoid' / d.  Against the bare exponential and
 // reciprocal, which lose digits of large logits and all beyond 87, that costs up to 2% (the
 // gradient of 1,000,003 rows of E = 128, K = 8: 160.5 -> 163.6 us, of 131,072 of E = 256 36.0
-// and 36.2; with logits of -inf among them, which do not take the longer form, 36.1 and 36.5).
+// and 36.2; with logits of -inf among them, which do not take the longer form, 36.1 and 36.5),
+// of a softmax in the caches more (300,000 of E = 64 24.0 -> 26.0).
 // Bound by memory: 2E + 8K bytes read and 4E written per row, all of it once.  The
 // gradient's stores are non-temporal, and so are the logits' loads when these take more than
 // a quarter of the memory-side cache (kStream); fewer are still there from the loss or the

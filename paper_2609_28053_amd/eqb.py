@@ -520,11 +520,13 @@ def _values(x):
 
 
 def _ptrs(tensors, dtype, numel, name):
-    """_ptr of each tensor of a list (217 tensors: 94 us, one by one 126)."""
-    if (all(isinstance(t, torch.Tensor) for t in tensors) and all(map(_on_gpu, tensors)) and
-            all(map(torch.Tensor.is_contiguous, tensors)) and set(map(_dtype_of, tensors)) <= {dtype} and
-            list(map(torch.Tensor.numel, tensors)) == numel):
-        return _addresses(tensors)
+    """_ptr of each tensor of a list (217 tensors: 83 us, one by one 127)."""
+    try:
+        if (all(map(_on_gpu, tensors)) and all(map(torch.Tensor.is_contiguous, tensors)) and
+                set(map(_dtype_of, tensors)) <= {dtype} and list(map(torch.Tensor.numel, tensors)) == numel):
+            return _addresses(tensors)
+    except (AttributeError, TypeError):       # something else than a tensor
+        pass
     return [_ptr(t, dtype, n, name) for t, n in zip(tensors, numel)]
 
 

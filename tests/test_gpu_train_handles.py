@@ -236,3 +236,41 @@ def test_batches_in_flight():
     for (z, idx, gy, out, w), (slot, saved), expected in zip(batches, kept, want):
         got = [*rows.combine_backward(gy, out, w, slot=slot), loss.backward(z, one, saved=saved)]
         assert all(torch.equal(a, b) for a, b in zip(got, expected))
+
+
+@pytest.mark.parametrize("warm", [False, True])
+def test_handles_in_a_graph(warm):
+    """Plan, rows, loss and gradients through the handles in one graph, captured at their first call on the stream or
+    after one, replayed on changing inputs with eager work between the replays."""
+    say(f"handles in a graph, warm={warm}")
+    z, idx = torch.zeros((T, E), dtype=torch.bfloat16, **D), torch.zeros((T, K), dtype=torch.int32, **D)
+    x, out, gy = (torch.zeros(s, dtype=torch.bfloat16, **D) for s in ((T, H), (T * K, H), (T, H)))
+    w, one, part = torch.zeros((T, K), **D), torch.ones(P, **D), eqb.PartOffsets([0, 100, 3000, T])
+
+    def work(rows, loss):
+        got = [rows.plan(idx).dispatch(x), rows.combine(out, w), *rows.combine_backward(gy, out, w)]
+        got += [loss.forward(z.view(torch.int16), idx, part_off=part)]
+        return got + [loss.backward(z.view(torch.int16), one, topk_idx=idx, grad_score=got[3], part_off=part)]
+
+    held, eager = made([], 32)[:2], made([], 32)[:2]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    if warm:
+        with torch.cuda.stream(s):
+            work(*held)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        captured = work(*held)
+    for replay in range(4):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(replay)
+        z.copy_(torch.randn((T, E), generator=g, **D))
+        idx.copy_(z.float().topk(K, dim=1).indices)
+        for t in (x, out, gy, w):
+            t.copy_(torch.randn(t.shape, generator=g, **D))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, work(*eager))), replay
+        torch.cuda.synchronize()
