@@ -486,6 +486,122 @@ eqb_status eqb_adamw_step_counted(const eqb_adamw_tensor* tensors, int32_t n, in
                                   const float* grad_scale, const float* found_inf, void* stream);
 
 /*
+ * ------------------------------------------------------------------------
+ * Routing by scores, and the experts' products in 8 bits.  The conventions
+ * above hold, every output is WRITTEN, and the buffers of one call must not
+ * overlap.  Pointers need the alignment of their elements where nothing else
+ * is said.
+ * ------------------------------------------------------------------------
+ */
+
+/*
+ * The experts of every token by their scores, and their weights.
+ *   s_e = sigmoid(z_e) (EQB_SCORE_SIGMOID) or exp(z_e) / sum_e' exp(z_e') (EQB_SCORE_SOFTMAX)
+ *   q_e = s_e + bias_e: what decides; an expert whose z_e or q_e is -inf or NaN is masked out of the
+ *     row.  z_e = +inf counts as the largest finite number.
+ *   groups > 1: the E experts are `groups` groups of E / groups neighbours.  A group's score is the
+ *     sum of its group_top (1 or 2) largest q that are not masked (of the one it has, or -inf without
+ *     any); only the experts of the top_groups groups of the largest scores take part.
+ *   The K largest q are chosen, in that order.  Where masks leave fewer, the last entries are
+ *     expert -1 of weight 0: dropped pairs to eqb_dispatch_plan.
+ *   weight_k = scale s_k / (sum of the chosen s) (normalize; 0 where that sum is 0) or scale s_k,
+ *     in binary32.  Scores below 2^-126 may count as 0 there.
+ * Ties go to the lower expert and to the lower group.  Which of two scores is larger is decided as
+ * in binary64 (without a bias: by the logits), so that the choice does not depend on a rounding of
+ * binary32.
+ *   z [T,E] of type dtype (EQB_DTYPE_*), 16-byte aligned; bias [E] binary32 (nullable: 0).
+ *   topk_idx [T,K] int32 (out); topk_weight [T,K] binary32 (out).
+ * groups: a power of two up to E; 1 <= top_groups <= groups; group_top <= E / groups;
+ * K <= top_groups E / groups; K < E.  T*K < 2^31.
+ */
+eqb_status eqb_route_scored(const void* z, const float* bias, int64_t T, int32_t E, int32_t K, int32_t groups,
+                            int32_t top_groups, int32_t group_top, int32_t score, int32_t normalize, double scale,
+                            int32_t dtype, int32_t* topk_idx, float* topk_weight, void* stream);
+
+/*
+ * The gradient of topk_weight with respect to the logits, the choice held fixed (the bias has none).
+ * With S = sum of the chosen s and a_k = scale (g_k - sum_j g_j s_j / S) / S (normalize) or scale g_k:
+ *   grad_z_e = (sum of a_k over the k that chose e) s_e (1 - s_e)                  (sigmoid)
+ *   grad_z_e = s_e ((sum of a_k over the k that chose e) - sum_k a_k s_k)          (softmax)
+ *   grad_weight [T,K] binary32 (in): the combine's grad_weight.  Entries whose topk_idx lies outside
+ *     [0, E) take no part.
+ *   grad_z [T,E] binary32 (out, 16-byte aligned).
+ */
+eqb_status eqb_route_scored_backward(const void* z, const int32_t* topk_idx, const float* grad_weight, int64_t T,
+                                     int32_t E, int32_t K, int32_t score, int32_t normalize, double scale,
+                                     int32_t dtype, float* grad_z, void* stream);
+
+/*
+ * Numbers in 8 bits: E4M3 codes (sign, 4 exponent and 3 mantissa bits, largest 448, no infinities)
+ * with a power of two for each block of EQB_CODE_BLOCK.  A block's scale is 2^x with the least
+ * x >= -126 for which no finite value exceeds 448 2^x; a code is value 2^-x rounded to nearest, ties
+ * to even; infinities and NaN become NaN.  A scale is kept as the byte x + 127.
+ *   A row of H elements is eqb_code_width(H) codes (H rounded up to whole blocks, zeros behind H) and
+ *   eqb_scale_width(H) scale bytes (one per block, rounded up to a multiple of 4, zeros behind).
+ * Codes and scales are 16-byte aligned.  1 <= H <= 2^24.
+ *
+ *   eqb_quantize_rows: codes [rows, eqb_code_width(hidden)], scales [rows, eqb_scale_width(hidden)] of
+ *     x [rows, hidden].  count (nullable, device int32): only the first *count rows are read and
+ *     written (the offsets[E] of a plan).
+ *   eqb_dispatch_quantized: eqb_dispatch and eqb_quantize_rows in one: x [T, hidden] to the rows that
+ *     slot names; rows that no slot names are left as they are.
+ *   eqb_quantize_columns: the same values along the other axis, for eqb_experts_grad_weight: codes
+ *     [hidden, W] with W = eqb_column_width(rows, E), scales [hidden, eqb_scale_width(W)].  Row
+ *     offsets[e] + i of expert e is column 128 (offsets[e] / 128 + e) + i; zeros fill an expert's last
+ *     block.  Columns of no expert's block are left as they are.
+ *   eqb_quantize_weights: w [E,N,hidden] with one scale for each 128 x 128: codes
+ *     [E,N,eqb_code_width(hidden)], scales [E, ceil(N/128), eqb_scale_width(hidden)], and the transposed
+ *     codes_t [E,hidden,eqb_code_width(N)], scales_t [E, ceil(hidden/128), eqb_scale_width(N)], the same
+ *     values for the gradient of the rows.  Either pair may be null.
+ * Offsets are taken as if they lay in [0, rows].  1 <= E <= 256 here, not only powers of two.
+ */
+#define EQB_CODE_BLOCK       128
+int64_t eqb_code_width(int64_t hidden);                      /* host only */
+int64_t eqb_scale_width(int64_t hidden);                     /* host only */
+int64_t eqb_column_width(int64_t rows, int32_t E);           /* host only */
+eqb_status eqb_quantize_rows(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype,
+                             uint8_t* codes, uint8_t* scales, void* stream);
+eqb_status eqb_dispatch_quantized(const void* x, const int32_t* slot, int64_t T, int32_t K, int64_t rows,
+                                  int32_t hidden, int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream);
+eqb_status eqb_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
+                                int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream);
+eqb_status eqb_quantize_weights(const void* w, int32_t E, int32_t N, int32_t hidden, int32_t dtype, uint8_t* codes,
+                                uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/*
+ * The experts' products (what FFN_e of Eq. 1 is made of), in the codes above, summed in binary32 and
+ * rounded once to dtype.
+ *   eqb_experts_product: out[r,n] = sum_k x[r,k] w[e,n,k] for the rows r of expert e (offsets [E+1],
+ *     device, as eqb_dispatch_plan writes them): codes and scales of x [rows, hidden] and of w
+ *     [E,N,hidden].  Rows outside the experts' ranges are left as they are.  With the transposed weights
+ *     it is the gradient of the rows: grad_x[r,k] = sum_n grad_out[r,n] w[e,n,k].
+ *   eqb_experts_grad_weight: out[e,n,k] = sum over the rows r of expert e of grad[r,n] x[r,k], from the
+ *     columns' codes of grad [rows, N] and of x [rows, hidden]; zeros for an expert without rows.
+ */
+eqb_status eqb_experts_product(const uint8_t* codes, const uint8_t* scales, const uint8_t* w_codes,
+                               const uint8_t* w_scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,
+                               int32_t hidden, int32_t dtype, void* out, void* stream);
+eqb_status eqb_experts_grad_weight(const uint8_t* grad_codes, const uint8_t* grad_scales, const uint8_t* codes,
+                                   const uint8_t* scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,
+                                   int32_t hidden, int32_t dtype, void* out, void* stream);
+
+/*
+ * The gated activation between an expert's two products: x [rows, 2 hidden] holds a row's gate g and
+ * then its u, h = g sigmoid(g) u.  Computed in binary32, rounded once.
+ *   eqb_gated: h [rows, hidden] of x's type.  eqb_gated_quantize: h as eqb_quantize_rows leaves it,
+ *   without a rounding in between.
+ *   eqb_gated_backward: grad_x [rows, 2 hidden] from grad_h [rows, hidden]:
+ *     grad_g = grad_h u s (1 + g (1 - s)), grad_u = grad_h g s, s = sigmoid(g).
+ * count as in eqb_quantize_rows.
+ */
+eqb_status eqb_gated(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype, void* h,
+                     void* stream);
+eqb_status eqb_gated_quantize(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype,
+                              uint8_t* codes, uint8_t* scales, void* stream);
+eqb_status eqb_gated_backward(const void* grad_h, const void* x, const int32_t* count, int64_t rows, int32_t hidden,
+                              int32_t dtype, void* grad_x, void* stream);
+
+/*
  * Test control (host only, no HIP call): caps the number of blocks of the
  * streaming kernels (routing, the margin passes, the LEI kernels, the balance
  * loss and its gradient, the experts' rows) at max_blocks for the calls that

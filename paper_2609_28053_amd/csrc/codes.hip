@@ -1,0 +1,403 @@
+// codes.hip - rows, columns and weights as E4M3 codes with a power of two for each block
+// of 128, and the gated activation between an expert's two products (what FFN_e of Eq. 1,
+// arXiv 2609.28053, works on).
+//
+// A block's scale is the least power of two under which no finite value exceeds 448, so
+// that scaling is exact and a code's rounding is the only one.  All of it is bound by
+// memory.
+#include "eqb_internal.hpp"
+
+namespace eqb {
+namespace {
+
+// Eight neighbouring elements of a row, and what they are in memory.
+template <int kDtype>
+struct Elem;
+template <>
+struct Elem<EQB_DTYPE_BF16> {
+  typedef uint16_t raw;
+  static __device__ __forceinline__ float to_f(raw x) { return __uint_as_float((uint32_t)x << 16); }
+  static __device__ __forceinline__ raw from_f(float x) { return (raw)bf16x2_bits(x, x); }
+};
+template <>
+struct Elem<EQB_DTYPE_F16> {
+  typedef _Float16 raw;
+  static __device__ __forceinline__ float to_f(raw x) { return (float)x; }
+  static __device__ __forceinline__ raw from_f(float x) { return (raw)x; }
+};
+template <>
+struct Elem<EQB_DTYPE_F32> {
+  typedef float raw;
+  static __device__ __forceinline__ float to_f(raw x) { return x; }
+  static __device__ __forceinline__ raw from_f(float x) { return x; }
+};
+
+constexpr int kPer = 8;                  // elements of a lane
+template <int kDtype>
+struct Eight {
+  typedef typename Elem<kDtype>::raw raw;
+  typedef raw vec __attribute__((ext_vector_type(kPer)));
+  // gfx950's global loads and stores take any address
+  typedef vec any __attribute__((aligned(alignof(raw))));
+};
+
+// Elements c .. c + 7 of a row of H, zeros behind its end.
+template <int kDtype>
+__device__ __forceinline__ void load8(const typename Elem<kDtype>::raw* row, int c, int H, float (&v)[kPer]) {
+  typedef Elem<kDtype> D;
+  if (c + kPer <= H) {
+    const typename Eight<kDtype>::vec x = *reinterpret_cast<const typename Eight<kDtype>::any*>(row + c);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = D::to_f(x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = c + i < H ? D::to_f(row[c + i]) : 0.0f;
+  }
+}
+
+template <int kDtype>
+__device__ __forceinline__ void store8(typename Elem<kDtype>::raw* row, int c, int H, const float (&v)[kPer]) {
+  typedef Elem<kDtype> D;
+  typename Eight<kDtype>::vec x;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) x[i] = D::from_f(v[i]);
+  if (c + kPer <= H) {
+    *reinterpret_cast<typename Eight<kDtype>::any*>(row + c) = x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (c + i < H) row[c + i] = x[i];
+  }
+}
+
+// |v| where it is finite, else 0
+__device__ __forceinline__ float finite_abs(float v) {
+  const float a = fabsf(v);
+  return a < __builtin_inff() ? a : 0.0f;
+}
+// The scale's byte for a largest magnitude: its exponent less 8, one more where its
+// significand exceeds 1.75.
+__device__ __forceinline__ int scale_byte(float top) {
+  const int b = (int)((__float_as_uint(top) + 0x1FFFFFu) >> 23) - 8;
+  return b > 1 ? b : 1;
+}
+__device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+// Codes of four values, rounded to nearest even by the conversion itself.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+
+// sigmoid(x) and 1 - sigmoid(x) of any x: exp(-|x|) = 2^(-p) (1 - l ln 2) with p + l = |x| log2 e
+// in two parts (the hardware's 2^p is off by one ulp), then a reciprocal with one Newton step.
+__device__ __forceinline__ void sigmoid_both(float x, float& s, float& rest) {
+  const float kLog2e = 1.44269502162933349609375f, kLow = 1.92596303e-8f, kLn2 = 0.693147182f;
+  const float a = fminf(fabsf(x), 200.0f);
+  const float p = a * kLog2e;
+  const float l = __builtin_fmaf(a, kLow, __builtin_fmaf(a, kLog2e, -p));
+  const float e0 = __builtin_amdgcn_exp2f(-p);
+  const float e = __builtin_fmaf(-e0 * kLn2, l, e0);
+  const float r = newton_rcp(1.0f + e), q = e * r;
+  s = x >= 0.0f ? r : q;
+  rest = x >= 0.0f ? q : r;
+}
+
+// ------------------------------------------------------------- the rows --
+constexpr int kCodeThreads = 256, kCodeWaves = kCodeThreads / 64;
+constexpr int kWaveCols = 64 * kPer;          // a wave's part of a row: four blocks, one word of scales
+
+template <int kDtype>
+struct PlainRow {
+  typedef typename Elem<kDtype>::raw raw;
+  static __device__ __forceinline__ void load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+    load8<kDtype>(static_cast<const raw*>(a.x) + t * a.H, c, a.H, v);
+  }
+};
+template <int kDtype>
+struct GatedRow {
+  typedef typename Elem<kDtype>::raw raw;
+  static __device__ __forceinline__ void load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+    const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
+    float g[kPer], u[kPer];
+    load8<kDtype>(row, c, a.H, g);
+    load8<kDtype>(row + a.H, c, a.H, u);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      float s, rest;
+      sigmoid_both(g[i], s, rest);
+      v[i] = g[i] * s * u[i];
+    }
+  }
+};
+
+__device__ __forceinline__ int64_t rows_in_use(const CodeArgs& a) {
+  if (!a.count) return a.T;
+  const int64_t n = *a.count;
+  return n < a.T ? n : a.T;
+}
+
+// Sixteen lanes hold a block; a wave holds four.  With slots, a token's codes go to all of
+// its rows.
+template <class Row>
+__global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeArgs a, int segments) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t rows = rows_in_use(a), width = code_width(a.H), scales = scale_width(a.H);
+  for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
+    const int c = (int)seg * kWaveCols + lane * kPer;
+    for (int64_t t = (int64_t)blockIdx.y * kCodeWaves + wave; t < rows; t += (int64_t)gridDim.y * kCodeWaves) {
+      float v[kPer], top = 0.0f;
+      Row::load(a, t, c, v);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = fmaxf(top, finite_abs(v[i]));
+      const int byte = scale_byte(group_max<16>(top));
+      const float inv = scale_inverse(byte);
+      uint2 code;
+      code.x = codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      code.y = codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+      const int mine = c < width ? byte : 0;
+      const uint32_t word = (uint32_t)__builtin_amdgcn_readlane(mine, 0) | (uint32_t)__builtin_amdgcn_readlane(mine, 16) << 8 |
+                            (uint32_t)__builtin_amdgcn_readlane(mine, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(mine, 48) << 24;
+      for (int k = 0; k < a.K; ++k) {
+        const int64_t r = a.slot ? a.slot[t * a.K + k] : t;
+        if (r < 0 || r >= a.rows) continue;
+        if (c < width) *reinterpret_cast<uint2*>(a.codes + r * width + c) = code;
+        if (lane == 0) *reinterpret_cast<uint32_t*>(a.scales + r * scales + seg * 4) = word;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------- the gate --
+template <int kDtype, bool kBackward>
+__global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, int segments) {
+  typedef typename Elem<kDtype>::raw raw;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t rows = rows_in_use(a);
+  for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
+    const int c = (int)seg * kWaveCols + lane * kPer;
+    if (c >= a.H) continue;
+    for (int64_t t = (int64_t)blockIdx.y * kCodeWaves + wave; t < rows; t += (int64_t)gridDim.y * kCodeWaves) {
+      if constexpr (!kBackward) {
+        float v[kPer];
+        GatedRow<kDtype>::load(a, t, c, v);
+        store8<kDtype>(static_cast<raw*>(a.out) + t * a.H, c, a.H, v);
+      } else {
+        const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
+        raw* to = static_cast<raw*>(a.out) + t * 2 * a.H;
+        float g[kPer], u[kPer], h[kPer];
+        load8<kDtype>(row, c, a.H, g);
+        load8<kDtype>(row + a.H, c, a.H, u);
+        load8<kDtype>(static_cast<const raw*>(a.grad) + t * a.H, c, a.H, h);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          float s, rest;
+          sigmoid_both(g[i], s, rest);
+          const float hs = h[i] * s;
+          const float gu = hs * g[i];
+          g[i] = hs * u[i] * __builtin_fmaf(g[i], rest, 1.0f);
+          u[i] = gu;
+        }
+        store8<kDtype>(to, c, a.H, g);
+        store8<kDtype>(to + a.H, c, a.H, u);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------- columns and weights --
+// A tile of 128 x 128: a thread holds 8 neighbouring rows of 8 neighbouring columns, and the
+// transposed codes go through LDS.  kWeights: one scale for the tile, and the codes in the
+// rows' order too.
+constexpr int kTileStride = kCodeBlock + 16;       // bytes of a column in LDS
+
+// The expert whose blocks of columns hold block b: the last one whose first block is at most b.
+__device__ __forceinline__ int expert_of_block(const int32_t* offsets, int E, int64_t rows, int64_t b, int lane) {
+  int n = 0;
+  for (int e0 = 0; e0 < E; e0 += 64) {
+    const int e = e0 + lane;
+    int64_t off = e < E ? offsets[e] : 0;
+    off = off < 0 ? 0 : off > rows ? rows : off;
+    n += __popcll(__ballot(e < E && off / kCodeBlock + e <= b));
+  }
+  return n - 1;
+}
+
+template <int kDtype, bool kWeights>
+__global__ __launch_bounds__(256) void quantize_tiles_kernel(const CodeArgs a) {
+  typedef typename Elem<kDtype>::raw raw;
+  __shared__ uint8_t sh_code[kCodeBlock * kTileStride];
+  __shared__ float sh_top[4][kCodeBlock];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = tid & 15, rg = tid >> 4;
+  // this tile's place among the tiles of columns, and of (an expert's) rows
+  const uint32_t across = (uint32_t)(code_width(a.H) / kCodeBlock);
+  const uint32_t bx = blockIdx.x % across, down = (uint32_t)(code_width(a.N) / kCodeBlock);
+  const uint32_t by = kWeights ? blockIdx.x / across % down : blockIdx.x / across;
+  int e, first;                 // the expert, and the first of its rows here
+  int64_t base;                 // the row before those
+  int nr;                       // rows of the tile
+  if (kWeights) {
+    e = blockIdx.x / across / down;
+    first = by * kCodeBlock;
+    base = (int64_t)e * a.N;
+    nr = a.N - first;
+  } else {
+    e = expert_of_block(a.offsets, a.E, a.rows, by, lane);
+    if (e < 0) return;
+    int64_t begin = a.offsets[e], end = a.offsets[e + 1];
+    begin = begin < 0 ? 0 : begin > a.rows ? a.rows : begin;
+    end = end > a.rows ? a.rows : end;
+    const int64_t local = ((int64_t)by - (begin / kCodeBlock + e)) * kCodeBlock;
+    if (local >= end - begin) return;
+    first = (int)local;
+    base = begin;
+    nr = (int)(end - begin - local);
+  }
+  if (nr > kCodeBlock) nr = kCodeBlock;
+  const int c0 = bx * kCodeBlock, c = c0 + cg * kPer;
+  float v[kPer][kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = rg * kPer + i;
+    if (r < nr && c < a.H) {
+      load8<kDtype>(static_cast<const raw*>(a.x) + (base + first + r) * a.H, c, a.H, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) v[i][j] = 0.0f;
+    }
+  }
+  float top[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    top[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) top[j] = fmaxf(top[j], finite_abs(v[i][j]));
+    top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
+    top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+  }
+  if (kWeights) {
+#pragma unroll
+    for (int j = 1; j < kPer; ++j) top[0] = fmaxf(top[0], top[j]);
+    top[0] = group_max<16>(top[0]);
+    if (lane == 0) sh_top[wave][0] = top[0];
+  } else if (lane < 16) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) sh_top[wave][cg * kPer + j] = top[j];
+  }
+  __syncthreads();
+  int byte[kPer];
+  float inv[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int at = kWeights ? 0 : cg * kPer + j;
+    byte[j] = scale_byte(fmaxf(fmaxf(sh_top[0][at], sh_top[1][at]), fmaxf(sh_top[2][at], sh_top[3][at])));
+    inv[j] = scale_inverse(byte[j]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) v[i][j] *= inv[j];
+  if (kWeights && a.codes) {
+    const int64_t width = code_width(a.H);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int r = rg * kPer + i;
+      if (r >= nr) continue;
+      uint2 code;
+      code.x = codes4(v[i][0], v[i][1], v[i][2], v[i][3]);
+      code.y = codes4(v[i][4], v[i][5], v[i][6], v[i][7]);
+      *reinterpret_cast<uint2*>(a.codes + (base + first + r) * width + c) = code;
+    }
+    // with the last block of a row, the zeros behind its scales
+    const int64_t scales = scale_width(a.H);
+    const int more = (int)(bx + 1 == across ? scales - bx : 1);
+    if (tid < more)
+      a.scales[((int64_t)e * down + by) * scales + bx + tid] = tid == 0 ? (uint8_t)byte[0] : 0;
+  }
+  uint8_t* const to = kWeights ? a.codes_t : a.codes;
+  if (!to) return;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    uint2 code;
+    code.x = codes4(v[0][j], v[1][j], v[2][j], v[3][j]);
+    code.y = codes4(v[4][j], v[5][j], v[6][j], v[7][j]);
+    *reinterpret_cast<uint2*>(sh_code + (cg * kPer + j) * kTileStride + rg * kPer) = code;
+  }
+  __syncthreads();
+  const int64_t width = kWeights ? code_width(a.N) : column_width(a.rows, a.E);
+  const int64_t lead = kWeights ? (int64_t)e * a.H : 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = tid + i * 256, col = at >> 3, piece = at & 7;
+    if (c0 + col < a.H)
+      *reinterpret_cast<uint4*>(to + (lead + c0 + col) * width + (int64_t)by * kCodeBlock + piece * 16) =
+          *reinterpret_cast<const uint4*>(sh_code + col * kTileStride + piece * 16);
+  }
+  const int64_t scales = scale_width(width);
+  if (kWeights) {
+    const int more = (int)(by + 1 == down ? scales - by : 1);
+    if (tid < more)
+      a.scales_t[((int64_t)e * across + bx) * scales + by + tid] = tid == 0 ? (uint8_t)byte[0] : 0;
+  } else if (rg == 0) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (c + j < a.H) a.scales[(int64_t)(c + j) * scales + by] = (uint8_t)byte[j];
+  }
+}
+
+dim3 row_grid(const CodeArgs& a, int64_t width, int* segments) {
+  *segments = (int)((width + kWaveCols - 1) / kWaveCols);
+  int64_t y = (a.T + kCodeWaves - 1) / kCodeWaves, most = 65535;
+  const int cap = max_blocks_cap();
+  if (cap > 0 && cap < most) most = cap;
+  if (y > most) y = most;
+  return dim3((uint32_t)(*segments < 1024 ? *segments : 1024), (uint32_t)y);
+}
+
+template <template <int> class Row>
+eqb_status launch_rows_of(const CodeArgs& a, hipStream_t s) {
+  int segments;
+  const dim3 grid = row_grid(a, code_width(a.H), &segments);
+  if (a.dtype == EQB_DTYPE_BF16) quantize_rows_kernel<Row<EQB_DTYPE_BF16>><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else if (a.dtype == EQB_DTYPE_F16) quantize_rows_kernel<Row<EQB_DTYPE_F16>><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else quantize_rows_kernel<Row<EQB_DTYPE_F32>><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  return launch_status();
+}
+
+template <bool kBackward>
+eqb_status launch_gate(const CodeArgs& a, hipStream_t s) {
+  int segments;
+  const dim3 grid = row_grid(a, a.H, &segments);
+  if (a.dtype == EQB_DTYPE_BF16) gated_kernel<EQB_DTYPE_BF16, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else if (a.dtype == EQB_DTYPE_F16) gated_kernel<EQB_DTYPE_F16, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else gated_kernel<EQB_DTYPE_F32, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  return launch_status();
+}
+
+template <bool kWeights>
+eqb_status launch_tiles(const CodeArgs& a, int64_t tiles, hipStream_t s) {
+  if (tiles > INT32_MAX) return EQB_ERR_UNSUPPORTED;
+  const uint32_t grid = (uint32_t)tiles;
+  if (a.dtype == EQB_DTYPE_BF16) quantize_tiles_kernel<EQB_DTYPE_BF16, kWeights><<<grid, 256, 0, s>>>(a);
+  else if (a.dtype == EQB_DTYPE_F16) quantize_tiles_kernel<EQB_DTYPE_F16, kWeights><<<grid, 256, 0, s>>>(a);
+  else quantize_tiles_kernel<EQB_DTYPE_F32, kWeights><<<grid, 256, 0, s>>>(a);
+  return launch_status();
+}
+
+}  // namespace
+
+eqb_status launch_quantize_rows(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, s); }
+eqb_status launch_dispatch_quantized(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, s); }
+eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s) { return launch_rows_of<GatedRow>(a, s); }
+eqb_status launch_gated(const CodeArgs& a, hipStream_t s) { return launch_gate<false>(a, s); }
+eqb_status launch_gated_backward(const CodeArgs& a, hipStream_t s) { return launch_gate<true>(a, s); }
+
+eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s) {
+  return launch_tiles<false>(a, code_width(a.H) / kCodeBlock * (column_width(a.rows, a.E) / kCodeBlock), s);
+}
+eqb_status launch_quantize_weights(const CodeArgs& a, hipStream_t s) {
+  return launch_tiles<true>(a, code_width(a.H) / kCodeBlock * (code_width(a.N) / kCodeBlock) * a.E, s);
+}
+
+}  // namespace eqb

@@ -68,6 +68,11 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 // Whether all pointers have the alignment of their 32-bit elements.
 template <class... P>
 bool aligned4(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0; }
+// Whether all pointers have the alignment of elements of the type.
+template <class... P>
+bool aligned_as(int32_t dtype, const P*... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & (dtype == EQB_DTYPE_F32 ? 3 : 1)) == 0;
+}
 
 }  // namespace
 }  // namespace eqb
@@ -533,6 +538,199 @@ eqb_status eqb_adamw_step_counted(const eqb_adamw_tensor* tensors, int32_t n, in
   if (reinterpret_cast<uintptr_t>(counter) % 8 != 0) return EQB_ERR_UNSUPPORTED;
   return adamw_call(tensors, n, grad_dtype, state_bits, 1, static_cast<AdamwCounter*>(counter), lr, beta1, beta2, eps,
                     seed, grad_scale, found_inf, stream);
+}
+
+// ------------------------------------------- routing by scores, 8 bits --
+static bool row_dtype(int32_t dtype) {
+  return dtype == EQB_DTYPE_F32 || dtype == EQB_DTYPE_BF16 || dtype == EQB_DTYPE_F16;
+}
+
+static eqb_status scored_shape(int64_t T, int32_t E, int32_t K, int32_t score, double scale, int32_t dtype) {
+  if (!plan_shape(T, K) || K >= E) return EQB_ERR_INVALID_ARG;
+  if (!supported_E(E)) return EQB_ERR_UNSUPPORTED;
+  if (score != EQB_SCORE_SIGMOID && score != EQB_SCORE_SOFTMAX) return EQB_ERR_INVALID_ARG;
+  if (!std::isfinite((float)scale) || !row_dtype(dtype)) return EQB_ERR_INVALID_ARG;
+  return EQB_OK;
+}
+
+eqb_status eqb_route_scored(const void* z, const float* bias, int64_t T, int32_t E, int32_t K, int32_t groups,
+                            int32_t top_groups, int32_t group_top, int32_t score, int32_t normalize, double scale,
+                            int32_t dtype, int32_t* topk_idx, float* topk_weight, void* stream) {
+  const eqb_status st = scored_shape(T, E, K, score, scale, dtype);
+  if (st != EQB_OK) return st;
+  if (groups < 1 || groups > E || E % groups != 0 || top_groups < 1 || top_groups > groups) return EQB_ERR_INVALID_ARG;
+  const int32_t each = E / groups;
+  if ((group_top != 1 && group_top != 2) || group_top > each || K > top_groups * each) return EQB_ERR_INVALID_ARG;
+  if (T == 0) return EQB_OK;
+  if (!z || !topk_idx || !topk_weight) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(z) || !aligned4(bias, topk_idx, topk_weight)) return EQB_ERR_UNSUPPORTED;
+  const ScoredArgs a{z, bias, T, E, K, groups, top_groups, group_top, score == EQB_SCORE_SOFTMAX, normalize != 0,
+                     (float)scale, dtype, topk_idx, topk_weight, nullptr, nullptr};
+  return launch_route_scored(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_route_scored_backward(const void* z, const int32_t* topk_idx, const float* grad_weight, int64_t T,
+                                     int32_t E, int32_t K, int32_t score, int32_t normalize, double scale,
+                                     int32_t dtype, float* grad_z, void* stream) {
+  const eqb_status st = scored_shape(T, E, K, score, scale, dtype);
+  if (st != EQB_OK) return st;
+  if (T == 0) return EQB_OK;
+  if (!z || !topk_idx || !grad_weight || !grad_z) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(z) || !aligned16(grad_z) || !aligned4(topk_idx, grad_weight)) return EQB_ERR_UNSUPPORTED;
+  const ScoredArgs a{z, nullptr, T, E, K, 1, 1, 1, score == EQB_SCORE_SOFTMAX, normalize != 0, (float)scale, dtype,
+                     const_cast<int32_t*>(topk_idx), nullptr, grad_weight, grad_z};
+  return launch_route_scored_backward(a, static_cast<hipStream_t>(stream));
+}
+
+constexpr int64_t kMostHidden = (int64_t)1 << 24;
+static bool code_shape(int64_t rows, int64_t hidden, int32_t dtype) {
+  return rows >= 0 && rows <= INT32_MAX && hidden >= 1 && hidden <= kMostHidden && row_dtype(dtype);
+}
+
+int64_t eqb_code_width(int64_t hidden) { return hidden < 1 ? 0 : code_width(hidden); }
+int64_t eqb_scale_width(int64_t hidden) { return hidden < 1 ? 0 : scale_width(hidden); }
+int64_t eqb_column_width(int64_t rows, int32_t E) {
+  return rows < 0 || E < 1 || E > kMostExperts ? 0 : column_width(rows, E);
+}
+
+eqb_status eqb_quantize_rows(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype,
+                             uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!code_shape(rows, hidden, dtype)) return EQB_ERR_INVALID_ARG;
+  if (rows == 0) return EQB_OK;
+  if (!x || !codes || !scales) return EQB_ERR_INVALID_ARG;
+  if (!aligned_as(dtype, x) || !aligned4(count) || !aligned16(codes) || !aligned16(scales)) return EQB_ERR_UNSUPPORTED;
+  CodeArgs a{};
+  a.x = x;
+  a.count = count;
+  a.T = a.rows = rows;
+  a.K = 1;
+  a.H = hidden;
+  a.dtype = dtype;
+  a.codes = codes;
+  a.scales = scales;
+  return launch_quantize_rows(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_dispatch_quantized(const void* x, const int32_t* slot, int64_t T, int32_t K, int64_t rows,
+                                  int32_t hidden, int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!plan_shape(T, K) || !code_shape(rows, hidden, dtype)) return EQB_ERR_INVALID_ARG;
+  if (T == 0) return EQB_OK;
+  if (!x || !slot || ((!codes || !scales) && rows > 0)) return EQB_ERR_INVALID_ARG;
+  if (!aligned_as(dtype, x) || !aligned4(slot) || !aligned16(codes) || !aligned16(scales)) return EQB_ERR_UNSUPPORTED;
+  CodeArgs a{};
+  a.x = x;
+  a.slot = slot;
+  a.T = T;
+  a.rows = rows;
+  a.K = K;
+  a.H = hidden;
+  a.dtype = dtype;
+  a.codes = codes;
+  a.scales = scales;
+  return launch_dispatch_quantized(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
+                                int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!code_shape(rows, hidden, dtype) || E < 1) return EQB_ERR_INVALID_ARG;
+  if (E > kMostExperts) return EQB_ERR_UNSUPPORTED;
+  if (rows == 0) return EQB_OK;
+  if (!x || !offsets || !codes || !scales) return EQB_ERR_INVALID_ARG;
+  if (!aligned_as(dtype, x) || !aligned4(offsets) || !aligned16(codes) || !aligned16(scales)) return EQB_ERR_UNSUPPORTED;
+  CodeArgs a{};
+  a.x = x;
+  a.offsets = offsets;
+  a.rows = rows;
+  a.E = E;
+  a.H = hidden;
+  a.dtype = dtype;
+  a.codes = codes;
+  a.scales = scales;
+  return launch_quantize_columns(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_quantize_weights(const void* w, int32_t E, int32_t N, int32_t hidden, int32_t dtype, uint8_t* codes,
+                                uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* stream) {
+  if (E < 1 || !code_shape(1, hidden, dtype) || !code_shape(1, N, dtype)) return EQB_ERR_INVALID_ARG;
+  if (E > kMostExperts) return EQB_ERR_UNSUPPORTED;
+  if (!w || (!codes) != (!scales) || (!codes_t) != (!scales_t) || (!codes && !codes_t)) return EQB_ERR_INVALID_ARG;
+  if (!aligned_as(dtype, w) || !aligned16(codes) || !aligned16(scales) || !aligned16(codes_t) || !aligned16(scales_t))
+    return EQB_ERR_UNSUPPORTED;
+  CodeArgs a{};
+  a.x = w;
+  a.E = E;
+  a.N = N;
+  a.H = hidden;
+  a.dtype = dtype;
+  a.codes = codes;
+  a.scales = scales;
+  a.codes_t = codes_t;
+  a.scales_t = scales_t;
+  return launch_quantize_weights(a, static_cast<hipStream_t>(stream));
+}
+
+static eqb_status product_call(eqb_status (*launch)(const ProductArgs&, hipStream_t), const ProductArgs& a,
+                               bool weights, void* stream) {
+  if (!code_shape(a.rows, a.H, a.dtype) || !code_shape(1, a.N, a.dtype) || a.E < 1) return EQB_ERR_INVALID_ARG;
+  if (a.E > kMostExperts) return EQB_ERR_UNSUPPORTED;
+  if (a.rows == 0 && !weights) return EQB_OK;
+  if (!a.x || !a.x_scales || !a.w || !a.w_scales || !a.offsets || !a.out) return EQB_ERR_INVALID_ARG;
+  if (!aligned16(a.x) || !aligned16(a.x_scales) || !aligned16(a.w) || !aligned16(a.w_scales)) return EQB_ERR_UNSUPPORTED;
+  if (!aligned4(a.offsets) || !aligned_as(a.dtype, a.out)) return EQB_ERR_UNSUPPORTED;
+  return launch(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_experts_product(const uint8_t* codes, const uint8_t* scales, const uint8_t* w_codes,
+                               const uint8_t* w_scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,
+                               int32_t hidden, int32_t dtype, void* out, void* stream) {
+  const ProductArgs a{codes, scales, w_codes, w_scales, offsets, rows, E, N, hidden, dtype, out};
+  return product_call(launch_experts_product, a, false, stream);
+}
+
+eqb_status eqb_experts_grad_weight(const uint8_t* grad_codes, const uint8_t* grad_scales, const uint8_t* codes,
+                                   const uint8_t* scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,
+                                   int32_t hidden, int32_t dtype, void* out, void* stream) {
+  const ProductArgs a{grad_codes, grad_scales, codes, scales, offsets, rows, E, N, hidden, dtype, out};
+  return product_call(launch_experts_grad_weight, a, true, stream);
+}
+
+static eqb_status gated_call(eqb_status (*launch)(const CodeArgs&, hipStream_t), const void* grad, const void* x,
+                             const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype, void* out, bool pointers,
+                             uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!code_shape(rows, hidden, dtype)) return EQB_ERR_INVALID_ARG;
+  if (rows == 0) return EQB_OK;
+  if (!pointers) return EQB_ERR_INVALID_ARG;
+  if (!aligned_as(dtype, x, grad, out) || !aligned4(count) || !aligned16(codes) || !aligned16(scales))
+    return EQB_ERR_UNSUPPORTED;
+  CodeArgs a{};
+  a.x = x;
+  a.count = count;
+  a.T = a.rows = rows;
+  a.K = 1;
+  a.H = hidden;
+  a.dtype = dtype;
+  a.grad = grad;
+  a.out = out;
+  a.codes = codes;
+  a.scales = scales;
+  return launch(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_gated(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype, void* h,
+                     void* stream) {
+  return gated_call(launch_gated, nullptr, x, count, rows, hidden, dtype, h, x && h, nullptr, nullptr, stream);
+}
+
+eqb_status eqb_gated_quantize(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype,
+                              uint8_t* codes, uint8_t* scales, void* stream) {
+  return gated_call(launch_gated_quantize, nullptr, x, count, rows, hidden, dtype, nullptr, x && codes && scales, codes,
+                    scales, stream);
+}
+
+eqb_status eqb_gated_backward(const void* grad_h, const void* x, const int32_t* count, int64_t rows, int32_t hidden,
+                              int32_t dtype, void* grad_x, void* stream) {
+  return gated_call(launch_gated_backward, grad_h, x, count, rows, hidden, dtype, grad_x, grad_h && x && grad_x, nullptr,
+                    nullptr, stream);
 }
 
 eqb_status eqb_set_max_blocks(int32_t max_blocks) {

@@ -190,6 +190,64 @@ eqb_status launch_dispatch(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine(const RowArgs& a, hipStream_t s);
 eqb_status launch_combine_backward(const RowArgs& a, hipStream_t s);
 
+// ------------------------------------------- routing by scores, 8 bits --
+struct ScoredArgs {
+  const void* z;
+  const float* bias;         // nullable
+  int64_t T;
+  int E, K, groups, top_groups, group_top;
+  bool softmax, normalize;
+  float scale;
+  int dtype;
+  int32_t* idx;              // out, and the gradient's input
+  float* weight;
+  const float* grad_weight;
+  float* grad_z;
+};
+eqb_status launch_route_scored(const ScoredArgs& a, hipStream_t s);
+eqb_status launch_route_scored_backward(const ScoredArgs& a, hipStream_t s);
+
+constexpr int kCodeBlock = EQB_CODE_BLOCK;
+constexpr int kMostExperts = 256;       // of the products
+__host__ __device__ inline int64_t code_width(int64_t H) { return (H + kCodeBlock - 1) / kCodeBlock * kCodeBlock; }
+__host__ __device__ inline int64_t scale_width(int64_t H) { return (code_width(H) / kCodeBlock + 3) / 4 * 4; }
+__host__ __device__ inline int64_t column_width(int64_t rows, int E) { return kCodeBlock * (rows / kCodeBlock + E); }
+
+struct CodeArgs {
+  const void* x;             // [rows,H], or [T,H] to be dispatched, or [rows,2H] gated, or the weights [E,N,H]
+  const int32_t* slot = nullptr;      // dispatch
+  const int32_t* count = nullptr;     // nullable: rows in use
+  const int32_t* offsets = nullptr;   // columns
+  int64_t T = 0, rows;
+  int K = 1, E = 1, N = 0, H, dtype;
+  uint8_t* codes;
+  uint8_t* scales;
+  uint8_t* codes_t = nullptr;
+  uint8_t* scales_t = nullptr;
+  const void* grad = nullptr;         // gated: the gradient of h
+  void* out = nullptr;                // gated: h, or the gradient of x
+};
+eqb_status launch_quantize_rows(const CodeArgs& a, hipStream_t s);
+eqb_status launch_dispatch_quantized(const CodeArgs& a, hipStream_t s);
+eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s);
+eqb_status launch_quantize_weights(const CodeArgs& a, hipStream_t s);
+eqb_status launch_gated(const CodeArgs& a, hipStream_t s);
+eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s);
+eqb_status launch_gated_backward(const CodeArgs& a, hipStream_t s);
+
+struct ProductArgs {
+  const uint8_t* x;          // codes of the rows, or of the gradient's columns
+  const uint8_t* x_scales;
+  const uint8_t* w;          // codes of the weights, or of the rows' columns
+  const uint8_t* w_scales;
+  const int32_t* offsets;
+  int64_t rows;
+  int E, N, H, dtype;
+  void* out;
+};
+eqb_status launch_experts_product(const ProductArgs& a, hipStream_t s);
+eqb_status launch_experts_grad_weight(const ProductArgs& a, hipStream_t s);
+
 // The number of steps kept on the device, and what the step at hand takes from it.
 struct AdamwCounter {
   int64_t steps;

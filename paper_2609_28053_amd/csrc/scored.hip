@@ -1,0 +1,447 @@
+// scored.hip - routing by scores (arXiv 2609.28053, Eq. 1 with the choice made on the scores
+// themselves): the experts of the largest score plus bias within the best groups, their
+// weights, and the gradient with respect to the logits.
+#include "eqb_internal.hpp"
+
+namespace eqb {
+namespace {
+
+constexpr int kPer = 8;                 // experts of a lane
+constexpr int kScoredThreads = 256, kScoredWaves = kScoredThreads / 64;
+
+template <int kDtype>
+struct Logit;
+template <>
+struct Logit<EQB_DTYPE_BF16> {
+  typedef uint16_t raw;
+  static __device__ __forceinline__ float to_f(raw x) { return __uint_as_float((uint32_t)x << 16); }
+};
+template <>
+struct Logit<EQB_DTYPE_F16> {
+  typedef _Float16 raw;
+  static __device__ __forceinline__ float to_f(raw x) { return (float)x; }
+};
+template <>
+struct Logit<EQB_DTYPE_F32> {
+  typedef float raw;
+  static __device__ __forceinline__ float to_f(raw x) { return x; }
+};
+
+// A masked logit (-inf or NaN) becomes -inf, +inf the largest finite number.
+__device__ __forceinline__ float clean(float z) {
+  const float lowest = -__builtin_inff();
+  return z > lowest ? fminf(z, 3.402823466e38f) : lowest;
+}
+
+// exp(-a), a >= 0 (infinity gives 0): 2^(-p) (1 - l ln 2) with p + l = a log2 e in two parts,
+// within 2^-22; without subnormal results.
+__device__ __forceinline__ float exp_neg(float a) {
+  const float kLog2e = 1.44269502162933349609375f, kLow = 1.92596303e-8f, kLn2 = 0.693147182f;
+  a = fminf(a, 200.0f);
+  const float p = a * kLog2e;
+  const float l = __builtin_fmaf(a, kLow, __builtin_fmaf(a, kLog2e, -p));
+  const float e = __builtin_amdgcn_exp2f(-p);
+  return __builtin_fmaf(-e * kLn2, l, e);
+}
+__device__ __forceinline__ double exp_neg(double a) { return exp(-a); }
+
+// sigmoid(z) and 1 - sigmoid(z); of -inf 0 and 1
+__device__ __forceinline__ void sigmoid_pair(float z, float& s, float& rest) {
+  const float e = exp_neg(fabsf(z)), r = newton_rcp(1.0f + e), q = e * r;
+  s = z >= 0.0f ? r : q;
+  rest = z >= 0.0f ? q : r;
+}
+__device__ __forceinline__ float sigmoid_of(float z) {
+  float s, rest;
+  sigmoid_pair(z, s, rest);
+  return s;
+}
+__device__ __forceinline__ double sigmoid_of(double z) { return 1.0 / (1.0 + exp(-z)); }
+
+template <class F>
+__device__ __forceinline__ F lowest_of() { return -(F)__builtin_inf(); }
+
+// Folds over the L lanes of a row.
+template <int L>
+__device__ __forceinline__ float row_max(float x) { return group_max<L>(x); }
+template <int L>
+__device__ __forceinline__ double row_max(double x) {
+#pragma unroll
+  for (int d = 1; d < L; d <<= 1) x = fmax(x, __shfl_xor(x, d));
+  return x;
+}
+template <int L>
+__device__ __forceinline__ float row_sum(float x) { return group_sum<L>(x); }
+template <int L>
+__device__ __forceinline__ double row_sum(double x) {
+#pragma unroll
+  for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+template <int L>
+__device__ __forceinline__ int row_min(int x) {
+  return group_fold<L>(x, [](int a, int b) { return a < b ? a : b; });
+}
+
+// The scores of a row's kPer experts of this lane in F, and what decides (-inf: masked).
+template <int L, class F>
+__device__ __forceinline__ void scores_of(const float (&z)[kPer], const float (&b)[kPer], bool softmax, F (&q)[kPer]) {
+  if (softmax) {
+    float top = z[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) top = fmaxf(top, z[i]);
+    top = row_max<L>(top);
+    if (top == -__builtin_inff()) top = 0.0f;
+    F sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      q[i] = exp_neg((F)top - (F)z[i]);
+      sum += q[i];
+    }
+    sum = row_sum<L>(sum);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) q[i] = q[i] / sum;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) q[i] = sigmoid_of((F)z[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const F v = q[i] + (F)b[i];
+    q[i] = z[i] > -__builtin_inff() && v == v ? v : lowest_of<F>();
+  }
+}
+
+// (a1, a2): the largest and the next of two such pairs
+template <class F>
+__device__ __forceinline__ void merge2(F& a1, F& a2, F b1, F b2) {
+  const F lo = fmin(a1, b1);
+  a1 = fmax(a1, b1);
+  a2 = fmax(lo, fmax(a2, b2));
+}
+
+// Every expert's group score.
+template <int L, class F>
+__device__ __forceinline__ void group_scores(const F (&q)[kPer], int each, int group_top, F (&g)[kPer]) {
+  F t1[kPer], t2[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    t1[i] = q[i];
+    t2[i] = lowest_of<F>();
+  }
+#pragma unroll
+  for (int d = 1; d < kPer; d <<= 1) {
+    if (each > d) {
+      F o1[kPer], o2[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        o1[i] = t1[i ^ d];
+        o2[i] = t2[i ^ d];
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) merge2(t1[i], t2[i], o1[i], o2[i]);
+    }
+  }
+  if (each > kPer) {
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) {
+      if (each > d * kPer) {
+        const F o1 = __shfl_xor(t1[0], d), o2 = __shfl_xor(t2[0], d);
+        merge2(t1[0], t2[0], o1, o2);
+      }
+    }
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) {
+      t1[i] = t1[0];
+      t2[i] = t2[0];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) g[i] = group_top == 2 && t2[i] > lowest_of<F>() ? t1[i] + t2[i] : t1[i];
+}
+
+// The largest of a row's values and the lowest place that has it (kNone: all -inf).
+constexpr int kNone = 1 << 20;
+template <int L, class F>
+__device__ __forceinline__ int largest(const F (&q)[kPer], int l, F& top) {
+  F m = q[0];
+#pragma unroll
+  for (int i = 1; i < kPer; ++i) m = fmax(m, q[i]);
+  top = row_max<L>(m);
+  int at = kNone;
+#pragma unroll
+  for (int i = kPer - 1; i >= 0; --i) at = q[i] == top ? l * kPer + i : at;
+  at = row_min<L>(at);
+  return top > lowest_of<F>() ? at : kNone;
+}
+
+// Two scores in binary32 nearer than this may be the other way round: a score s is within
+// 2^-19 s of its value (a softmax's sum of 256 in a tree of 8 and 5 levels is most of that), and
+// the sum with the bias is rounded once; s is at most |q| and the largest bias.
+__device__ __forceinline__ bool near(float a, float b, float most_bias) {
+  return a - b <= 0x1p-18f * (fabsf(a) + most_bias + 0x1p-40f);
+}
+__device__ __forceinline__ bool near(double, double, float) { return false; }
+
+// Chooses a row's K experts by rank into `chosen` (kNone where there are none left); whether an
+// order that matters was too near to call.  In binary32 the (K + 1)st is looked at as well.
+template <int L, class F>
+__device__ __forceinline__ bool choose(const ScoredArgs& a, const float (&z)[kPer], const float (&b)[kPer],
+                                       float most_bias, int l, int16_t* chosen) {
+  constexpr bool kQuick = sizeof(F) == 4;
+  F q[kPer];
+  scores_of<L>(z, b, a.softmax, q);
+  bool doubt = false;
+  if (a.top_groups < a.groups) {
+    const int each = a.E / a.groups;
+    F g[kPer];
+    group_scores<L>(q, each, a.group_top, g);
+    bool in[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      in[i] = false;
+      if ((l * kPer + i) & (each - 1)) g[i] = lowest_of<F>();     // the first of a group stands for it
+    }
+    F last = 0;
+    for (int k = 0; k < a.top_groups + (kQuick ? 1 : 0); ++k) {
+      F top;
+      const int at = largest<L>(g, l, top);
+      if (k == a.top_groups) {
+        doubt = doubt || (at != kNone && near(last, top, 2 * most_bias));
+      } else {
+        last = top;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int e = l * kPer + i;
+          in[i] = in[i] || (e & -each) == at;
+          if (e == at) g[i] = lowest_of<F>();
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (!in[i]) q[i] = lowest_of<F>();
+  }
+  // without a bias the scores are in the logits' order, which is exact
+  const bool by_logits = a.bias == nullptr;
+  if (by_logits) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) q[i] = q[i] > lowest_of<F>() ? (F)z[i] : lowest_of<F>();
+  }
+  F last = 0;
+  for (int k = 0; k < a.K + (kQuick && !by_logits ? 1 : 0); ++k) {
+    F top;
+    const int at = largest<L>(q, l, top);
+    if (kQuick && !by_logits && k > 0) doubt = doubt || (at != kNone && near(last, top, most_bias));
+    last = top;
+    if (k < a.K && l == 0) chosen[k] = (int16_t)(at == kNone ? -1 : at);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (l * kPer + i == at) q[i] = lowest_of<F>();
+  }
+  return doubt;
+}
+
+template <int E, int kDtype>
+__device__ __forceinline__ void load_row(const void* z, int64_t t, int l, float (&v)[kPer]) {
+  typedef typename Logit<kDtype>::raw raw;
+  typedef raw vec __attribute__((ext_vector_type(kPer)));
+  const vec x = *reinterpret_cast<const vec*>(static_cast<const raw*>(z) + t * E + l * kPer);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) v[i] = clean(Logit<kDtype>::to_f(x[i]));
+}
+
+template <int E, int kDtype>
+__global__ __launch_bounds__(kScoredThreads) void route_scored_kernel(const ScoredArgs a) {
+  constexpr int L = E / kPer, kRows = 64 / L;           // rows of a wave
+  __shared__ int16_t sh_chosen[kScoredWaves * kRows][E];
+  typedef typename Logit<kDtype>::raw raw;
+  const int lane = threadIdx.x & 63, l = lane % L;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int16_t* const chosen = sh_chosen[wave * kRows + lane / L];
+  float b[kPer];
+  float most_bias = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    b[i] = a.bias ? a.bias[l * kPer + i] : 0.0f;
+    const float m = fabsf(b[i]);
+    most_bias = fmaxf(most_bias, m < __builtin_inff() ? m : 0.0f);
+  }
+  most_bias = row_max<L>(most_bias);
+  const int64_t step = (int64_t)gridDim.x * kScoredWaves * kRows;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kScoredWaves + wave) * kRows; t0 < a.T; t0 += step) {
+    const bool live = t0 + lane / L < a.T;
+    const int64_t t = live ? t0 + lane / L : a.T - 1;
+    float z[kPer];
+    load_row<E, kDtype>(a.z, t, l, z);
+    const bool doubt = choose<L, float>(a, z, b, most_bias, l, chosen);
+    if (__ballot(doubt)) {
+      // all rows of the wave once more (the shuffles need all lanes): the same where they were right
+      choose<L, double>(a, z, b, most_bias, l, chosen);
+    }
+    lds_wave_sync();
+    // the weights, a chosen expert a lane
+    float top = 0.0f, total = 1.0f;
+    if (a.softmax) {
+      top = z[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) top = fmaxf(top, z[i]);
+      top = row_max<L>(top);
+      if (top == -__builtin_inff()) top = 0.0f;
+      total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) total += exp_neg(top - z[i]);
+      total = row_sum<L>(total);
+    }
+    const raw* row = static_cast<const raw*>(a.z) + t * E;
+    auto score = [&](int e) {
+      const float x = clean(Logit<kDtype>::to_f(row[e]));
+      return a.softmax ? exp_neg(top - x) / total : sigmoid_of(x);
+    };
+    float sum = 0.0f;
+    if (a.normalize) {
+      for (int k = l; k < a.K; k += L) sum += chosen[k] >= 0 ? score(chosen[k]) : 0.0f;
+      sum = row_sum<L>(sum);
+    }
+    if (live) {
+      for (int k = l; k < a.K; k += L) {
+        const int e = chosen[k];
+        float w = e >= 0 ? score(e) : 0.0f;
+        if (a.normalize) w = sum > 0.0f ? w / sum : 0.0f;
+        a.idx[t * a.K + k] = e;
+        a.weight[t * a.K + k] = a.scale * w;
+      }
+    }
+    lds_wave_sync();
+  }
+}
+
+template <int E, int kDtype>
+__global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(const ScoredArgs a) {
+  constexpr int L = E / kPer, kRows = 64 / L;
+  __shared__ __attribute__((aligned(16))) float sh_grad[kScoredWaves * kRows][E];
+  typedef typename Logit<kDtype>::raw raw;
+  const int lane = threadIdx.x & 63, l = lane % L;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float* const grad = sh_grad[wave * kRows + lane / L];
+  const int64_t step = (int64_t)gridDim.x * kScoredWaves * kRows;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kScoredWaves + wave) * kRows; t0 < a.T; t0 += step) {
+    const bool live = t0 + lane / L < a.T;
+    const int64_t t = live ? t0 + lane / L : a.T - 1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) grad[l * kPer + i] = 0.0f;
+    float z[kPer], top = 0.0f, total = 1.0f;
+    if (a.softmax) {
+      load_row<E, kDtype>(a.z, t, l, z);
+      top = z[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) top = fmaxf(top, z[i]);
+      top = row_max<L>(top);
+      if (top == -__builtin_inff()) top = 0.0f;
+      total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        z[i] = exp_neg(top - z[i]);
+        total += z[i];
+      }
+      total = row_sum<L>(total);
+    }
+    const raw* row = static_cast<const raw*>(a.z) + t * E;
+    const int32_t* idx = a.idx + t * a.K;
+    const float* gw = a.grad_weight + t * a.K;
+    auto score = [&](int e, float& s, float& rest) {
+      const float x = clean(Logit<kDtype>::to_f(row[e]));
+      if (a.softmax) {
+        s = total > 0.0f ? exp_neg(top - x) / total : 0.0f;
+        rest = 1.0f;
+      } else {
+        sigmoid_pair(x, s, rest);
+      }
+    };
+    // S = sum of the chosen scores and the sum of g s
+    float S = 0.0f, gs = 0.0f;
+    for (int k = l; k < a.K; k += L) {
+      const int e = idx[k];
+      if (e < 0 || e >= E) continue;
+      float s, rest;
+      score(e, s, rest);
+      S += s;
+      gs += gw[k] * s;
+    }
+    S = row_sum<L>(S);
+    gs = row_sum<L>(gs);
+    const float inv = a.normalize ? (S > 0.0f ? 1.0f / S : 0.0f) : 1.0f, mean = a.normalize ? gs * inv : 0.0f;
+    lds_wave_sync();
+    // entry by entry, so that an expert that a row names twice gets both in their order
+    for (int k0 = 0; k0 < a.K; k0 += L) {
+      const int k = k0 + l;
+      int e = -1;
+      float v = 0.0f;
+      if (k < a.K) {
+        e = idx[k];
+        if (e >= 0 && e < E) {
+          float s, rest;
+          score(e, s, rest);
+          v = a.scale * ((gw[k] - mean) * inv) * s * rest;
+        }
+      }
+      for (int j = 0; j < L && k0 + j < a.K; ++j) {
+        if (l == j && e >= 0 && e < E) grad[e] += v;
+        lds_wave_sync();
+      }
+    }
+    float out[kPer];
+    float back = 0.0f;
+    // a softmax of weights that are not normalized: every expert lowers the others
+    if (a.softmax && !a.normalize) back = total > 0.0f ? a.scale * gs / total : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      out[i] = grad[l * kPer + i];
+      if (a.softmax && !a.normalize) out[i] -= back * z[i];
+    }
+    if (live) {
+      float4* to = reinterpret_cast<float4*>(a.grad_z + t * E + l * kPer);
+      to[0] = make_float4(out[0], out[1], out[2], out[3]);
+      to[1] = make_float4(out[4], out[5], out[6], out[7]);
+    }
+    lds_wave_sync();
+  }
+}
+
+template <int E, int kDtype>
+eqb_status launch_scored_e(const ScoredArgs& a, bool backward, hipStream_t s) {
+  constexpr int kRows = 64 / (E / kPer) * kScoredWaves;
+  int64_t blocks = (a.T + kRows - 1) / kRows, most = (int64_t)num_cus() * 8;
+  const int cap = max_blocks_cap();
+  if (cap > 0 && cap < most) most = cap;
+  if (blocks > most) blocks = most;
+  if (backward) route_scored_backward_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  else route_scored_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  return launch_status();
+}
+
+template <int kDtype>
+eqb_status launch_scored_d(const ScoredArgs& a, bool backward, hipStream_t s) {
+  switch (a.E) {
+    case 8: return launch_scored_e<8, kDtype>(a, backward, s);
+    case 16: return launch_scored_e<16, kDtype>(a, backward, s);
+    case 32: return launch_scored_e<32, kDtype>(a, backward, s);
+    case 64: return launch_scored_e<64, kDtype>(a, backward, s);
+    case 128: return launch_scored_e<128, kDtype>(a, backward, s);
+    case 256: return launch_scored_e<256, kDtype>(a, backward, s);
+    default: return EQB_ERR_UNSUPPORTED;
+  }
+}
+
+eqb_status launch_scored(const ScoredArgs& a, bool backward, hipStream_t s) {
+  if (a.dtype == EQB_DTYPE_BF16) return launch_scored_d<EQB_DTYPE_BF16>(a, backward, s);
+  if (a.dtype == EQB_DTYPE_F16) return launch_scored_d<EQB_DTYPE_F16>(a, backward, s);
+  return launch_scored_d<EQB_DTYPE_F32>(a, backward, s);
+}
+
+}  // namespace
+
+eqb_status launch_route_scored(const ScoredArgs& a, hipStream_t s) { return launch_scored(a, false, s); }
+eqb_status launch_route_scored_backward(const ScoredArgs& a, hipStream_t s) { return launch_scored(a, true, s); }
+
+}  // namespace eqb

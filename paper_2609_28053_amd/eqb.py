@@ -40,6 +40,7 @@ EQB_SCORE_SIGMOID = 0
 EQB_SCORE_SOFTMAX = 1
 EQB_ADAMW_BLOCK = 256
 EQB_ADAMW_COUNTER_BYTES = 64
+EQB_CODE_BLOCK = 128
 
 EXPORTS = (
     "eqb_route_topk",
@@ -70,6 +71,20 @@ EXPORTS = (
     "eqb_combine_backward",
     "eqb_adamw_step",
     "eqb_adamw_step_counted",
+    "eqb_route_scored",
+    "eqb_route_scored_backward",
+    "eqb_code_width",
+    "eqb_scale_width",
+    "eqb_column_width",
+    "eqb_quantize_rows",
+    "eqb_dispatch_quantized",
+    "eqb_quantize_columns",
+    "eqb_quantize_weights",
+    "eqb_experts_product",
+    "eqb_experts_grad_weight",
+    "eqb_gated",
+    "eqb_gated_quantize",
+    "eqb_gated_backward",
     "eqb_set_max_blocks",
     "eqb_get_max_blocks",
     "eqb_rank",
@@ -115,6 +130,20 @@ def _load():
         "eqb_combine_backward": [P, P, P, P, i64, i32, i64, i32, i32, P, P, P],
         "eqb_adamw_step": [P, i32, i32, i32, i64] + [ctypes.c_double] * 4 + [ctypes.c_uint64, P, P, P],
         "eqb_adamw_step_counted": [P, i32, i32, i32, P] + [ctypes.c_double] * 4 + [ctypes.c_uint64, P, P, P],
+        "eqb_route_scored": [P, P, i64, i32, i32, i32, i32, i32, i32, i32, ctypes.c_double, i32, P, P, P],
+        "eqb_route_scored_backward": [P, P, P, i64, i32, i32, i32, i32, ctypes.c_double, i32, P, P],
+        "eqb_code_width": [i64],
+        "eqb_scale_width": [i64],
+        "eqb_column_width": [i64, i32],
+        "eqb_quantize_rows": [P, P, i64, i32, i32, P, P, P],
+        "eqb_dispatch_quantized": [P, P, i64, i32, i64, i32, i32, P, P, P],
+        "eqb_quantize_columns": [P, P, i64, i32, i32, i32, P, P, P],
+        "eqb_quantize_weights": [P, i32, i32, i32, i32, P, P, P, P, P],
+        "eqb_experts_product": [P, P, P, P, P, i64, i32, i32, i32, i32, P, P],
+        "eqb_experts_grad_weight": [P, P, P, P, P, i64, i32, i32, i32, i32, P, P],
+        "eqb_gated": [P, P, i64, i32, i32, P, P],
+        "eqb_gated_quantize": [P, P, i64, i32, i32, P, P, P],
+        "eqb_gated_backward": [P, P, P, i64, i32, i32, P, P],
         "eqb_set_max_blocks": [i32],
         "eqb_get_max_blocks": [],
         "eqb_rank": [i64, i32, i32],
@@ -125,6 +154,9 @@ def _load():
         fn.argtypes = args
         fn.restype = i32
     lib.eqb_rank.restype = i64
+    lib.eqb_code_width.restype = i64
+    lib.eqb_scale_width.restype = i64
+    lib.eqb_column_width.restype = i64
     lib.eqb_layer_workspace_size.restype = ctypes.c_size_t
     lib.eqb_layer_workspace_zero_bytes.restype = ctypes.c_size_t
     lib.eqb_balance_workspace_size.restype = ctypes.c_size_t
@@ -628,6 +660,147 @@ def eqb_adamw_step_counted(tensors: AdamwTensors, counter, lr, beta1=0.9, beta2=
         _ptr(counter, torch.int64, EQB_ADAMW_COUNTER_BYTES // 8, "counter"), float(lr), float(beta1), float(beta2),
         float(eps), int(seed) & (2**64 - 1), _ptr(grad_scale, torch.float32, 1, "grad_scale"),
         _ptr(found_inf, torch.float32, 1, "found_inf"), _stream(stream)))
+
+
+_LOGITS = {**_ROW_TYPES, **{t: EQB_DTYPE_BF16 for t in _Z}}
+
+
+def _logit_type(z):
+    if z.dtype not in _LOGITS:
+        raise TypeError(f"z has dtype {z.dtype}, expected one of {tuple(_LOGITS)}")
+    return _LOGITS[z.dtype]
+
+
+def eqb_route_scored(z, bias, K, topk_idx, topk_weight, score=EQB_SCORE_SIGMOID, groups=1, top_groups=1, group_top=1,
+                     normalize=True, scale=1.0, stream=None):
+    """The K experts of the largest score plus bias in each row of z [T,E] (binary32, float16, or BF16, also as bit
+    patterns), within the top_groups best of the groups of neighbouring experts, and their weights: scale times the
+    score, over the chosen scores' sum with normalize.  Entries that masks (logits of -inf) leave over are expert -1
+    of weight 0."""
+    T, E = z.shape
+    _check("eqb_route_scored", lib.eqb_route_scored(
+        _ptr(z, name="z"), _ptr(bias, torch.float32, E, "bias"), T, E, K, groups, top_groups, group_top, score,
+        int(bool(normalize)), float(scale), _logit_type(z), _ptr(topk_idx, torch.int32, T * K, "topk_idx"),
+        _ptr(topk_weight, torch.float32, T * K, "topk_weight"), _stream(stream)))
+
+
+def eqb_route_scored_backward(z, topk_idx, grad_weight, grad_z, score=EQB_SCORE_SIGMOID, normalize=True, scale=1.0,
+                              stream=None):
+    """The gradient of eqb_route_scored's weights with respect to z (grad_z [T,E] binary32), the choice held fixed."""
+    (T, E), K = z.shape, topk_idx.shape[1]
+    _check("eqb_route_scored_backward", lib.eqb_route_scored_backward(
+        _ptr(z, name="z"), _ptr(topk_idx, torch.int32, T * K, "topk_idx"),
+        _ptr(grad_weight, torch.float32, T * K, "grad_weight"), T, E, K, score, int(bool(normalize)), float(scale),
+        _logit_type(z), _ptr(grad_z, torch.float32, T * E, "grad_z"), _stream(stream)))
+
+
+def eqb_code_width(hidden: int) -> int:
+    """Codes of a row: hidden rounded up to whole blocks."""
+    return (hidden + 127) // 128 * 128 if hidden > 0 else 0
+
+
+def eqb_scale_width(hidden: int) -> int:
+    """Scale bytes of a row: one per block, rounded up to a multiple of 4."""
+    return (hidden + 511) // 512 * 4 if hidden > 0 else 0
+
+
+def eqb_column_width(rows: int, E: int) -> int:
+    """Columns of eqb_quantize_columns: the rows, each expert's on whole blocks."""
+    return 128 * (rows // 128 + E) if rows >= 0 and 1 <= E <= 256 else 0
+
+
+_CODES, _SCALES = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _coded(codes, scales, lead, hidden, name, scale_lead=None):
+    """Pointers of the codes and scales of rows of `hidden` elements."""
+    for t, shape, what in ((codes, (*lead, (hidden + 127) // 128 * 128), "codes"),
+                           (scales, (*(scale_lead or lead), (hidden + 511) // 512 * 4), "scales")):
+        if t is not None and getattr(t, "shape", None) != shape:
+            raise ValueError(f"{name}{what} has shape {tuple(getattr(t, 'shape', ()))}, expected {shape}")
+    return _ptr(codes, _CODES, None, name + "codes"), _ptr(scales, _SCALES, None, name + "scales")
+
+
+def eqb_quantize_rows(x, codes, scales, count=None, stream=None):
+    """Rows x [R,H] as E4M3 codes [R, eqb_code_width(H)] with a power of two for each block of 128 (scales [R,
+    eqb_scale_width(H)]); with count (one int32 on the device) only the first rows."""
+    R, H = x.shape
+    _check("eqb_quantize_rows", lib.eqb_quantize_rows(
+        _ptr(x, name="x"), _ptr(count, torch.int32, 1, "count"), R, H, _row_type(x, "x"),
+        *_coded(codes, scales, (R,), H, ""), _stream(stream)))
+
+
+def eqb_dispatch_quantized(x, slot, codes, scales, stream=None):
+    """eqb_dispatch of the rows x [T,H] as codes: row slot[t, k] takes x[t]."""
+    (T, H), K, R = x.shape, slot.shape[1], codes.shape[0]
+    _check("eqb_dispatch_quantized", lib.eqb_dispatch_quantized(
+        _ptr(x, name="x"), _ptr(slot, torch.int32, T * K, "slot"), T, K, R, H, _row_type(x, "x"),
+        *_coded(codes, scales, (R,), H, ""), _stream(stream)))
+
+
+def eqb_quantize_columns(x, offsets, codes, scales, stream=None):
+    """Columns of x [R,H] in blocks of 128 rows of one expert: codes [H, eqb_column_width(R, E)] and their scales, what
+    eqb_experts_grad_weight contracts over."""
+    (R, H), E = x.shape, offsets.numel() - 1
+    _check("eqb_quantize_columns", lib.eqb_quantize_columns(
+        _ptr(x, name="x"), _ptr(offsets, torch.int32, E + 1, "offsets"), R, E, H, _row_type(x, "x"),
+        *_coded(codes, scales, (H,), eqb_column_width(R, E), ""), _stream(stream)))
+
+
+def eqb_quantize_weights(w, codes=None, scales=None, codes_t=None, scales_t=None, stream=None):
+    """The experts' weights w [E,N,H] as codes with a power of two for each 128 x 128 (codes [E,N,.], scales [E,
+    ceil(N/128),.]), and as the transposed codes_t [E,H,.], scales_t [E,ceil(H/128),.]; either pair may be left out."""
+    E, N, H = w.shape
+    up = lambda n: -(-n // EQB_CODE_BLOCK)  # noqa: E731
+    _check("eqb_quantize_weights", lib.eqb_quantize_weights(
+        _ptr(w, name="w"), E, N, H, _row_type(w, "w"), *_coded(codes, scales, (E, N), H, "", (E, up(N))),
+        *_coded(codes_t, scales_t, (E, H), N, "transposed ", (E, up(H))), _stream(stream)))
+
+
+def eqb_experts_product(codes, scales, w_codes, w_scales, offsets, out, stream=None):
+    """out[r] = x[r] w[e]^T [R,N] for the rows of each expert, from the codes of x [R,H] and of w [E,N,H]."""
+    (R, N), E, H = out.shape, w_codes.shape[0], codes.shape[1]
+    _check("eqb_experts_product", lib.eqb_experts_product(
+        *_coded(codes, scales, (R,), H, ""), *_coded(w_codes, w_scales, (E, N), H, "weights' ", (E, -(-N // EQB_CODE_BLOCK))),
+        _ptr(offsets, torch.int32, E + 1, "offsets"), R, E, N, H, _row_type(out, "out"), _ptr(out, name="out"),
+        _stream(stream)))
+
+
+def eqb_experts_grad_weight(grad_codes, grad_scales, codes, scales, offsets, out, stream=None):
+    """out[e] = grad[rows of e]^T x[rows of e] [E,N,H], from the columns' codes of grad [R,N] and of x [R,H]."""
+    E, N, H = out.shape
+    W = codes.shape[1]
+    rows = W - E * EQB_CODE_BLOCK        # what the width leaves of them: a whole number of blocks
+    _check("eqb_experts_grad_weight", lib.eqb_experts_grad_weight(
+        *_coded(grad_codes, grad_scales, (N,), W, "gradient's "), *_coded(codes, scales, (H,), W, ""),
+        _ptr(offsets, torch.int32, E + 1, "offsets"), rows + EQB_CODE_BLOCK - 1, E, N, H, _row_type(out, "out"),
+        _ptr(out, name="out"), _stream(stream)))
+
+
+def eqb_gated(x, h, count=None, stream=None):
+    """h = g sigmoid(g) u [R,H] of the rows x = (g, u) [R,2H]."""
+    R, H = h.shape
+    _check("eqb_gated", lib.eqb_gated(
+        _ptr(x, h.dtype, 2 * R * H, "x"), _ptr(count, torch.int32, 1, "count"), R, H, _row_type(h, "h"),
+        _ptr(h, name="h"), _stream(stream)))
+
+
+def eqb_gated_quantize(x, codes, scales, count=None, stream=None):
+    """The same as codes: what the second product takes."""
+    R, H = x.shape[0], x.shape[1] // 2
+    if x.shape[1] % 2:
+        raise ValueError("x holds gate and u in rows of an even number of elements")
+    _check("eqb_gated_quantize", lib.eqb_gated_quantize(
+        _ptr(x, name="x"), _ptr(count, torch.int32, 1, "count"), R, H, _row_type(x, "x"),
+        *_coded(codes, scales, (R,), H, ""), _stream(stream)))
+
+
+def eqb_gated_backward(grad_h, x, grad_x, count=None, stream=None):
+    """The gradient of eqb_gated with respect to x [R,2H] from grad_h [R,H]."""
+    R, H = grad_h.shape
+    _check("eqb_gated_backward", lib.eqb_gated_backward(
+        _ptr(grad_h, name="grad_h"), _ptr(x, grad_h.dtype, 2 * R * H, "x"), _ptr(count, torch.int32, 1, "count"), R, H,
+        _row_type(grad_h, "grad_h"), _ptr(grad_x, grad_h.dtype, 2 * R * H, "grad_x"), _stream(stream)))
 
 
 def eqb_set_max_blocks(max_blocks: int) -> None:
