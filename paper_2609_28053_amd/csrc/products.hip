@@ -22,7 +22,6 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 typedef __attribute__((address_space(3))) uint32_t lds_word;
-typedef const __attribute__((address_space(1))) uint32_t global_word;
 
 template <int kDtype>
 struct OutType;
@@ -42,55 +41,51 @@ struct OutType<EQB_DTYPE_F16> {
   static __device__ __forceinline__ raw from_f(float x) { return (raw)x; }
 };
 
-// Tiles of an expert's rows, found from the offsets alone: lane l of every wave holds the
-// experts 4l .. 4l + 3 and how many tiles come before them.
+// The experts' rows in LDS, and how many tiles of rows come before every fourth expert.
 struct Experts {
-  int begin[4], count[4], tiles[4], before;
-  int total;
-  __device__ __forceinline__ Experts(const int32_t* offsets, int E, int64_t rows, int BP) {
+  int2 rows[kMostExperts];        // first row, and how many
+  int before[kMostExperts / 4], total;
+
+  // By every wave of the block; lane l takes the experts 4l .. 4l + 3.
+  __device__ __forceinline__ void fill(const int32_t* offsets, int E, int64_t most, int BP) {
     const int lane = threadIdx.x & 63;
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int e = lane * 4 + i;
       int64_t a = e < E ? offsets[e] : 0, b = e < E ? offsets[e + 1] : 0;
-      a = a < 0 ? 0 : a > rows ? rows : a;
-      b = b > rows ? rows : b;
-      begin[i] = (int)a;
-      count[i] = b > a ? (int)(b - a) : 0;
-      tiles[i] = (count[i] + BP - 1) / BP;
-      sum += tiles[i];
+      a = a < 0 ? 0 : a > most ? most : a;
+      b = b > most ? most : b;
+      const int n = b > a ? (int)(b - a) : 0;
+      rows[e] = make_int2((int)a, n);
+      sum += (n + BP - 1) / BP;
     }
     int incl = sum;
     for (int d = 1; d < 64; d <<= 1) {
       const int y = __shfl_up(incl, d);
       if (lane >= d) incl += y;
     }
-    before = incl - sum;
-    total = __builtin_amdgcn_readlane(incl, 63);
+    before[lane] = incl - sum;
+    if (lane == 63) total = incl;
+  }
+  __device__ __forceinline__ int2 of(int e) const {
+    const int2 r = rows[e];
+    return make_int2(__builtin_amdgcn_readfirstlane(r.x), __builtin_amdgcn_readfirstlane(r.y));
   }
   // Expert and first row of row tile t < total; n: the expert's rows from there on.
   __device__ __forceinline__ void find(int t, int BP, int& e, int64_t& first, int& n) const {
-    const int l = __popcll(__ballot(before <= t)) - 1;
-    int left = t - __builtin_amdgcn_readlane(before, l);
+    const int l = __popcll(__ballot(before[threadIdx.x & 63] <= t)) - 1;
+    int left = t - __builtin_amdgcn_readfirstlane(before[l]);
     e = l * 4;
-    int b = 0, c = 0;
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int m = __builtin_amdgcn_readlane(tiles[i], l);
-      const int bi = __builtin_amdgcn_readlane(begin[i], l), ci = __builtin_amdgcn_readlane(count[i], l);
-      if (!found && left < m) {
-        found = true;
-        e = l * 4 + i;
-        b = bi;
-        c = ci;
-      } else if (!found) {
-        left -= m;
-      }
+    int2 r = of(e);
+    for (int i = 0; i < 3; ++i) {
+      const int m = (r.y + BP - 1) / BP;
+      if (left < m) break;
+      left -= m;
+      r = of(++e);
     }
-    first = (int64_t)b + (int64_t)left * BP;
-    n = c - left * BP;
+    first = (int64_t)r.x + (int64_t)left * BP;
+    n = r.y - left * BP;
   }
 };
 
@@ -105,193 +100,395 @@ __device__ __forceinline__ bf16x8_t widen(const int8v& code, int j, float scale)
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// BP x BQ of out per block of WP x WQ waves.
+// Waits for this wave's loads, stores and LDS reads, then for the block's other waves.
+__device__ __forceinline__ void step_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Memory to LDS: 16 (4) bytes a lane from base + off to to + 16 (4) lane.  Written out, since
+// the compiler would wait for all of them before any LDS read: step_barrier waits for them.
+__device__ __forceinline__ void copy16(uint8_t* to, const uint8_t* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(lds_word*)to), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t* to, const uint8_t* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"((uint32_t)(uintptr_t)(lds_word*)to), "v"(off), "s"(base)
+               : "memory");
+}
+
+// What a tile of out is computed from.
+struct Tile {
+  int64_t row;             // first row of out
+  int col, np, nq;         // first column, rows and columns that exist
+  int block, end;          // the blocks of codes to contract over
+  const uint8_t *p, *q, *ps, *qs;      // the first row's first code and scale (of block 0)
+};
+
+// BP x BQ of out per block of WP x WQ waves.  Blocks are as many as run at once and go from
+// tile to tile, and the steps of all their tiles (128 of k each) are one sequence: codes and
+// scales go from memory to LDS directly, two steps ahead.  A wave reads a step's fragments in
+// this order: first the columns and the first rows, while the matrix instructions of the last
+// kTail rows of the step before run; then the other rows, each ahead of its instructions.  When
+// it has the last of them its buffer is free for the step after the next: that is the barrier.
 template <int BP, int BQ, int WP, int WQ, bool kGrad, int kDtype>
-__global__ __launch_bounds__(64 * WP * WQ) void product_kernel(const ProductArgs a) {
-  constexpr int kWaves = WP * WQ, TP = BP / WP / 16, TQ = BQ / WQ / 16;
-  constexpr int kLoads = (BP + BQ) / 8 / kWaves;      // a wave's loads of 8 rows per step
+__global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductArgs a) {
   typedef OutType<kDtype> O;
+  typedef typename O::raw raw;
+  constexpr bool kWide = kDtype == EQB_DTYPE_F32;     // by BF16
+  constexpr int kWaves = WP * WQ, TP = BP / WP / 16, TQ = BQ / WQ / 16;
+  constexpr int kTail = kWide ? TP : TP >= 4 ? 2 : 1;
+  constexpr int kAhead = TP >= 8 ? 2 : 1;      // rows whose fragments are read before they are needed
+  constexpr bool kOneScale = !kGrad;     // a wave's columns lie in one block of the weights
+  static_assert(kGrad || kCodeBlock % (TQ * 16) == 0, "they do");
+  constexpr int kLoadsP = BP / 8 / kWaves, kLoadsQ = BQ / 8 / kWaves;      // a wave's loads of 8 rows per step
+  // A lane gets four neighbouring columns of out from a matrix instruction.  With results of 16
+  // bits, two instructions' columns are interleaved in fours, so that it has eight: 16 bytes.
+  constexpr int kPair = sizeof(raw) == 2 ? 2 : 1;
+  static_assert(TQ % kPair == 0 && kLoadsP > 0 && kLoadsQ > 0 && TP >= kTail, "whole loads and stores");
   __shared__ __attribute__((aligned(16))) uint8_t sh[2][(BP + BQ) * kStep];
+  __shared__ __attribute__((aligned(16))) uint32_t sh_scale[2][BP + BQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wp = wave / WQ, wq = wave % WQ;
-  const int lrow = lane & 15, quarter = lane >> 4;
+  const int wp = wave / WQ, wq = wave % WQ, lrow = lane & 15, quarter = lane >> 4;
   const int64_t W = kGrad ? column_width(a.rows, a.E) : code_width(a.H);
-  const int64_t SW = scale_width(W);
+  const int SW = (int)scale_width(W);
   const int q_tiles = ((kGrad ? a.H : a.N) + BQ - 1) / BQ;
   const int p_tiles = kGrad ? (a.N + BP - 1) / BP : 0;
-  const Experts experts(a.offsets, a.E, a.rows, kGrad ? 1 : BP);
-  const int64_t tiles = kGrad ? (int64_t)a.E * p_tiles * q_tiles : (int64_t)experts.total * q_tiles;
+  __shared__ __attribute__((aligned(16))) Experts experts;
+  experts.fill(a.offsets, a.E, a.rows, BP);
+  __syncthreads();
+  const uint32_t tiles = (uint32_t)((kGrad ? a.E * p_tiles : __builtin_amdgcn_readfirstlane(experts.total)) * q_tiles);
 
-  for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
-    const int qt = (int)(id % q_tiles);
-    const int64_t pt = id / q_tiles;
-    int64_t p0;              // row of out
-    int np, nq, steps, e;
-    const uint8_t *p, *q, *ps, *qs;
-    const int q0 = qt * BQ;
+  auto tile_of = [&](uint32_t id) {
+    Tile t;
+    const uint32_t pt = id / (uint32_t)q_tiles;
+    t.col = (int)(id - pt * q_tiles) * BQ;
     if (kGrad) {
-      e = (int)(pt / p_tiles);
-      p0 = pt % p_tiles * BP;
-      np = a.N - (int)p0;
-      nq = a.H - q0;
-      const int l = e >> 2;
-      int begin = 0, count = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int b = __builtin_amdgcn_readlane(experts.begin[i], l), c = __builtin_amdgcn_readlane(experts.count[i], l);
-        if ((e & 3) == i) {
-          begin = b;
-          count = c;
-        }
-      }
-      const int64_t block = begin / kCodeBlock + e;
-      steps = (count + kCodeBlock - 1) / kCodeBlock;
-      p = a.x + p0 * W + block * kStep;
-      ps = a.x_scales + p0 * SW + block;
-      q = a.w + (int64_t)q0 * W + block * kStep;
-      qs = a.w_scales + (int64_t)q0 * SW + block;
+      const int e = (int)(pt / (uint32_t)p_tiles), p0 = ((int)pt - e * p_tiles) * BP;
+      t.row = (int64_t)e * a.N + p0;
+      t.np = a.N - p0;
+      t.nq = a.H - t.col;
+      const int2 r = experts.of(e);
+      t.block = r.x / kCodeBlock + e;
+      t.end = t.block + (r.y + kCodeBlock - 1) / kCodeBlock;
+      t.p = a.x + p0 * W;
+      t.ps = a.x_scales + (int64_t)p0 * SW;
+      t.q = a.w + t.col * W;
+      t.qs = a.w_scales + (int64_t)t.col * SW;
     } else {
-      experts.find((int)pt, BP, e, p0, np);
-      nq = a.N - q0;
-      steps = (int)(W / kStep);
-      p = a.x + p0 * W;
-      ps = a.x_scales + p0 * SW;
-      q = a.w + ((int64_t)e * a.N + q0) * W;
-      qs = a.w_scales + ((int64_t)e * ((a.N + kCodeBlock - 1) / kCodeBlock) + q0 / kCodeBlock) * SW;
+      int e;
+      experts.find((int)pt, BP, e, t.row, t.np);
+      t.nq = a.N - t.col;
+      t.block = 0;
+      t.end = (int)(W / kStep);
+      t.p = a.x + t.row * W;
+      t.ps = a.x_scales + t.row * SW;
+      t.q = a.w + ((int64_t)e * a.N + t.col) * W;
+      t.qs = a.w_scales + ((int64_t)e * ((a.N + kCodeBlock - 1) / kCodeBlock) + t.col / kCodeBlock) * SW;
     }
-    np = np < BP ? np : BP;
-    nq = nq < BQ ? nq : BQ;
+    t.np = t.np < BP ? t.np : BP;
+    t.nq = t.nq < BQ ? t.nq : BQ;
+    return t;
+  };
 
-    // this lane's place in each of the wave's loads: row, and the 16 bytes that its place in
-    // LDS is for (the pieces of a row are permuted by the row's number, so that lanes that
-    // read the same piece of neighbouring rows use different banks)
-    const uint8_t* from[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int r = (wave * kLoads + i) * 8 + (lane >> 3);
-      const int piece = (lane & 7) ^ (r & 7);
-      const bool is_p = r < BP;
-      r = is_p ? r : r - BP;
-      const int most = (is_p ? np : nq) - 1;
-      r = r < most ? r : most;
-      from[i] = (is_p ? p : q) + r * W + piece * 16;
-    }
-    auto load = [&](int step) {
+  // Column of row r of Q in LDS, within its tile: row 16 j + m of a pair's 32 is column
+  // 8 (m / 4) + 4 j + m % 4.
+  auto column_of = [](int r) { return kPair == 2 ? (r & ~31) + (r >> 2 & 3) * 8 + (r >> 4 & 1) * 4 + (r & 3) : r; };
+
+  // ---- the loads: a sequence of steps over this block's tiles
+  const uint32_t eighth = gridDim.x / 8;
+  const uint32_t first_id = blockIdx.x < eighth * 8 ? (blockIdx.x % 8) * eighth + blockIdx.x / 8 : blockIdx.x;
+  // A load takes 8 rows (64 of scales).  A lane's place in each load is found once a tile, as an
+  // offset from the tile's first row: its row, and the 16 bytes that its place in LDS is for.  The
+  // pieces of a row are permuted by half the row's number, so that lanes that read the same piece
+  // of neighbouring rows use different banks.  Rows behind the last are the last once more.
+  constexpr int kLoads = kLoadsP + kLoadsQ, kScaleLoads = ((BP + BQ) / 64 + kWaves - 1) / kWaves;
+  static_assert(BP % 64 == 0 && BQ % 64 == 0, "whole loads of scales");
+  uint32_t load_id = first_id, off[kLoads], scale_off[kScaleLoads];
+  const uint8_t *from_p = nullptr, *from_q = nullptr, *from_ps = nullptr, *from_qs = nullptr;
+  int from_block = 0, from_end = 0, from_word = 0;
+  int buffer = 0;                     // where the next step's codes and scales go
+  // Goes on to the next step; behind the last one it stays, and what is loaded again is not used.
+  auto aim = [&]() {
+    while (from_block == from_end && load_id < tiles) {
+      const Tile t = tile_of(load_id);
+      load_id += gridDim.x;
+      from_block = t.block;
+      from_end = t.end;
+      if (t.block == t.end) continue;
+      from_p = t.p + (int64_t)t.block * kStep - kStep;
+      from_q = t.q + (int64_t)t.block * kStep - kStep;
+      from_ps = t.ps;
+      from_qs = t.qs;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        __builtin_amdgcn_global_load_lds((global_word*)(from[i] + (int64_t)step * kStep),
-                                         (lds_word*)(&sh[step & 1][(wave * kLoads + i) * 8 * kStep]), 16, 0, 0);
+        const bool is_p = i < kLoadsP;
+        const int group = is_p ? wave * kLoadsP + i : wave * kLoadsQ + i - kLoadsP, most = (is_p ? t.np : t.nq) - 1;
+        const int to = group * 8 + (lane >> 3);
+        const int r = is_p ? to : column_of(to);
+        off[i] = (uint32_t)(r < most ? r : most) * (uint32_t)W + (((lane & 7) ^ (to >> 1 & 7)) * 16);
       }
-    };
-    // the scales of this lane's rows
-    const uint8_t *p_scale[TP], *q_scale[TQ];
 #pragma unroll
-    for (int i = 0; i < TP; ++i) {
-      int r = (wp * TP + i) * 16 + lrow;
-      r = r < np ? r : np - 1;
-      p_scale[i] = ps + r * SW;
+      for (int k = 0; k < kScaleLoads; ++k) {
+        const int i = k * kWaves + wave;
+        const bool is_p = i * 64 < BP;
+        const int r = (is_p ? i * 64 : i * 64 - BP) + lane, most = (is_p ? t.np : t.nq) - 1;
+        const int at = r < most ? r : most;
+        scale_off[k] = (uint32_t)(kGrad || is_p ? at : at / kCodeBlock) * (uint32_t)SW;
+      }
     }
+    if (from_block < from_end) {
+      from_p += kStep;
+      from_q += kStep;
+      from_word = from_block & ~3;
+      ++from_block;
+    }
+  };
+  // the words with the step's scales (and those of its neighbours)
+  auto load_scales = [&]() {
 #pragma unroll
-    for (int i = 0; i < TQ; ++i) {
-      int r = (wq * TQ + i) * 16 + lrow;
-      r = r < nq ? r : nq - 1;
-      q_scale[i] = kGrad ? qs + r * SW : qs + r / kCodeBlock * SW;
+    for (int k = 0; k < kScaleLoads; ++k) {
+      const int i = k * kWaves + wave;
+      if ((BP + BQ) / 64 % kWaves != 0 && i >= (BP + BQ) / 64) break;
+      copy4(&sh_scale[buffer][i * 64], (i * 64 < BP ? from_ps : from_qs) + from_word, scale_off[k]);
     }
+  };
+  // the i-th of a wave's loads of codes
+  auto load_codes = [&](int i) {
+    const bool is_p = i < kLoadsP;
+    const int group = is_p ? wave * kLoadsP + i : BP / 8 + wave * kLoadsQ + i - kLoadsP;
+    copy16(sh[buffer] + group * 8 * kStep, is_p ? from_p : from_q, off[i]);
+  };
 
-    float4v acc[TP][TQ];
+  // ---- the fragments
+  const uint8_t* codes = sh[0];            // of the step that they are read from
+  const uint8_t* scales = nullptr;
+  int8v fp[TP], fq[TQ];
+  int sp[TP], sq[kOneScale ? 1 : TQ];
+  // rows 16 i + lrow: the permutation of the pieces is the same for all i
+  const int piece0 = lrow * kStep + ((quarter * 2) ^ (lrow >> 1)) * 16, piece1 = lrow * kStep + ((quarter * 2 + 1) ^ (lrow >> 1)) * 16;
+  auto fragment = [&](int base, int i) {
+    const uint8_t* at = codes + base * kStep + i * 16 * kStep;
+    return __builtin_shufflevector(*reinterpret_cast<const int4v*>(at + piece0), *reinterpret_cast<const int4v*>(at + piece1),
+                                   0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read_p = [&](int i) {
+    fp[i] = fragment(wp * TP * 16, i);
+    sp[i] = scales[(wp * TP * 16 + lrow) * 4 + i * 64];
+  };
+  auto read_q = [&](int j) {
+    fq[j] = fragment(BP + wq * TQ * 16, j);
+    if (!kOneScale || j == TQ - 1) sq[kOneScale ? 0 : j] = scales[(BP + wq * TQ * 16 + column_of(lrow)) * 4 + column_of(j * 16) * 4];
+  };
+  float4v acc[TP][TQ];
+  auto multiply = [&](int i, int j) {
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fq[j], fp[i], acc[i][j], 0, 0, 0, sq[kOneScale ? 0 : j], 0, sp[i]);
+  };
+
+  if (first_id >= tiles) return;
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    aim();
+    if (from_p == nullptr) break;        // no tile has steps
+    load_scales();
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_codes(i);
+    buffer ^= 1;
+  }
+  step_barrier();
+  int read_buffer = 0;     // of the next step to be read
+  auto next_step = [&](int block) {
+    codes = sh[read_buffer];
+    scales = reinterpret_cast<const uint8_t*>(sh_scale[read_buffer]) + (block & 3);
+    read_buffer ^= 1;
+  };
+
+  uint32_t id = first_id;
+  Tile t = tile_of(id);
+  bool ready = false;      // whether the tile's first fragments are read (or being read)
+  while (true) {
 #pragma unroll
     for (int i = 0; i < TP; ++i)
 #pragma unroll
       for (int j = 0; j < TQ; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-
-    __syncthreads();       // the last tile's reads of LDS are done
-    if (steps > 0) load(0);
-    for (int step = 0; step < steps; ++step) {
-      int sp[TP], sq[TQ];
+    const uint32_t next_id = id + gridDim.x;
+    if (t.block < t.end && !ready) {
+      next_step(t.block);
 #pragma unroll
-      for (int i = 0; i < TP; ++i) sp[i] = p_scale[i][step];
+      for (int j = 0; j < TQ; ++j) read_q(j);
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) sq[j] = q_scale[j][step];
-      __syncthreads();     // this step's codes are there, and the other buffer is free
-      if (step + 1 < steps) load(step + 1);
-      const uint8_t* at = sh[step & 1];
-      int8v fp[TP], fq[TQ];
-      auto piece = [&](int r, int k) {
-        return *reinterpret_cast<const int4v*>(at + r * kStep + ((k ^ (r & 7)) * 16));
-      };
+      for (int i = 0; i < kAhead; ++i) read_p(i);
+    }
+    Tile next = t;
+    for (int block = t.block; block < t.end; ++block) {
+      const bool last = block + 1 == t.end;
+      aim();
+      bool on = !last;         // whether another step follows that is known here
+      if (last && next_id < tiles) {
+        next = tile_of(next_id);
+        on = next.block < next.end;
+      }
 #pragma unroll
       for (int i = 0; i < TP; ++i) {
-        const int r = (wp * TP + i) * 16 + lrow;
-        fp[i] = __builtin_shufflevector(piece(r, quarter * 2), piece(r, quarter * 2 + 1), 0, 1, 2, 3, 4, 5, 6, 7);
-      }
+        if (i + kAhead < TP) read_p(i + kAhead);
+        if (i >= TP - kTail) continue;
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) {
-        const int r = BP + (wq * TQ + j) * 16 + lrow;
-        fq[j] = __builtin_shufflevector(piece(r, quarter * 2), piece(r, quarter * 2 + 1), 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int j = 0; j < TQ; ++j) multiply(i, j);
+        __builtin_amdgcn_sched_barrier(0);      // or all rows are read at once, into registers that there are not
       }
-      if constexpr (kDtype == EQB_DTYPE_F32) {
+      __builtin_amdgcn_sched_barrier(0);
+      step_barrier();
+      if (on) next_step(last ? next.block : block + 1);
+      load_scales();
+      __builtin_amdgcn_sched_barrier(0);
+      // the last rows, column by column, and the next step's fragments in the place of those
+      // that are not needed any more (with no next step they are not used)
+      if constexpr (kWide) {
+        auto power = [&](int byte) { return __uint_as_float((uint32_t)byte << 23); };
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+#pragma unroll
+          for (int i = k; i < kLoads; i += 4) load_codes(i);
           bf16x8_t wide[TQ];
 #pragma unroll
-          for (int j = 0; j < TQ; ++j) wide[j] = widen(fq[j], k, __uint_as_float((uint32_t)sq[j] << 23));
+          for (int j = 0; j < TQ; ++j) wide[j] = widen(fq[j], k, power(sq[kOneScale ? 0 : j]));
 #pragma unroll
           for (int i = 0; i < TP; ++i) {
-            const bf16x8_t x = widen(fp[i], k, __uint_as_float((uint32_t)sp[i] << 23));
+            const bf16x8_t x = widen(fp[i], k, power(sp[i]));
 #pragma unroll
             for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[j], x, acc[i][j], 0, 0, 0);
           }
         }
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) read_q(j);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_p(i);
       } else {
+        static_assert(kTail + kAhead <= TP, "row 0 is read while the last rows are multiplied");
 #pragma unroll
-        for (int i = 0; i < TP; ++i)
+        for (int i = 0; i < kAhead; ++i) read_p(i);
 #pragma unroll
-          for (int j = 0; j < TQ; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fq[j], fp[i], acc[i][j], 0, 0, 0, sq[j], 0, sp[i]);
-      }
-    }
-
-    // a lane holds four neighbouring q of one p
-    typename O::raw* const out = static_cast<typename O::raw*>(a.out);
-    const int64_t width = kGrad ? a.H : a.N;
-    const int64_t row0 = kGrad ? (int64_t)e * a.N + p0 : p0;
+        for (int j = 0; j < TQ; ++j) {
 #pragma unroll
-    for (int i = 0; i < TP; ++i) {
-      const int r = (wp * TP + i) * 16 + lrow;
-      if (r >= np) continue;
+          for (int i = TP - kTail; i < TP; ++i) multiply(i, j);
+          read_q(j);
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) {
-        const int c = (wq * TQ + j) * 16 + quarter * 4;
-        typename O::raw* to = out + (row0 + r) * width + q0 + c;
-        typedef typename O::raw vec __attribute__((ext_vector_type(4)));
-        typedef vec any __attribute__((aligned(alignof(typename O::raw))));
-        const vec v = {O::from_f(acc[i][j][0]), O::from_f(acc[i][j][1]), O::from_f(acc[i][j][2]), O::from_f(acc[i][j][3])};
-        if (c + 4 <= nq) {
-          *reinterpret_cast<any*>(to) = v;
-        } else {
-#pragma unroll
-          for (int k = 0; k < 3; ++k)
-            if (c + k < nq) to[k] = v[k];
+          for (int i = j; i < kLoads; i += TQ) load_codes(i);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
+      buffer ^= 1;
+      if (last) ready = on;
     }
+
+    // the places in out are computed here, not kept in registers through the loops above
+    int64_t width = kGrad ? a.H : a.N;
+    int row = wp * TP * 16 + lrow, col = wq * TQ * 16 + quarter * 4 * kPair;
+    asm volatile("" : "+s"(width), "+v"(row), "+v"(col));
+    typedef raw vec __attribute__((ext_vector_type(4 * kPair)));
+    typedef vec any __attribute__((aligned(alignof(raw))));
+    raw* to = static_cast<raw*>(a.out) + (t.row + row) * width + t.col + col;
+    auto values = [&](int i, int j) {
+      vec v;
+#pragma unroll
+      for (int h = 0; h < kPair; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[h * 4 + k] = O::from_f(acc[i][j + h][k]);
+      return v;
+    };
+    if (t.np == BP && t.nq == BQ) {
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+#pragma unroll
+        for (int j = 0; j < TQ; j += kPair) {
+          if constexpr (kPair == 2 && TQ % 4 == 0) {
+            if (j % 4 != 0) continue;
+            // a store of 8 whole lines of 128 bytes instead of 16 halves: lanes of rows 8 apart
+            // exchange halves (884,736 rows of 1,024 by 1,024: 1,179 -> 1,168 us)
+            const int4v x = __builtin_bit_cast(int4v, values(i, j)), y = __builtin_bit_cast(int4v, values(i, j + 2));
+            int4v up, down;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              up[k] = __builtin_amdgcn_update_dpp(x[k], y[k], 0x128, 0xF, 0xC, false);
+              down[k] = __builtin_amdgcn_update_dpp(y[k], x[k], 0x128, 0xF, 0x3, false);
+            }
+            raw* const at = to + j * 16 + ((lane & 8) ? 32 - 8 * width : 0);
+            *reinterpret_cast<any*>(at) = __builtin_bit_cast(vec, up);
+            *reinterpret_cast<any*>(at + 8 * width) = __builtin_bit_cast(vec, down);
+          } else {
+            *reinterpret_cast<any*>(to + j * 16) = values(i, j);
+          }
+        }
+        to += 16 * width;
+      }
+    } else {
+      const int left = t.nq - col;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        if (row + i * 16 < t.np) {
+#pragma unroll
+          for (int j = 0; j < TQ; j += kPair) {
+            const vec v = values(i, j);
+            if (left >= j * 16 + 4 * kPair) {
+              *reinterpret_cast<any*>(to + j * 16) = v;
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4 * kPair - 1; ++k)
+                if (left > j * 16 + k) to[j * 16 + k] = v[k];
+            }
+          }
+        }
+        to += 16 * width;
+      }
+    }
+    if (next_id >= tiles) return;
+    if (t.block == t.end) {
+      next = tile_of(next_id);
+      ready = false;
+    }
+    id = next_id;
+    t = next;
   }
 }
 
-template <bool kGrad>
-eqb_status launch_product(const ProductArgs& a, hipStream_t s) {
-  constexpr int BP = 128, BQ = 128;
+template <int BP, int BQ, int WP, int WQ, bool kGrad, bool kWide>
+eqb_status launch_form(const ProductArgs& a, int per_cu, hipStream_t s) {
   const int64_t q_tiles = ((kGrad ? a.H : a.N) + BQ - 1) / BQ;
   const int64_t p_tiles = kGrad ? (int64_t)a.E * ((a.N + BP - 1) / BP) : a.rows / BP + (a.rows < a.E ? a.rows : a.E);
-  int64_t grid = (int64_t)num_cus() * 2;
+  int64_t grid = (int64_t)num_cus() * per_cu;
+  if (p_tiles * q_tiles > INT32_MAX - grid) return EQB_ERR_UNSUPPORTED;
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < grid) grid = cap;
   if (p_tiles * q_tiles < grid) grid = p_tiles * q_tiles;
-  const uint32_t blocks = (uint32_t)grid;
-  if (a.dtype == EQB_DTYPE_BF16) product_kernel<BP, BQ, 2, 2, kGrad, EQB_DTYPE_BF16><<<blocks, 256, 0, s>>>(a);
-  else if (a.dtype == EQB_DTYPE_F16) product_kernel<BP, BQ, 2, 2, kGrad, EQB_DTYPE_F16><<<blocks, 256, 0, s>>>(a);
-  else product_kernel<BP, BQ, 2, 2, kGrad, EQB_DTYPE_F32><<<blocks, 256, 0, s>>>(a);
+  const uint32_t blocks = (uint32_t)grid, threads = 64 * WP * WQ;
+  if constexpr (kWide) product_kernel<BP, BQ, WP, WQ, kGrad, EQB_DTYPE_F32><<<blocks, threads, 0, s>>>(a);
+  else if (a.dtype == EQB_DTYPE_BF16) product_kernel<BP, BQ, WP, WQ, kGrad, EQB_DTYPE_BF16><<<blocks, threads, 0, s>>>(a);
+  else product_kernel<BP, BQ, WP, WQ, kGrad, EQB_DTYPE_F16><<<blocks, threads, 0, s>>>(a);
   return launch_status();
+}
+
+// Tiles of 64 x 64 (four blocks on a compute unit), 128 x 128 (two) and 256 x 256 (one, for results
+// of 16 bits), all times in us, results bf16 where nothing is said:
+//   few rows an expert, up to 64 on average: 64 rows of 2,048 to 2,048 columns, E = 256, 38.5 with 64,
+//   39.6 with 128, 54 with 256; one row 9.9, 13.0, 25; 4,096 rows of 1,024, E = 64, 21.7, 24.1, 23.8;
+//   but 4,096 rows of 1,024, E = 8, 16.7, 14.7, 20.8.
+//   weight gradients of few tiles: 16 of 512 x 256, 15.2, 18.4, 40; but 8 of 1,024 x 1,024, 20.2, 17.0, 23.4.
+//   256 once two of its tiles come on a compute unit and what they reach over the edges costs no more
+//   than an eighth: 98,304 rows of 2,048 to 2,048, E = 64, 454 against 561 with 128; 196,608 of 1,024
+//   to 1,024, E = 256, 304, 352; 24,576 rows of 2,048 160 both; but 80,000 of 500 to 300, E = 32,
+//   37.6, 30.8; gradients 64 of 2,048 x 2,048 over 98,304 rows 583, 794; 32 of 777 x 1,001 59, 55.
+template <bool kGrad>
+eqb_status launch_product(const ProductArgs& a, hipStream_t s) {
+  const int64_t cus = num_cus(), E = a.E, most = a.rows < E ? a.rows : E;
+  const int64_t p = kGrad ? a.N : a.rows, q = kGrad ? a.H : a.N;
+  auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to; };
+  // an expert's rows end in the middle of a tile
+  auto tiles = [&](int64_t side) { return (kGrad ? E * up(p, side) : p / side + most / 2) * up(q, side); };
+  const bool small = kGrad ? tiles(128) < cus : a.rows <= 64 * E;
+  if (a.dtype == EQB_DTYPE_F32) {
+    if (small) return launch_form<64, 64, 2, 2, kGrad, true>(a, 4, s);
+    return launch_form<128, 128, 2, 2, kGrad, true>(a, 2, s);
+  }
+  if (small) return launch_form<64, 64, 2, 2, kGrad, false>(a, 4, s);
+  if (tiles(256) >= 2 * cus && 4 * tiles(256) * 8 <= tiles(128) * 9) return launch_form<256, 256, 2, 4, kGrad, false>(a, 1, s);
+  return launch_form<128, 128, 2, 2, kGrad, false>(a, 2, s);
 }
 
 }  // namespace
