@@ -175,11 +175,13 @@ __device__ __forceinline__ int largest(const F (&q)[kPer], int l, F& top) {
   return top > lowest_of<F>() ? at : kNone;
 }
 
-// Two scores in binary32 nearer than this may be the other way round: a score s is within
-// 2^-19 s of its value (a softmax's sum of 256 in a tree of 8 and 5 levels is most of that), and
-// the sum with the bias is rounded once; s is at most |q| and the largest bias.
+// Two scores in binary32 nearer than this may be the other way round.  A score s is within 2^-18 s of
+// its value, or 2^-58: the argument of an exponential, up to 58 ln 2 below which the score is nothing,
+// is off by 58 (2^-24 + 2^-25), the exponential, a softmax's sum of 256 (a tree of 32 and 3 levels, all
+// the same way for a row) and the quotient by a few 2^-24 each.  The sum with the bias is rounded once,
+// and s is at most |q| and the largest bias.
 __device__ __forceinline__ bool near(float a, float b, float most_bias) {
-  return a - b <= 0x1p-18f * (fabsf(a) + most_bias + 0x1p-40f);
+  return a - b <= 0x1p-16f * (fabsf(a) + most_bias) + 0x1p-56f;
 }
 __device__ __forceinline__ bool near(double, double, float) { return false; }
 
@@ -316,6 +318,318 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_kernel(const Scor
   }
 }
 
+// What the routing kernels share behind the choice: the weights of a row's experts `chosen`, a
+// lane's k at a time.  z: this lane's logits of the row, L lanes together all of them.
+template <int L, int kDtype, int V>
+__device__ __forceinline__ void softmax_of(const float (&z)[V], float& top, float& total) {
+  top = z[0];
+#pragma unroll
+  for (int i = 1; i < V; ++i) top = fmaxf(top, z[i]);
+  top = row_max<L>(top);
+  if (top == -__builtin_inff()) top = 0.0f;
+  total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) total += exp_neg(top - z[i]);
+  total = row_sum<L>(total);
+}
+
+// ------------------------------------------------------ up to eight experts --
+// Keys are binary64: a binary32 score with its expert's place in the low bits, so that one maximum
+// and one minimum order two of them, ties to the lower expert.  A row lies in L lanes of V experts
+// each; a lane sorts its keys in eights, merges those to its best eight, and the lanes' eights are
+// merged in pairs.  It is bound by the issue of instructions, some 75 a row, and needs four waves on
+// a SIMD for it: 147,456 tokens of 256 experts, 8 groups, K = 6, bf16 logits: 76 us (0.9 TB/s; the bytes
+// alone take 15); with all 32 keys of a lane in registers at two waves 151; with K rounds of a
+// maximum over 32 lanes, as above, 215.
+__device__ __forceinline__ double key_max(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double key_min(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+constexpr uint32_t kMaskedHigh = 0xFFE00000u;       // below every score, whatever the low bits
+__device__ __forceinline__ double key_of(float q, int e) {
+  q += 0.0f;                            // -0 is 0
+  const uint64_t u = __builtin_bit_cast(uint64_t, (double)q);
+  const uint32_t low = q < 0.0f ? (uint32_t)e : 255u - e;       // a larger significand is less there
+  const uint32_t high = q > -__builtin_inff() ? (uint32_t)(u >> 32) : kMaskedHigh;
+  return __builtin_bit_cast(double, (uint64_t)high << 32 | ((uint32_t)u | low));
+}
+__device__ __forceinline__ bool key_masked(double k) { return k < -1e300; }
+__device__ __forceinline__ int key_expert(double k) {
+  const int low = (int)(__builtin_bit_cast(uint64_t, k) & 255u);
+  return k < 0.0 ? low : 255 - low;
+}
+__device__ __forceinline__ void order(double& a, double& b) {
+  const double hi = key_max(a, b);
+  b = key_min(a, b);
+  a = hi;
+}
+__device__ __forceinline__ void sort8(double* k) {
+  constexpr int pairs[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                                {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+  for (int i = 0; i < 19; ++i) order(k[pairs[i][0]], k[pairs[i][1]]);
+}
+// The best eight of two sorted eights, sorted, in a; lost: the largest of those that are not among
+// them (kNinth).
+template <bool kNinth>
+__device__ __forceinline__ void merge8(double* a, const double* b, double& lost) {
+  if constexpr (kNinth) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lost = key_max(lost, key_min(a[i], b[7 - i]));
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = key_max(a[i], b[7 - i]);
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((i & d) == 0) order(a[i], a[i + d]);
+}
+template <int kCtrl, class T>
+__device__ __forceinline__ T moved(T x) {
+  if constexpr (sizeof(T) == 8) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, kCtrl, 0xF, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), kCtrl, 0xF, 0xF, false);
+    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), kCtrl, 0xF, 0xF, false));
+  }
+}
+// From the lane whose number within the row's eight differs by x
+template <int x, class T>
+__device__ __forceinline__ T from_lane(T v) {
+  static_assert(x >= 1 && x <= 7, "eight lanes");
+  if constexpr (x == 1) return moved<0xB1>(v);
+  else if constexpr (x == 2) return moved<0x4E>(v);
+  else if constexpr (x == 3) return moved<0x1B>(v);
+  else if constexpr (x == 7) return moved<0x141>(v);
+  else return from_lane<7 - x>(moved<0x141>(v));
+}
+
+// The sums of a group's two best in this lane and, over the lanes that share the group, theirs;
+// whether the lane's group is among the best, and whether that was too near to call.
+template <int L>
+__device__ __forceinline__ bool group_kept(const ScoredArgs& a, float t1, float t2, int V, int l, float most_bias, bool& doubt) {
+  const int share = a.E / a.groups / V;         // lanes of a group
+  auto join = [&](float o1, float o2) { merge2(t1, t2, o1, o2); };
+  if constexpr (L >= 2) {
+    if (share >= 2) join(from_lane<1>(t1), from_lane<1>(t2));
+  }
+  if constexpr (L >= 4) {
+    if (share >= 4) join(from_lane<2>(t1), from_lane<2>(t2));
+  }
+  const float none = -__builtin_inff();
+  const float g = a.group_top == 2 && t2 > none ? t1 + t2 : t1;
+  const int mine = l / share;
+  int better = 0;
+  auto look = [&](auto x) {
+    constexpr int d = decltype(x)::value;
+    if constexpr (d < L) {
+      const float o = from_lane<d>(g);
+      better += o > g || (o == g && (l ^ d) / share < mine) ? 1 : 0;
+    }
+  };
+  look(std::integral_constant<int, 1>{});
+  look(std::integral_constant<int, 2>{});
+  look(std::integral_constant<int, 3>{});
+  look(std::integral_constant<int, 4>{});
+  look(std::integral_constant<int, 5>{});
+  look(std::integral_constant<int, 6>{});
+  look(std::integral_constant<int, 7>{});
+  const bool kept = better < a.top_groups * share;
+  const float least = -row_max<L>(kept ? -g : none), most = row_max<L>(kept ? none : g);
+  doubt = doubt || (most > none && near(least, most, 2.0f * most_bias));
+  return kept;
+}
+
+template <int E, int kDtype, bool kNinth>
+__global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(const ScoredArgs a) {
+  constexpr int V = E / 8 > kPer ? E / 8 : kPer, L = E / V, kRows = 64 / L, kLists = V / 8;
+  constexpr int kSlow = E / kPer;               // lanes of a row that is looked at once more
+  typedef typename Logit<kDtype>::raw raw;
+  typedef raw vec __attribute__((ext_vector_type(kPer)));
+  __shared__ __attribute__((aligned(16))) float sh_bias[E];
+  __shared__ int16_t sh_chosen[kScoredWaves][8];
+  const int lane = threadIdx.x & 63, l = lane % L;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float none = -__builtin_inff();
+  float most_bias = 0.0f;
+  if (a.bias) {
+    for (int e = threadIdx.x; e < E; e += kScoredThreads) sh_bias[e] = a.bias[e];
+    __syncthreads();
+    for (int i = 0; i < V; ++i) {
+      const float m = fabsf(sh_bias[l * V + i]);
+      most_bias = fmaxf(most_bias, m < -none ? m : 0.0f);
+    }
+    most_bias = row_max<L>(most_bias);
+  }
+  const bool by_groups = a.top_groups < a.groups, by_logits = a.bias == nullptr;
+  const int64_t step = (int64_t)gridDim.x * kScoredWaves * kRows;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kScoredWaves + wave) * kRows; t0 < a.T; t0 += step) {
+    const bool live = t0 + lane / L < a.T;
+    const int64_t t = live ? t0 + lane / L : a.T - 1;
+    const raw* row = static_cast<const raw*>(a.z) + t * E;
+    auto piece = [&](int i, float (&z)[kPer]) {
+      const vec x = *reinterpret_cast<const vec*>(row + l * V + i * kPer);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) z[j] = clean(Logit<kDtype>::to_f(x[j]));
+    };
+    float top = 0.0f, total = 1.0f;
+    if (a.softmax) {
+      top = none;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        float z[kPer];
+        piece(i, z);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) top = fmaxf(top, z[j]);
+      }
+      top = row_max<L>(top);
+      if (top == none) top = 0.0f;
+      if (!a.normalize || !by_logits || by_groups) {        // else the sum is not needed
+        total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) {
+          float z[kPer];
+          piece(i, z);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) total += exp_neg(top - z[j]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        total = row_sum<L>(total);
+      }
+    }
+    // scores for the choice only: within 2^-18 of their value (or 2^-58)
+    const float rcp_total = __builtin_amdgcn_rcpf(total);
+    auto quick = [&](float x) {
+      const float kLog2e = 1.44269502162933349609375f;
+      if (a.softmax) return __builtin_amdgcn_exp2f((x - top) * kLog2e) * rcp_total;
+      return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
+    };
+    bool doubt = false;
+    double key[8], lost = __builtin_bit_cast(double, (uint64_t)kMaskedHigh << 32);
+    // eight at a time, so that few registers are in use and many waves run
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+      float z[kPer];
+      piece(i, z);
+      double other[8], (&to)[8] = i == 0 ? key : other;
+      if (by_logits) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) to[j] = key_of(z[j], l * V + i * kPer + j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPer; j += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(&sh_bias[l * V + i * kPer + j]);
+          const float bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const float q = quick(z[j + h]) + bs[h];
+            to[j + h] = key_of(z[j + h] > none && q == q ? q : none, l * V + i * kPer + j + h);
+          }
+        }
+      }
+      sort8(to);
+      if (i > 0) merge8<kNinth>(key, other, lost);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    bool kept = true;
+    if (by_groups) {
+      auto score = [&](double k) { return key_masked(k) ? none : by_logits ? quick((float)k) : (float)k; };
+      kept = group_kept<L>(a, score(key[0]), score(key[1]), V, l, most_bias, doubt);
+    }
+    auto drop = [&](double k) {
+      const uint64_t u = __builtin_bit_cast(uint64_t, k);
+      return __builtin_bit_cast(double, (uint64_t)(kept ? (uint32_t)(u >> 32) : kMaskedHigh) << 32 | (uint32_t)u);
+    };
+    if (by_groups) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) key[i] = drop(key[i]);
+      lost = drop(lost);
+    }
+    auto meet = [&](auto x) {
+      constexpr int d = decltype(x)::value;
+      double other[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) other[i] = from_lane<d>(key[i]);
+      if constexpr (kNinth) lost = key_max(lost, from_lane<d>(lost));
+      merge8<kNinth>(key, other, lost);
+    };
+    if constexpr (L >= 2) meet(std::integral_constant<int, 1>{});
+    if constexpr (L >= 4) meet(std::integral_constant<int, 2>{});
+    if constexpr (L >= 8) meet(std::integral_constant<int, 7>{});    // the four lanes of a half have the same
+    // the k-th best to lane k (and k + L, ...)
+    constexpr int kEach = 8 / L > 1 ? 8 / L : 1;
+    int e[kEach];
+    float s[kEach], sum = 0.0f;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+      const int k = l + h * L;
+      double mine = key[0], next = key[1];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) {
+        mine = k == i ? key[i] : mine;
+        next = k == i ? (i < 7 ? key[i + 1 < 8 ? i + 1 : 7] : lost) : next;
+      }
+      const bool on = k < a.K && !key_masked(mine);
+      e[h] = on ? key_expert(mine) : -1;
+      if (!by_logits) doubt = doubt || (on && !key_masked(next) && near((float)mine, (float)next, most_bias));
+      s[h] = 0.0f;
+      if (on) {
+        const float x = clean(Logit<kDtype>::to_f(row[e[h]]));
+        s[h] = a.softmax ? exp_neg(top - x) : sigmoid_of(x);
+      }
+      sum += s[h];
+    }
+    const float by = a.normalize ? row_sum<L>(sum) : total;
+    const uint64_t doubts = __ballot(doubt && live);
+    const bool again = (doubts >> (lane / L * L) & (L == 64 ? ~0ull : (1ull << (L & 63)) - 1)) != 0;
+    if (live && !again) {
+#pragma unroll
+      for (int h = 0; h < kEach; ++h) {
+        const int k = l + h * L;
+        if (k < a.K) {
+          a.idx[t * a.K + k] = e[h];
+          a.weight[t * a.K + k] = by > 0.0f ? a.scale * (s[h] / by) : 0.0f;
+        }
+      }
+    }
+    // rows with scores too near to call, one at a time in binary64, by all lanes
+    for (uint64_t left = __ballot(again && l == 0); left != 0; left &= left - 1) {
+      const int64_t tr = t0 + __builtin_ctzll(left) / L;
+      const int ls = lane % kSlow;
+      float zs[kPer], bs[kPer];
+      load_row<E, kDtype>(a.z, tr, ls, zs);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) bs[i] = a.bias ? sh_bias[ls * kPer + i] : 0.0f;
+      choose<kSlow, double>(a, zs, bs, most_bias, ls, sh_chosen[wave]);
+      lds_wave_sync();
+      float top_s = 0.0f, total_s = 1.0f;
+      if (a.softmax) softmax_of<kSlow, kDtype>(zs, top_s, total_s);
+      const raw* at = static_cast<const raw*>(a.z) + tr * E;
+      const int es = lane < a.K ? sh_chosen[wave][lane & 7] : -1;
+      float ss = 0.0f;
+      if (es >= 0) {
+        const float x = clean(Logit<kDtype>::to_f(at[es]));
+        ss = a.softmax ? exp_neg(top_s - x) : sigmoid_of(x);
+      }
+      const float by_s = a.normalize ? row_sum<8>(ss) : total_s;      // lanes 0 .. 7 hold them
+      if (lane < a.K) {
+        a.idx[tr * a.K + lane] = es;
+        a.weight[tr * a.K + lane] = by_s > 0.0f ? a.scale * (ss / by_s) : 0.0f;
+      }
+      lds_wave_sync();
+    }
+  }
+}
+
 template <int E, int kDtype>
 __global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(const ScoredArgs a) {
   constexpr int L = E / kPer, kRows = 64 / L;
@@ -409,13 +723,28 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(c
 }
 
 template <int E, int kDtype>
+void launch_eight(const ScoredArgs& a, hipStream_t s) {
+  constexpr int V = E / 8 > kPer ? E / 8 : kPer, kRows = 64 / (E / V) * kScoredWaves;
+  int64_t blocks = (a.T + kRows - 1) / kRows, most = (int64_t)num_cus() * 8;
+  const int cap = max_blocks_cap();
+  if (cap > 0 && cap < most) most = cap;
+  if (blocks > most) blocks = most;
+  if (a.K == 8) route_scored_eight_kernel<E, kDtype, true><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  else route_scored_eight_kernel<E, kDtype, false><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+}
+
+template <int E, int kDtype>
 eqb_status launch_scored_e(const ScoredArgs& a, bool backward, hipStream_t s) {
   constexpr int kRows = 64 / (E / kPer) * kScoredWaves;
   int64_t blocks = (a.T + kRows - 1) / kRows, most = (int64_t)num_cus() * 8;
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
   if (blocks > most) blocks = most;
+  // whole lanes of a group, and up to eight experts
+  constexpr int V = E / 8 > kPer ? E / 8 : kPer;
+  const bool eight = a.K <= 8 && (a.top_groups == a.groups || a.E / a.groups >= V);
   if (backward) route_scored_backward_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  else if (eight) launch_eight<E, kDtype>(a, s);
   else route_scored_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
   return launch_status();
 }
