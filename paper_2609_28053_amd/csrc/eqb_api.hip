@@ -691,6 +691,8 @@ eqb_status eqb_experts_grad_weight(const uint8_t* grad_codes, const uint8_t* gra
                                    const uint8_t* scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,
                                    int32_t hidden, int32_t dtype, void* out, void* stream) {
   const ProductArgs a{grad_codes, grad_scales, codes, scales, offsets, rows, E, N, hidden, dtype, out};
+  // a tile's rows are reached by 32-bit offsets
+  if (code_shape(rows, hidden, dtype) && E >= 1 && column_width(rows, E) > kMostHidden) return EQB_ERR_UNSUPPORTED;
   return product_call(launch_experts_grad_weight, a, true, stream);
 }
 

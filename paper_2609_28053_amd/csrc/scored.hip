@@ -353,7 +353,7 @@ __device__ __forceinline__ double key_min(double a, double b) {
 }
 constexpr uint32_t kMaskedHigh = 0xFFE00000u;       // below every score, whatever the low bits
 __device__ __forceinline__ double key_of(float q, int e) {
-  q += 0.0f;                            // -0 is 0
+  q = fminf(q + 0.0f, 3.402823466e38f);   // -0 is 0; an infinity with low bits would be no number
   const uint64_t u = __builtin_bit_cast(uint64_t, (double)q);
   const uint32_t low = q < 0.0f ? (uint32_t)e : 255u - e;       // a larger significand is less there
   const uint32_t high = q > -__builtin_inff() ? (uint32_t)(u >> 32) : kMaskedHigh;

@@ -19,6 +19,15 @@ import torch
 from . import eqb
 
 
+def _as_stream(stream):
+    """A torch stream of what ``stream`` may be: one, a handle as a number, or None for the current one."""
+    if stream is None:
+        return torch.cuda.current_stream()
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+
+
 class _Handle:
     """A handle's buffers and the streams that are behind their fills."""
 
@@ -45,10 +54,7 @@ class _Handle:
         first = eqb._stream(stream) not in self._behind
         if stream is None and not first:
             return contextlib.nullcontext()
-        if stream is None:
-            stream = torch.cuda.current_stream()
-        elif not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+        stream = _as_stream(stream)
         if first:
             with torch.cuda.stream(stream):
                 capturing = torch.cuda.is_current_stream_capturing()
