@@ -28,9 +28,10 @@ struct Logit<EQB_DTYPE_F32> {
 };
 
 // A masked logit (-inf or NaN) becomes -inf, +inf the largest finite number.
+constexpr float kLargest = 3.402823466e38f;
 __device__ __forceinline__ float clean(float z) {
   const float lowest = -__builtin_inff();
-  return z > lowest ? fminf(z, 3.402823466e38f) : lowest;
+  return z > lowest ? fminf(z, kLargest) : lowest;
 }
 
 // exp(-a), a >= 0 (infinity gives 0): 2^(-p) (1 - l ln 2) with p + l = a log2 e in two parts,
@@ -175,15 +176,18 @@ __device__ __forceinline__ int largest(const F (&q)[kPer], int l, F& top) {
   return top > lowest_of<F>() ? at : kNone;
 }
 
-// Two scores in binary32 nearer than this may be the other way round.  A score s is within 2^-18 s of
-// its value, or 2^-58: the argument of an exponential, up to 58 ln 2 below which the score is nothing,
-// is off by 58 (2^-24 + 2^-25), the exponential, a softmax's sum of 256 (a tree of 32 and 3 levels, all
-// the same way for a row) and the quotient by a few 2^-24 each.  The sum with the bias is rounded once,
-// and s is at most |q| and the largest bias.
-__device__ __forceinline__ bool near(float a, float b, float most_bias) {
-  return a - b <= 0x1p-16f * (fabsf(a) + most_bias) + 0x1p-56f;
+// Two sums q of a score and its bias in binary32 nearer than this may be the other way round. s is at most
+// |q| and the largest bias, and q is rounded once (2^-24 |q|).
+//   A sigmoid is off by (1 - s) |z| 2^-23.4 of itself from its exponential's argument and by 2^-21.7 from the
+//   exponential, the sum and the reciprocal. Of each 0.75 2^-20 (|q| + bias) covers all but
+//   s max(0, |z| - 3.8) 2^-23.4 < 2^-30.3 (the maximum of e^-z (z - 3.8), at z = 4.8): 2^-28 covers that for two pairs.
+//   A softmax's exponential is off by d 2^-22.7 of itself, d the distance to the largest logit (2^-17.4 up to
+//   d = 39, less than 2^-56 behind that), and its sum of 256, a tree of 32 and 3 levels or of 8 and 5, by 35
+//   2^-24, the same way for a row: 2^-16 (|q| + bias) + 2^-54.
+__device__ __forceinline__ bool near(float a, float b, float most_bias, bool softmax) {
+  return a - b <= (softmax ? 0x1p-16f : 0x1.8p-20f) * (fabsf(a) + most_bias) + (softmax ? 0x1p-54f : 0x1p-28f);
 }
-__device__ __forceinline__ bool near(double, double, float) { return false; }
+__device__ __forceinline__ bool near(double, double, float, bool) { return false; }
 
 // Chooses a row's K experts by rank into `chosen` (kNone where there are none left); whether an
 // order that matters was too near to call.  In binary32 the (K + 1)st is looked at as well.
@@ -209,7 +213,7 @@ __device__ __forceinline__ bool choose(const ScoredArgs& a, const float (&z)[kPe
       F top;
       const int at = largest<L>(g, l, top);
       if (k == a.top_groups) {
-        doubt = doubt || (at != kNone && near(last, top, 2 * most_bias));
+        doubt = doubt || (at != kNone && near(last, top, 2 * most_bias, a.softmax));
       } else {
         last = top;
 #pragma unroll
@@ -234,7 +238,7 @@ __device__ __forceinline__ bool choose(const ScoredArgs& a, const float (&z)[kPe
   for (int k = 0; k < a.K + (kQuick && !by_logits ? 1 : 0); ++k) {
     F top;
     const int at = largest<L>(q, l, top);
-    if (kQuick && !by_logits && k > 0) doubt = doubt || (at != kNone && near(last, top, most_bias));
+    if (kQuick && !by_logits && k > 0) doubt = doubt || (at != kNone && near(last, top, most_bias, a.softmax));
     last = top;
     if (k < a.K && l == 0) chosen[k] = (int16_t)(at == kNone ? -1 : at);
 #pragma unroll
@@ -337,10 +341,12 @@ __device__ __forceinline__ void softmax_of(const float (&z)[V], float& top, floa
 // Keys are binary64: a binary32 score with its expert's place in the low bits, so that one maximum
 // and one minimum order two of them, ties to the lower expert.  A row lies in L lanes of V experts
 // each; a lane sorts its keys in eights, merges those to its best eight, and the lanes' eights are
-// merged in pairs.  It is bound by the issue of instructions, some 75 a row, and needs four waves on
-// a SIMD for it: 147,456 tokens of 256 experts, 8 groups, K = 6, bf16 logits: 76 us (0.9 TB/s; the bytes
-// alone take 15); with all 32 keys of a lane in registers at two waves 151; with K rounds of a
-// maximum over 32 lanes, as above, 215.
+// merged in pairs.  It is bound by the issue of instructions and of the waves that wait for their rows:
+// 147,456 tokens of 256 experts, 8 groups, K = 6, bf16 logits, at four waves on a SIMD: 55 us (1.4 TB/s;
+// the bytes alone take 15), K = 8 60, without groups 47, without a bias as well 35, a softmax 77.  Where
+// a wider bound of doubt sent more rows to binary64: four waves 68, five 70, six 79, two waves with all
+// 32 keys of a lane in registers 151.  With K rounds of a maximum
+// over 32 lanes, as above, 215.
 __device__ __forceinline__ double key_max(double a, double b) {
   double r;
   asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -351,18 +357,24 @@ __device__ __forceinline__ double key_min(double a, double b) {
   asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
   return r;
 }
-constexpr uint32_t kMaskedHigh = 0xFFE00000u;       // below every score, whatever the low bits
-__device__ __forceinline__ double key_of(float q, int e) {
-  q = fminf(q + 0.0f, 3.402823466e38f);   // -0 is 0; an infinity with low bits would be no number
-  const uint64_t u = __builtin_bit_cast(uint64_t, (double)q);
-  const uint32_t low = q < 0.0f ? (uint32_t)e : 255u - e;       // a larger significand is less there
-  const uint32_t high = q > -__builtin_inff() ? (uint32_t)(u >> 32) : kMaskedHigh;
-  return __builtin_bit_cast(double, (uint64_t)high << 32 | ((uint32_t)u | low));
+// Below every score, whatever the low bits.
+constexpr uint32_t kMaskedHigh = 0xFFE00000u;
+constexpr double kMasked = -0x1p1023;
+__device__ __forceinline__ double key_with(double q, uint32_t low) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, key_max(q, kMasked));    // an infinity with low bits would be no number
+  return __builtin_bit_cast(double, (u & 0xFFFFFFFF00000000ull) | ((uint32_t)u + low));
 }
+// Of a logit: ties go to the lower expert.
+__device__ __forceinline__ double key_of_logit(float z, int e) {
+  z += 0.0f;                            // -0 is 0
+  return key_with(z, z < 0.0f ? (uint32_t)e : 255u - e);      // a larger significand is less there
+}
+// Of a score, e = first + i: the order of equal scores does not matter, they are too near to call.
+__device__ __forceinline__ double key_of_score(float q, uint32_t last, int i) { return key_with(q, last + (uint32_t)(31 - i)); }
 __device__ __forceinline__ bool key_masked(double k) { return k < -1e300; }
-__device__ __forceinline__ int key_expert(double k) {
+__device__ __forceinline__ int key_expert(double k, bool of_logit) {
   const int low = (int)(__builtin_bit_cast(uint64_t, k) & 255u);
-  return k < 0.0 ? low : 255 - low;
+  return of_logit && k < 0.0 ? low : 255 - low;
 }
 __device__ __forceinline__ void order(double& a, double& b) {
   const double hi = key_max(a, b);
@@ -376,10 +388,9 @@ __device__ __forceinline__ void sort8(double* k) {
   for (int i = 0; i < 19; ++i) order(k[pairs[i][0]], k[pairs[i][1]]);
 }
 // The best eight of two sorted eights, sorted, in a; lost: the largest of those that are not among
-// them (kNinth).
-template <bool kNinth>
-__device__ __forceinline__ void merge8(double* a, const double* b, double& lost) {
-  if constexpr (kNinth) {
+// them (ninth: eight are to be chosen, and how near the next one is matters).
+__device__ __forceinline__ void merge8(double* a, const double* b, double& lost, bool ninth) {
+  if (ninth) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) lost = key_max(lost, key_min(a[i], b[7 - i]));
   }
@@ -445,11 +456,11 @@ __device__ __forceinline__ bool group_kept(const ScoredArgs& a, float t1, float 
   look(std::integral_constant<int, 7>{});
   const bool kept = better < a.top_groups * share;
   const float least = -row_max<L>(kept ? -g : none), most = row_max<L>(kept ? none : g);
-  doubt = doubt || (most > none && near(least, most, 2.0f * most_bias));
+  doubt = doubt || (most > none && near(least, most, 2.0f * most_bias, a.softmax));
   return kept;
 }
 
-template <int E, int kDtype, bool kNinth>
+template <int E, int kDtype, bool kSoftmax>
 __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(const ScoredArgs a) {
   constexpr int V = E / 8 > kPer ? E / 8 : kPer, L = E / V, kRows = 64 / L, kLists = V / 8;
   constexpr int kSlow = E / kPer;               // lanes of a row that is looked at once more
@@ -462,15 +473,18 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
   const float none = -__builtin_inff();
   float most_bias = 0.0f;
   if (a.bias) {
-    for (int e = threadIdx.x; e < E; e += kScoredThreads) sh_bias[e] = a.bias[e];
+    for (int e = threadIdx.x; e < E; e += kScoredThreads) {
+      const float v = a.bias[e];
+      sh_bias[e] = v == v ? fminf(v, kLargest) : none;
+    }
     __syncthreads();
     for (int i = 0; i < V; ++i) {
       const float m = fabsf(sh_bias[l * V + i]);
-      most_bias = fmaxf(most_bias, m < -none ? m : 0.0f);
+      most_bias = fmaxf(most_bias, m < kLargest ? m : 0.0f);
     }
     most_bias = row_max<L>(most_bias);
   }
-  const bool by_groups = a.top_groups < a.groups, by_logits = a.bias == nullptr;
+  const bool by_groups = a.top_groups < a.groups, by_logits = a.bias == nullptr, ninth = a.K == 8;
   const int64_t step = (int64_t)gridDim.x * kScoredWaves * kRows;
   for (int64_t t0 = ((int64_t)blockIdx.x * kScoredWaves + wave) * kRows; t0 < a.T; t0 += step) {
     const bool live = t0 + lane / L < a.T;
@@ -482,7 +496,7 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       for (int j = 0; j < kPer; ++j) z[j] = clean(Logit<kDtype>::to_f(x[j]));
     };
     float top = 0.0f, total = 1.0f;
-    if (a.softmax) {
+    if (kSoftmax) {
       top = none;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
@@ -506,40 +520,45 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
         total = row_sum<L>(total);
       }
     }
-    // scores for the choice only: within 2^-18 of their value (or 2^-58)
+    // scores for the choice only, as near() says
     const float rcp_total = __builtin_amdgcn_rcpf(total);
     auto quick = [&](float x) {
       const float kLog2e = 1.44269502162933349609375f;
-      if (a.softmax) return __builtin_amdgcn_exp2f((x - top) * kLog2e) * rcp_total;
-      return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
+      if constexpr (kSoftmax) return __builtin_amdgcn_exp2f((x - top) * kLog2e) * rcp_total;
+      else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
     };
     bool doubt = false;
     double key[8], lost = __builtin_bit_cast(double, (uint64_t)kMaskedHigh << 32);
     // eight at a time, so that few registers are in use and many waves run
+    auto lists = [&](auto logits) {
 #pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-      float z[kPer];
-      piece(i, z);
-      double other[8], (&to)[8] = i == 0 ? key : other;
-      if (by_logits) {
+      for (int i = 0; i < kLists; ++i) {
+        const vec x = *reinterpret_cast<const vec*>(row + l * V + i * kPer);
+        double other[8], (&to)[8] = i == 0 ? key : other;
+        if constexpr (decltype(logits)::value) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) to[j] = key_of(z[j], l * V + i * kPer + j);
-      } else {
+          for (int j = 0; j < kPer; ++j) to[j] = key_of_logit(clean(Logit<kDtype>::to_f(x[j])), l * V + i * kPer + j);
+        } else {
 #pragma unroll
-        for (int j = 0; j < kPer; j += 4) {
-          const float4 b = *reinterpret_cast<const float4*>(&sh_bias[l * V + i * kPer + j]);
-          const float bs[4] = {b.x, b.y, b.z, b.w};
+          for (int j = 0; j < kPer; j += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(&sh_bias[l * V + i * kPer + j]);
+            const float bs[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const float q = quick(z[j + h]) + bs[h];
-            to[j + h] = key_of(z[j + h] > none && q == q ? q : none, l * V + i * kPer + j + h);
+            for (int h = 0; h < 4; ++h) {
+              // +inf gives a sigmoid of 1 as it is
+              const float z = kSoftmax ? clean(Logit<kDtype>::to_f(x[j + h])) : Logit<kDtype>::to_f(x[j + h]);
+              const float q = quick(z) + bs[h];
+              to[j + h] = key_of_score(z > none ? q : none, 224u - (uint32_t)(l * V), i * kPer + j + h);
+            }
           }
         }
+        sort8(to);
+        if (i > 0) merge8(key, other, lost, ninth);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      sort8(to);
-      if (i > 0) merge8<kNinth>(key, other, lost);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    };
+    if (by_logits) lists(std::integral_constant<bool, true>{});
+    else lists(std::integral_constant<bool, false>{});
     bool kept = true;
     if (by_groups) {
       auto score = [&](double k) { return key_masked(k) ? none : by_logits ? quick((float)k) : (float)k; };
@@ -559,8 +578,8 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       double other[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) other[i] = from_lane<d>(key[i]);
-      if constexpr (kNinth) lost = key_max(lost, from_lane<d>(lost));
-      merge8<kNinth>(key, other, lost);
+      if (ninth) lost = key_max(lost, from_lane<d>(lost));
+      merge8(key, other, lost, ninth);
     };
     if constexpr (L >= 2) meet(std::integral_constant<int, 1>{});
     if constexpr (L >= 4) meet(std::integral_constant<int, 2>{});
@@ -579,12 +598,12 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
         next = k == i ? (i < 7 ? key[i + 1 < 8 ? i + 1 : 7] : lost) : next;
       }
       const bool on = k < a.K && !key_masked(mine);
-      e[h] = on ? key_expert(mine) : -1;
-      if (!by_logits) doubt = doubt || (on && !key_masked(next) && near((float)mine, (float)next, most_bias));
+      e[h] = on ? key_expert(mine, by_logits) : -1;
+      if (!by_logits) doubt = doubt || (on && !key_masked(next) && near((float)mine, (float)next, most_bias, kSoftmax));
       s[h] = 0.0f;
       if (on) {
         const float x = clean(Logit<kDtype>::to_f(row[e[h]]));
-        s[h] = a.softmax ? exp_neg(top - x) : sigmoid_of(x);
+        s[h] = kSoftmax ? exp_neg(top - x) : sigmoid_of(x);
       }
       sum += s[h];
     }
@@ -608,17 +627,17 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       float zs[kPer], bs[kPer];
       load_row<E, kDtype>(a.z, tr, ls, zs);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) bs[i] = a.bias ? sh_bias[ls * kPer + i] : 0.0f;
+      for (int i = 0; i < kPer; ++i) bs[i] = a.bias ? a.bias[ls * kPer + i] : 0.0f;
       choose<kSlow, double>(a, zs, bs, most_bias, ls, sh_chosen[wave]);
       lds_wave_sync();
       float top_s = 0.0f, total_s = 1.0f;
-      if (a.softmax) softmax_of<kSlow, kDtype>(zs, top_s, total_s);
+      if (kSoftmax) softmax_of<kSlow, kDtype>(zs, top_s, total_s);
       const raw* at = static_cast<const raw*>(a.z) + tr * E;
       const int es = lane < a.K ? sh_chosen[wave][lane & 7] : -1;
       float ss = 0.0f;
       if (es >= 0) {
         const float x = clean(Logit<kDtype>::to_f(at[es]));
-        ss = a.softmax ? exp_neg(top_s - x) : sigmoid_of(x);
+        ss = kSoftmax ? exp_neg(top_s - x) : sigmoid_of(x);
       }
       const float by_s = a.normalize ? row_sum<8>(ss) : total_s;      // lanes 0 .. 7 hold them
       if (lane < a.K) {
@@ -729,7 +748,7 @@ void launch_eight(const ScoredArgs& a, hipStream_t s) {
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
   if (blocks > most) blocks = most;
-  if (a.K == 8) route_scored_eight_kernel<E, kDtype, true><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  if (a.softmax) route_scored_eight_kernel<E, kDtype, true><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
   else route_scored_eight_kernel<E, kDtype, false><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
 }
 
