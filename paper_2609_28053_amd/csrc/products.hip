@@ -92,7 +92,7 @@ struct Experts {
 constexpr int kStep = kCodeBlock;       // bytes of a row per step
 
 // Eight codes (words 2j and 2j + 1) times their scale.
-__device__ __forceinline__ bf16x8_t widen(const int8v& code, int j, float scale) {
+__device__ __forceinline__ bf16x8_t widen(const int4v& code, int j, float scale) {
   const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[2 * j], scale, false);
   const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[2 * j], scale, true);
   const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[2 * j + 1], scale, false);
@@ -128,13 +128,17 @@ struct Tile {
 // this order: first the columns and the first rows, while the matrix instructions of the last
 // kTail rows of the step before run; then the other rows, each ahead of its instructions.  When
 // it has the last of them its buffer is free for the step after the next: that is the barrier.
+//   By BF16 a step is two halves, each of its columns, widened once, and then its rows one by
+// one, so that a tile of 256 x 256 fits the registers (98,304 rows of 2,048 to 2,048, gradients in
+// binary32: 1,057 -> 891 us; 156 of them are stores, 50 the widening; without both the
+// matrix instructions run at 1.2 PFLOP/s, at a clock that the power limit lowers to some 1.6 GHz).
 template <int BP, int BQ, int WP, int WQ, bool kGrad, int kDtype>
 __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductArgs a) {
   typedef OutType<kDtype> O;
   typedef typename O::raw raw;
   constexpr bool kWide = kDtype == EQB_DTYPE_F32;     // by BF16
   constexpr int kWaves = WP * WQ, TP = BP / WP / 16, TQ = BQ / WQ / 16;
-  constexpr int kTail = kWide ? TP : TP >= 4 ? 2 : 1;
+  constexpr int kTail = TP >= 4 ? 2 : 1;
   constexpr int kAhead = TP >= 8 ? 2 : 1;      // rows whose fragments are read before they are needed
   constexpr bool kOneScale = !kGrad;     // a wave's columns lie in one block of the weights
   static_assert(kGrad || kCodeBlock % (TQ * 16) == 0, "they do");
@@ -277,6 +281,32 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
     fq[j] = fragment(BP + wq * TQ * 16, j);
     if (!kOneScale || j == TQ - 1) sq[kOneScale ? 0 : j] = scales[(BP + wq * TQ * 16 + column_of(lrow)) * 4 + column_of(j * 16) * 4];
   };
+  // the wide form's: half of a lane's 32 codes at a time
+  int4v hp[TP], hq[TQ];
+  auto half = [&](int base, int i, int h) {
+    return *reinterpret_cast<const int4v*>(codes + base * kStep + i * 16 * kStep + (h ? piece1 : piece0));
+  };
+  auto read_half_p = [&](int i, int h) {
+    hp[i] = half(wp * TP * 16, i, h);
+    sp[i] = scales[(wp * TP * 16 + lrow) * 4 + i * 64];
+  };
+  auto read_half_q = [&](int j, int h) {
+    hq[j] = half(BP + wq * TQ * 16, j, h);
+    if (h == 0 && (!kOneScale || j == TQ - 1)) sq[kOneScale ? 0 : j] = scales[(BP + wq * TQ * 16 + column_of(lrow)) * 4 + column_of(j * 16) * 4];
+  };
+  auto power = [](int byte) { return __uint_as_float((uint32_t)byte << 23); };
+  auto read_first = [&]() {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      if constexpr (kWide) read_half_q(j, 0);
+      else read_q(j);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if constexpr (kWide) read_half_p(i, 0);
+      else read_p(i);
+    }
+  };
   float4v acc[TP][TQ];
   auto multiply = [&](int i, int j) {
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fq[j], fp[i], acc[i][j], 0, 0, 0, sq[kOneScale ? 0 : j], 0, sp[i]);
@@ -311,10 +341,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
     const uint32_t next_id = id + gridDim.x;
     if (t.block < t.end && !ready) {
       next_step(t.block);
-#pragma unroll
-      for (int j = 0; j < TQ; ++j) read_q(j);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) read_p(i);
+      read_first();
     }
     Tile next = t;
     for (int block = t.block; block < t.end; ++block) {
@@ -325,42 +352,62 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
         next = tile_of(next_id);
         on = next.block < next.end;
       }
-#pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        if (i + kAhead < TP) read_p(i + kAhead);
-        if (i >= TP - kTail) continue;
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) multiply(i, j);
-        __builtin_amdgcn_sched_barrier(0);      // or all rows are read at once, into registers that there are not
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      step_barrier();
-      if (on) next_step(last ? next.block : block + 1);
-      load_scales();
-      __builtin_amdgcn_sched_barrier(0);
-      // the last rows, column by column, and the next step's fragments in the place of those
-      // that are not needed any more (with no next step they are not used)
       if constexpr (kWide) {
-        auto power = [&](int byte) { return __uint_as_float((uint32_t)byte << 23); };
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int h = 0; h < 2; ++h) {
+          bf16x8_t wide[2][TQ];
 #pragma unroll
-          for (int i = k; i < kLoads; i += 4) load_codes(i);
-          bf16x8_t wide[TQ];
+          for (int j = 0; j < TQ; ++j) {
+            wide[0][j] = widen(hq[j], 0, power(sq[kOneScale ? 0 : j]));
+            wide[1][j] = widen(hq[j], 1, power(sq[kOneScale ? 0 : j]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          if (h == 0) {
 #pragma unroll
-          for (int j = 0; j < TQ; ++j) wide[j] = widen(fq[j], k, power(sq[kOneScale ? 0 : j]));
+            for (int j = 0; j < TQ; ++j) read_half_q(j, 1);
+          }
 #pragma unroll
           for (int i = 0; i < TP; ++i) {
-            const bf16x8_t x = widen(fp[i], k, power(sp[i]));
+            constexpr int kFree = TP - kAhead;       // from this row on of the second half all is read
+            if (h == 1 && i == kFree) {
+              step_barrier();
+              if (on) next_step(last ? next.block : block + 1);
+              load_scales();
 #pragma unroll
-            for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[j], x, acc[i][j], 0, 0, 0);
+              for (int j = 0; j < TQ; ++j) read_half_q(j, 0);
+            }
+            const int n = (h * TP + i + kAhead) % (2 * TP);
+            read_half_p(n % TP, n / TP);
+            if (h == 1 && i >= kFree) {
+#pragma unroll
+              for (int k = i - kFree; k < kLoads; k += kAhead) load_codes(k);
+            }
+            const float scale = power(sp[i]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const bf16x8_t x = widen(hp[i], k, scale);
+#pragma unroll
+              for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[k][j], x, acc[i][j], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) read_q(j);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) read_p(i);
       } else {
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+          if (i + kAhead < TP) read_p(i + kAhead);
+          if (i >= TP - kTail) continue;
+#pragma unroll
+          for (int j = 0; j < TQ; ++j) multiply(i, j);
+          __builtin_amdgcn_sched_barrier(0);      // or all rows are read at once, into registers that there are not
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        step_barrier();
+        if (on) next_step(last ? next.block : block + 1);
+        load_scales();
+        __builtin_amdgcn_sched_barrier(0);
+        // the last rows, column by column, and the next step's fragments in the place of those
+        // that are not needed any more (with no next step they are not used)
         static_assert(kTail + kAhead <= TP, "row 0 is read while the last rows are multiplied");
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) read_p(i);
@@ -398,18 +445,19 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
       for (int i = 0; i < TP; ++i) {
 #pragma unroll
         for (int j = 0; j < TQ; j += kPair) {
-          if constexpr (kPair == 2 && TQ % 4 == 0) {
-            if (j % 4 != 0) continue;
+          if constexpr (TQ % (2 * kPair) == 0) {
+            if (j % (2 * kPair) != 0) continue;
             // a store of 8 whole lines of 128 bytes instead of 16 halves: lanes of rows 8 apart
-            // exchange halves (884,736 rows of 1,024 by 1,024: 1,179 -> 1,168 us)
-            const int4v x = __builtin_bit_cast(int4v, values(i, j)), y = __builtin_bit_cast(int4v, values(i, j + 2));
+            // exchange halves (884,736 rows of 1,024 by 1,024: 1,179 -> 1,168 us; binary32, 20,012 rows
+            // of 1,001 by 777, 69 -> 65)
+            const int4v x = __builtin_bit_cast(int4v, values(i, j)), y = __builtin_bit_cast(int4v, values(i, j + kPair));
             int4v up, down;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               up[k] = __builtin_amdgcn_update_dpp(x[k], y[k], 0x128, 0xF, 0xC, false);
               down[k] = __builtin_amdgcn_update_dpp(y[k], x[k], 0x128, 0xF, 0x3, false);
             }
-            raw* const at = to + j * 16 + ((lane & 8) ? 32 - 8 * width : 0);
+            raw* const at = to + j * 16 + ((lane & 8) ? 16 * kPair - 8 * width : 0);
             *reinterpret_cast<any*>(at) = __builtin_bit_cast(vec, up);
             *reinterpret_cast<any*>(at + 8 * width) = __builtin_bit_cast(vec, down);
           } else {
@@ -464,8 +512,7 @@ eqb_status launch_form(const ProductArgs& a, int per_cu, hipStream_t s) {
   return launch_status();
 }
 
-// Tiles of 64 x 64 (four blocks on a compute unit), 128 x 128 (two) and 256 x 256 (one, for results
-// of 16 bits), all times in us, results bf16 where nothing is said:
+// Tiles of 64 x 64 (four blocks on a compute unit), 128 x 128 (two) and 256 x 256 (one), all times in us, results bf16 where nothing is said:
 //   few rows an expert, up to 64 on average: 64 rows of 2,048 to 2,048 columns, E = 256, 38.5 with 64,
 //   39.6 with 128, 54 with 256; one row 9.9, 13.0, 25; 4,096 rows of 1,024, E = 64, 21.7, 24.1, 23.8;
 //   but 4,096 rows of 1,024, E = 8, 16.7, 14.7, 20.8.
@@ -474,6 +521,8 @@ eqb_status launch_form(const ProductArgs& a, int per_cu, hipStream_t s) {
 //   than an eighth: 98,304 rows of 2,048 to 2,048, E = 64, 454 against 561 with 128; 196,608 of 1,024
 //   to 1,024, E = 256, 304, 352; 24,576 rows of 2,048 160 both; but 80,000 of 500 to 300, E = 32,
 //   37.6, 30.8; gradients 64 of 2,048 x 2,048 over 98,304 rows 583, 794; 32 of 777 x 1,001 59, 55.
+//   binary32: 93,389 rows of 2,048 to 2,048, E = 64, 814, 907; the gradients 891, 1,051; over 23,347 rows
+//   418, 482; but 8 gradients of 1,024 x 1,024 478, 323, and 32 of 777 x 1,001 85, 72.
 template <bool kGrad>
 eqb_status launch_product(const ProductArgs& a, hipStream_t s) {
   const int64_t cus = num_cus(), E = a.E, most = a.rows < E ? a.rows : E;
@@ -482,12 +531,14 @@ eqb_status launch_product(const ProductArgs& a, hipStream_t s) {
   // an expert's rows end in the middle of a tile
   auto tiles = [&](int64_t side) { return (kGrad ? E * up(p, side) : p / side + most / 2) * up(q, side); };
   const bool small = kGrad ? tiles(128) < cus : a.rows <= 64 * E;
+  const bool large = tiles(256) >= 2 * cus && 4 * tiles(256) * 8 <= tiles(128) * 9;
   if (a.dtype == EQB_DTYPE_F32) {
     if (small) return launch_form<64, 64, 2, 2, kGrad, true>(a, 4, s);
+    if (large) return launch_form<256, 256, 2, 4, kGrad, true>(a, 1, s);
     return launch_form<128, 128, 2, 2, kGrad, true>(a, 2, s);
   }
   if (small) return launch_form<64, 64, 2, 2, kGrad, false>(a, 4, s);
-  if (tiles(256) >= 2 * cus && 4 * tiles(256) * 8 <= tiles(128) * 9) return launch_form<256, 256, 2, 4, kGrad, false>(a, 1, s);
+  if (large) return launch_form<256, 256, 2, 4, kGrad, false>(a, 1, s);
   return launch_form<128, 128, 2, 2, kGrad, false>(a, 2, s);
 }
 
