@@ -112,15 +112,16 @@ struct PlainRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = false;
   template <bool kExact>
-  static __device__ __forceinline__ void load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     load8<kDtype>(static_cast<const raw*>(a.x) + t * a.H, c, a.H, v);
+    return false;
   }
 };
-// A gated value that is to become a code is computed in binary32, within 11 2^-24 (a sigmoid 8, three
-// roundings).  Where that leaves open which of two codes it is, some six in a hundred thousand, it is computed
-// once more to 37 bits and rounded to the odd neighbour in binary32, so that the code's rounding is as if it
-// were the only one.  The exponential is then its series to y^9 for |y| <= ln 2 / 2 (off by 7e-12).  98,304
-// rows of 2,048 bf16: 291 us; all of them to 37 bits 385.
+// A gated value that is to become a code is computed in binary32, within 11 2^-24 for gates above -80 (a
+// sigmoid 8, three roundings).  Where that leaves open which of two codes it is, some six in a hundred
+// thousand, and for lower gates, it is computed once more to 37 bits and rounded to the odd neighbour in
+// binary32, so that the code's rounding is as if it were the only one.  The exponential is then its series to
+// y^9 for |y| <= ln 2 / 2 (off by 7e-12).  98,304 rows of 2,048 bf16: 291 us; all of them to 37 bits 385.
 __device__ __forceinline__ double sigmoid_wide(double x) {
   const double a = fmin(fabs(x), 200.0), n = __builtin_rint(a * 1.4426950408889634);
   const double y = __builtin_fma(n, 0.6931471805599453, -a);
@@ -144,8 +145,9 @@ template <int kDtype>
 struct GatedRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = true;        // its values are not exact
+  // whether a gate is so low that its sigmoid has fewer than 24 bits in binary32
   template <bool kExact>
-  static __device__ __forceinline__ void load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
     float g[kPer], u[kPer];
     load8<kDtype>(row, c, a.H, g);
@@ -160,6 +162,10 @@ struct GatedRow {
         v[i] = g[i] * s * u[i];
       }
     }
+    float least = g[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) least = fminf(least, g[i]);
+    return least < -80.0f;
   }
 };
 
@@ -192,12 +198,12 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
         byte = scale_byte(top);
         code = codes(scale_inverse(byte));
       };
-      Row::template load<false>(a, t, c, v);
+      const bool low = Row::template load<false>(a, t, c, v);
       encode();
       if constexpr (Row::kOpen) {
         constexpr float kLess = 1.0f - 0x1p-19f, kMore = 1.0f + 0x1p-19f;
         const uint2 less = codes(scale_inverse(byte) * kLess), more = codes(scale_inverse(byte) * kMore);
-        const bool open = less.x != more.x || less.y != more.y || scale_byte(top * kLess) != scale_byte(top * kMore);
+        const bool open = low || less.x != more.x || less.y != more.y || scale_byte(top * kLess) != scale_byte(top * kMore);
         if (__ballot(open)) {
           Row::template load<true>(a, t, c, v);
           encode();
@@ -306,7 +312,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
     begin = begin < 0 ? 0 : begin > a.rows ? a.rows : begin;
     end = end > a.rows ? a.rows : end;
     const int64_t local = ((int64_t)by - (begin / kCodeBlock + e)) * kCodeBlock;
-    if (local >= end - begin) return;
+    if (local < 0 || local >= end - begin) return;
     first = (int)local;
     base = begin;
     nr = (int)(end - begin - local);

@@ -249,3 +249,35 @@ def test_streams_and_blocks(eqb):  # noqa: F811
         finally:
             eqb.eqb_set_max_blocks(0)
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("low", [False, True])
+def test_gated_codes_are_the_exact_products(eqb, dtype, low):  # noqa: F811
+    """Bit for bit the codes of the products in 64 bits, of ordinary gates and of gates whose sigmoid has few bits or
+    none in 32 (2^-52 to 2^-126 there: the products of 37 bits leave one code in 2^32 open, and none of these)."""
+    say(f"exact gated codes {dtype} low={low}")
+    rng = np.random.default_rng(40 + low)
+    R, F = 300, 1000
+    g = rng.uniform(-94, -82, size=(R, 1)) + rng.uniform(-3, 3, size=(R, F)) if low else rng.normal(size=(R, F)) * 3
+    u = rng.normal(size=(R, F)) * (np.exp2(rng.integers(2, 9, size=(R, F))) if low else 1.0)
+    x = torch.from_numpy(np.concatenate([g, u], 1)).to(TYPES[dtype]).cuda()
+    codes, scales = buffers(eqb, (R,), F)
+    eqb.eqb_gated_quantize(x, codes, scales)
+    wc, ws = O.quantize_rows(O.gated(f64(x)))
+    assert (wc[:, :F] & 127 != 0).mean() > 0.5
+    assert same_codes(raw(codes), wc) and np.array_equal(raw(scales), ws)
+
+
+def test_columns_of_descending_offsets(eqb):  # noqa: F811
+    """Offsets that do not ascend name no rows: nothing is read or written before or behind the rows."""
+    say("columns of descending offsets")
+    R, H = 400, 70
+    around = torch.full((3 * R, H), 3.0, device="cuda")
+    x = around[R:2 * R].fill_(1.0)
+    for off in ([0, 390, 130, 400], [400, 0, 400, 0], [300, 300, 10, 10], [-5, 900, 200, -1]):
+        codes, scales = buffers(eqb, (H + 1,), eqb.eqb_column_width(R, 3))
+        eqb.eqb_quantize_columns(x, torch.tensor(off, dtype=torch.int32, device="cuda"), codes[:-1], scales[:-1])
+        # the fill, zeros, and 1 = 256 2^-8
+        assert np.isin(raw(codes), [0xA5, 0, 0x78]).all() and np.isin(raw(scales), [0xA5, 119]).all()
+        assert (raw(codes)[-1] == 0xA5).all() and (raw(scales)[-1] == 0xA5).all()
