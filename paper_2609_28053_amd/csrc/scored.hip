@@ -337,16 +337,16 @@ __device__ __forceinline__ void softmax_of(const float (&z)[V], float& top, floa
   total = row_sum<L>(total);
 }
 
-// ------------------------------------------------------ up to eight experts --
+// ---------------------------------------------------- up to sixteen experts --
 // Keys are binary64: a binary32 score with its expert's place in the low bits, so that one maximum
 // and one minimum order two of them, ties to the lower expert.  A row lies in L lanes of V experts
-// each; a lane sorts its keys in eights, merges those to its best eight, and the lanes' eights are
-// merged in pairs.  It is bound by the issue of instructions and of the waves that wait for their rows:
-// 147,456 tokens of 256 experts, 8 groups, K = 6, bf16 logits, at four waves on a SIMD: 55 us (1.4 TB/s;
-// the bytes alone take 15), K = 8 60, without groups 47, without a bias as well 35, a softmax 77.  Where
-// a wider bound of doubt sent more rows to binary64: four waves 68, five 70, six 79, two waves with all
-// 32 keys of a lane in registers 151.  With K rounds of a maximum
-// over 32 lanes, as above, 215.
+// each; a lane sorts its keys in lists of N (8, or 16 for K above 8), merges those to its best N, and
+// the lanes' lists are merged in pairs.  It is bound by the issue of instructions and of the waves that
+// wait for their rows: 147,456 tokens of 256 experts, 8 groups, K = 6, bf16 logits, at four waves on a
+// SIMD: 55 us (1.4 TB/s; the bytes alone take 15), K = 8 60, without groups 47, without a bias as well 35,
+// a softmax 77; K = 12 77 and K = 16 82 at three waves, 80 and 84 at four, 89 and 94 at two.  Where a wider
+// bound of doubt sent more rows to binary64: K = 6 at four waves 68, five 70, six 79, two waves with all
+// 32 keys of a lane in registers 151.  With K rounds of a maximum over 32 lanes, as above, K = 6 215, K = 12 280.
 __device__ __forceinline__ double key_max(double a, double b) {
   double r;
   asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -387,20 +387,36 @@ __device__ __forceinline__ void sort8(double* k) {
 #pragma unroll
   for (int i = 0; i < 19; ++i) order(k[pairs[i][0]], k[pairs[i][1]]);
 }
-// The best eight of two sorted eights, sorted, in a; lost: the largest of those that are not among
-// them (ninth: eight are to be chosen, and how near the next one is matters).
-__device__ __forceinline__ void merge8(double* a, const double* b, double& lost, bool ninth) {
-  if (ninth) {
+// What is sorted but for a turn in its middle, sorted.
+template <int N>
+__device__ __forceinline__ void straighten(double* k) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lost = key_max(lost, key_min(a[i], b[7 - i]));
+  for (int d = N / 2; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((i & d) == 0) order(k[i], k[i + d]);
+}
+// Sixteen keys; eight (half), the others masked.
+__device__ __forceinline__ void sort16(double* k, bool half) {
+  sort8(k);
+  if (half) return;
+  sort8(k + 8);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) order(k[i], k[15 - i]);
+  straighten<8>(k);
+  straighten<8>(k + 8);
+}
+// The best N of two sorted N, sorted, in a; lost: the largest of those that are not among
+// them (more: N are to be chosen, and how near the next one is matters).
+template <int N>
+__device__ __forceinline__ void merge(double* a, const double* b, double& lost, bool more) {
+  if (more) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) lost = key_max(lost, key_min(a[i], b[N - 1 - i]));
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = key_max(a[i], b[7 - i]);
-#pragma unroll
-  for (int d = 4; d > 0; d >>= 1)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((i & d) == 0) order(a[i], a[i + d]);
+  for (int i = 0; i < N; ++i) a[i] = key_max(a[i], b[N - 1 - i]);
+  straighten<N>(a);
 }
 template <int kCtrl, class T>
 __device__ __forceinline__ T moved(T x) {
@@ -460,14 +476,15 @@ __device__ __forceinline__ bool group_kept(const ScoredArgs& a, float t1, float 
   return kept;
 }
 
-template <int E, int kDtype, bool kSoftmax>
-__global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(const ScoredArgs a) {
-  constexpr int V = E / 8 > kPer ? E / 8 : kPer, L = E / V, kRows = 64 / L, kLists = V / 8;
+template <int E, int kDtype, bool kSoftmax, int N>
+__global__ __launch_bounds__(kScoredThreads, N == 8 ? 4 : 3) void route_scored_best_kernel(const ScoredArgs a) {
+  constexpr int V = E / 8 > kPer ? E / 8 : kPer, L = E / V, kRows = 64 / L, kPieces = V / 8;
+  constexpr int kLists = V > N ? V / N : 1, kListPieces = kPieces / kLists;       // a lane's lists of N
   constexpr int kSlow = E / kPer;               // lanes of a row that is looked at once more
   typedef typename Logit<kDtype>::raw raw;
   typedef raw vec __attribute__((ext_vector_type(kPer)));
   __shared__ __attribute__((aligned(16))) float sh_bias[E];
-  __shared__ int16_t sh_chosen[kScoredWaves][8];
+  __shared__ int16_t sh_chosen[kScoredWaves][N];
   const int lane = threadIdx.x & 63, l = lane % L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float none = -__builtin_inff();
@@ -484,7 +501,7 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
     }
     most_bias = row_max<L>(most_bias);
   }
-  const bool by_groups = a.top_groups < a.groups, by_logits = a.bias == nullptr, ninth = a.K == 8;
+  const bool by_groups = a.top_groups < a.groups, by_logits = a.bias == nullptr, more = a.K == N;
   const int64_t step = (int64_t)gridDim.x * kScoredWaves * kRows;
   for (int64_t t0 = ((int64_t)blockIdx.x * kScoredWaves + wave) * kRows; t0 < a.T; t0 += step) {
     const bool live = t0 + lane / L < a.T;
@@ -499,7 +516,7 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
     if (kSoftmax) {
       top = none;
 #pragma unroll
-      for (int i = 0; i < kLists; ++i) {
+      for (int i = 0; i < kPieces; ++i) {
         float z[kPer];
         piece(i, z);
 #pragma unroll
@@ -510,7 +527,7 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       if (!a.normalize || !by_logits || by_groups) {        // else the sum is not needed
         total = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kLists; ++i) {
+        for (int i = 0; i < kPieces; ++i) {
           float z[kPer];
           piece(i, z);
 #pragma unroll
@@ -528,32 +545,43 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
     };
     bool doubt = false;
-    double key[8], lost = __builtin_bit_cast(double, (uint64_t)kMaskedHigh << 32);
-    // eight at a time, so that few registers are in use and many waves run
+    const double masked = __builtin_bit_cast(double, (uint64_t)kMaskedHigh << 32);
+    double key[N], lost = masked;
+    // N at a time, so that few registers are in use and many waves run
     auto lists = [&](auto logits) {
 #pragma unroll
-      for (int i = 0; i < kLists; ++i) {
-        const vec x = *reinterpret_cast<const vec*>(row + l * V + i * kPer);
-        double other[8], (&to)[8] = i == 0 ? key : other;
-        if constexpr (decltype(logits)::value) {
+      for (int n = 0; n < kLists; ++n) {
+        double other[N], (&list)[N] = n == 0 ? key : other;
 #pragma unroll
-          for (int j = 0; j < kPer; ++j) to[j] = key_of_logit(clean(Logit<kDtype>::to_f(x[j])), l * V + i * kPer + j);
-        } else {
+        for (int h = 0; h < kListPieces; ++h) {
+          const int i = n * kListPieces + h;
+          const vec x = *reinterpret_cast<const vec*>(row + l * V + i * kPer);
+          double* const to = list + h * kPer;
+          if constexpr (decltype(logits)::value) {
 #pragma unroll
-          for (int j = 0; j < kPer; j += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(&sh_bias[l * V + i * kPer + j]);
-            const float bs[4] = {b.x, b.y, b.z, b.w};
+            for (int j = 0; j < kPer; ++j) to[j] = key_of_logit(clean(Logit<kDtype>::to_f(x[j])), l * V + i * kPer + j);
+          } else {
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              // +inf gives a sigmoid of 1 as it is
-              const float z = kSoftmax ? clean(Logit<kDtype>::to_f(x[j + h])) : Logit<kDtype>::to_f(x[j + h]);
-              const float q = quick(z) + bs[h];
-              to[j + h] = key_of_score(z > none ? q : none, 224u - (uint32_t)(l * V), i * kPer + j + h);
+            for (int j = 0; j < kPer; j += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(&sh_bias[l * V + i * kPer + j]);
+              const float bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
+                // +inf gives a sigmoid of 1 as it is
+                const float z = kSoftmax ? clean(Logit<kDtype>::to_f(x[j + m])) : Logit<kDtype>::to_f(x[j + m]);
+                const float q = quick(z) + bs[m];
+                to[j + m] = key_of_score(z > none ? q : none, 224u - (uint32_t)(l * V), i * kPer + j + m);
+              }
             }
           }
         }
-        sort8(to);
-        if (i > 0) merge8(key, other, lost, ninth);
+        if constexpr (N == 8) sort8(list);
+        else {
+#pragma unroll
+          for (int i = kListPieces * kPer; i < N; ++i) list[i] = masked;
+          sort16(list, kListPieces == 1);
+        }
+        if (n > 0) merge<N>(key, other, lost, more);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -570,22 +598,22 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
     };
     if (by_groups) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) key[i] = drop(key[i]);
+      for (int i = 0; i < N; ++i) key[i] = drop(key[i]);
       lost = drop(lost);
     }
     auto meet = [&](auto x) {
       constexpr int d = decltype(x)::value;
-      double other[8];
+      double other[N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) other[i] = from_lane<d>(key[i]);
-      if (ninth) lost = key_max(lost, from_lane<d>(lost));
-      merge8(key, other, lost, ninth);
+      for (int i = 0; i < N; ++i) other[i] = from_lane<d>(key[i]);
+      if (more) lost = key_max(lost, from_lane<d>(lost));
+      merge<N>(key, other, lost, more);
     };
     if constexpr (L >= 2) meet(std::integral_constant<int, 1>{});
     if constexpr (L >= 4) meet(std::integral_constant<int, 2>{});
     if constexpr (L >= 8) meet(std::integral_constant<int, 7>{});    // the four lanes of a half have the same
     // the k-th best to lane k (and k + L, ...)
-    constexpr int kEach = 8 / L > 1 ? 8 / L : 1;
+    constexpr int kEach = N / L > 1 ? N / L : 1;
     int e[kEach];
     float s[kEach], sum = 0.0f;
 #pragma unroll
@@ -593,9 +621,9 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       const int k = l + h * L;
       double mine = key[0], next = key[1];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) {
+      for (int i = 1; i < N; ++i) {
         mine = k == i ? key[i] : mine;
-        next = k == i ? (i < 7 ? key[i + 1 < 8 ? i + 1 : 7] : lost) : next;
+        next = k == i ? (i + 1 < N ? key[i + 1 < N ? i + 1 : 0] : lost) : next;
       }
       const bool on = k < a.K && !key_masked(mine);
       e[h] = on ? key_expert(mine, by_logits) : -1;
@@ -633,13 +661,13 @@ __global__ __launch_bounds__(kScoredThreads, 4) void route_scored_eight_kernel(c
       float top_s = 0.0f, total_s = 1.0f;
       if (kSoftmax) softmax_of<kSlow, kDtype>(zs, top_s, total_s);
       const raw* at = static_cast<const raw*>(a.z) + tr * E;
-      const int es = lane < a.K ? sh_chosen[wave][lane & 7] : -1;
+      const int es = lane < a.K ? sh_chosen[wave][lane & (N - 1)] : -1;
       float ss = 0.0f;
       if (es >= 0) {
         const float x = clean(Logit<kDtype>::to_f(at[es]));
         ss = kSoftmax ? exp_neg(top_s - x) : sigmoid_of(x);
       }
-      const float by_s = a.normalize ? row_sum<8>(ss) : total_s;      // lanes 0 .. 7 hold them
+      const float by_s = a.normalize ? row_sum<N>(ss) : total_s;      // lanes 0 .. N - 1 hold them
       if (lane < a.K) {
         a.idx[tr * a.K + lane] = es;
         a.weight[tr * a.K + lane] = by_s > 0.0f ? a.scale * (ss / by_s) : 0.0f;
@@ -741,15 +769,15 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(c
   }
 }
 
-template <int E, int kDtype>
-void launch_eight(const ScoredArgs& a, hipStream_t s) {
+template <int E, int kDtype, int N>
+void launch_best(const ScoredArgs& a, hipStream_t s) {
   constexpr int V = E / 8 > kPer ? E / 8 : kPer, kRows = 64 / (E / V) * kScoredWaves;
   int64_t blocks = (a.T + kRows - 1) / kRows, most = (int64_t)num_cus() * 8;
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
   if (blocks > most) blocks = most;
-  if (a.softmax) route_scored_eight_kernel<E, kDtype, true><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
-  else route_scored_eight_kernel<E, kDtype, false><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  if (a.softmax) route_scored_best_kernel<E, kDtype, true, N><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
+  else route_scored_best_kernel<E, kDtype, false, N><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
 }
 
 template <int E, int kDtype>
@@ -759,11 +787,13 @@ eqb_status launch_scored_e(const ScoredArgs& a, bool backward, hipStream_t s) {
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
   if (blocks > most) blocks = most;
-  // whole lanes of a group, and up to eight experts
+  // sorted lists: up to 16 experts, of groups that fill lanes
   constexpr int V = E / 8 > kPer ? E / 8 : kPer;
-  const bool eight = a.K <= 8 && (a.top_groups == a.groups || a.E / a.groups >= V);
+  const bool lanes = a.top_groups == a.groups || a.E / a.groups >= V;
+  constexpr int kMost = E > 8 ? 16 : 8;
   if (backward) route_scored_backward_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
-  else if (eight) launch_eight<E, kDtype>(a, s);
+  else if (lanes && a.K <= 8) launch_best<E, kDtype, 8>(a, s);
+  else if (lanes && a.K <= kMost) launch_best<E, kDtype, kMost>(a, s);
   else route_scored_kernel<E, kDtype><<<(uint32_t)blocks, kScoredThreads, 0, s>>>(a);
   return launch_status();
 }

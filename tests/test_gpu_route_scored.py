@@ -100,6 +100,43 @@ def test_route(eqb, T, E, K, groups, keep, pair, dtype, data, bias, softmax, nor
     assert (np.abs(gz.cpu().numpy() - grad) <= tol).all()
 
 
+MORE = [  # the same for up to sixteen experts, in lanes of 8, 16 and 32 of them
+    (1, 16, 9, 1, 1, 1, "bf16", "normal", "none", False, True), (70, 16, 15, 2, 2, 1, "f32", "masked", "normal", False, True),
+    (33, 16, 10, 2, 2, 2, "bf16", "ties", "steps", True, True), (200, 32, 16, 4, 3, 2, "f16", "ties", "none", False, True),
+    (129, 64, 10, 4, 2, 2, "bf16", "masked", "steps", False, True), (300, 64, 16, 1, 1, 1, "bf16", "ties", "zero", False, False),
+    (90, 128, 9, 8, 3, 2, "f32", "normal", "normal", True, True), (65, 128, 16, 2, 1, 1, "bf16", "masked", "normal", True, False),
+    (257, 256, 12, 8, 4, 2, "bf16", "normal", "normal", False, True), (1000, 256, 16, 8, 4, 2, "bf16", "ties", "steps", False, True),
+    (64, 256, 16, 1, 1, 1, "f32", "wide", "none", False, True), (100, 256, 13, 4, 1, 2, "f16", "masked", "none", True, True),
+    (3, 256, 11, 8, 1, 1, "bf16", "normal", "large", False, True), (400, 256, 17, 8, 4, 2, "bf16", "normal", "normal", False, True)]
+
+
+@pytest.mark.parametrize("T,E,K,groups,keep,pair,dtype,data,bias,softmax,normalize", MORE)
+def test_route_of_more(eqb, T, E, K, groups, keep, pair, dtype, data, bias, softmax, normalize):  # noqa: F811
+    say(f"route T={T} E={E} K={K} groups={groups},{keep},{pair} {dtype} {data} bias {bias} softmax={softmax}")
+    zt, bt = make(T * 3 + E + K, T, E, dtype, data, bias)
+    args = (K, softmax, groups, keep, pair, normalize)
+    idx, w = run(eqb, zt, bt, *args)
+    check(zt, bt, idx, w, *args)
+
+
+def test_near_scores_of_more(eqb):  # noqa: F811
+    """The K-th and the next of K = 9, 12, 15 and 16, within 2^-26 to 2^-40 of each other."""
+    say("near scores of more")
+    rng = np.random.default_rng(5)
+    T, E = 300, 256
+    zt = torch.from_numpy(np.float32(rng.normal(size=(T, E)))).to(torch.bfloat16)
+    s = O.scores(zt.to(torch.float64).numpy(), False)
+    for trial, K in enumerate((9, 12, 15, 16) * 2):
+        b = rng.normal(size=E) * 0.1
+        t = trial * 11
+        top = np.argsort(-(s[t] + b))
+        b[top[40]] += (s[t, top[K]] + b[top[K]]) - (s[t, top[40]] + b[top[40]]) + rng.choice([-1, 1]) * 2.0 ** -rng.integers(26, 40)
+        bt = torch.from_numpy(b.astype(np.float32)).cuda()
+        for groups, keep in ((1, 1), (8, 5)):
+            idx, w = run(eqb, zt.cuda(), bt, K, False, groups, keep, 2, True)
+            check(zt, bt, idx, w, K, False, groups, keep, 2, True)
+
+
 def test_near_scores_are_ordered_as_in_64_bits(eqb):  # noqa: F811
     """Logits and biases made so that score plus bias of two experts differ by 2^-26 to 2^-40, both ways."""
     say("near scores")
