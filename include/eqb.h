@@ -608,7 +608,8 @@ eqb_status eqb_gated_backward(const void* grad_h, const void* x, const int32_t* 
 /*
  * Test control (host only, no HIP call): caps the number of blocks of the
  * streaming kernels (routing, the margin passes, the LEI kernels, the balance
- * loss and its gradient, the experts' rows) at max_blocks for the calls that
+ * loss and its gradient, the experts' rows, their codes by rows, gates and
+ * products) at max_blocks for the calls that
  * follow FROM THE CALLING HOST THREAD; calls made from other threads keep their
  * own setting (the default 0: a whole number of blocks per compute unit).
  * Results do not depend on it, but for the last bits of the balance loss's

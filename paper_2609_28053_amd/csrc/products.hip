@@ -486,7 +486,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
         to += 16 * width;
       }
     }
-    if (next_id >= tiles) return;
+    if (next_id >= tiles) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the last loads to LDS, before it is another block's
+      return;
+    }
     if (t.block == t.end) {
       next = tile_of(next_id);
       ready = false;
