@@ -272,16 +272,25 @@ __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, i
 // codes in the rows' order too.
 constexpr int kTileStride = kCodeBlock + 4;        // bytes of a column in LDS: 33 words, so that columns 8 apart differ by 8 banks
 
-// The expert whose blocks of columns hold block b: the last one whose first block is at most b.
-__device__ __forceinline__ int expert_of_block(const int32_t* offsets, int E, int64_t rows, int64_t b, int lane) {
-  int n = 0;
+// The expert whose blocks of columns hold block b, the last one whose first block is at most b, and its rows
+// (e = -1: none).  By a whole wave, with one wait for the offsets.
+__device__ __forceinline__ void expert_of_block(const int32_t* offsets, int E, int64_t rows, int64_t b, int lane, int& e,
+                                                int64_t& begin, int64_t& end) {
+  e = -1;
+  begin = end = 0;
   for (int e0 = 0; e0 < E; e0 += 64) {
-    const int e = e0 + lane;
-    int64_t off = e < E ? offsets[e] : 0;
-    off = off < 0 ? 0 : off > rows ? rows : off;
-    n += __popcll(__ballot(e < E && off / kCodeBlock + e <= b));
+    const int i = e0 + lane;
+    const int from = i < E ? offsets[i] : 0, to = i < E ? offsets[i + 1] : 0;
+    const int64_t off = from < 0 ? 0 : from > rows ? rows : from;
+    const uint64_t up_to = __ballot(i < E && off / kCodeBlock + i <= b);
+    if (up_to == 0) break;
+    const int last = 63 - __builtin_clzll(up_to);
+    e = e0 + last;
+    begin = __builtin_amdgcn_readlane(from, last);
+    end = __builtin_amdgcn_readlane(to, last);
   }
-  return n - 1;
+  begin = begin < 0 ? 0 : begin > rows ? rows : begin;
+  end = end > rows ? rows : end;
 }
 
 template <int kDtype, bool kWeights, int kRows, int kCols>
@@ -306,11 +315,9 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
     base = (int64_t)e * a.N;
     nr = a.N - first;
   } else {
-    e = expert_of_block(a.offsets, a.E, a.rows, by, lane);
+    int64_t begin, end;
+    expert_of_block(a.offsets, a.E, a.rows, by, lane, e, begin, end);
     if (e < 0) return;
-    int64_t begin = a.offsets[e], end = a.offsets[e + 1];
-    begin = begin < 0 ? 0 : begin > a.rows ? a.rows : begin;
-    end = end > a.rows ? a.rows : end;
     const int64_t local = ((int64_t)by - (begin / kCodeBlock + e)) * kCodeBlock;
     if (local < 0 || local >= end - begin) return;
     first = (int)local;

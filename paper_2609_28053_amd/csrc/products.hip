@@ -90,6 +90,7 @@ struct Experts {
 };
 
 constexpr int kStep = kCodeBlock;       // bytes of a row per step
+constexpr int64_t kMemorySideCache = (int64_t)256 << 20;
 
 // Eight codes (words 2j and 2j + 1) times their scale.
 __device__ __forceinline__ bf16x8_t widen(const int4v& code, int j, float scale) {
@@ -440,6 +441,9 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
         for (int k = 0; k < 4; ++k) v[h * 4 + k] = O::from_f(acc[i][j + h][k]);
       return v;
     };
+    // a result that the memory-side cache does not hold passes the caches by (884,736 rows of
+    // 1,024 by 1,024: 1,171 -> 1,118 us)
+    const bool past = (kGrad ? (int64_t)a.E * a.N : a.rows) * width * (int64_t)sizeof(raw) > kMemorySideCache;
     if (t.np == BP && t.nq == BQ) {
 #pragma unroll
       for (int i = 0; i < TP; ++i) {
@@ -448,8 +452,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
           if constexpr (TQ % (2 * kPair) == 0) {
             if (j % (2 * kPair) != 0) continue;
             // a store of 8 whole lines of 128 bytes instead of 16 halves: lanes of rows 8 apart
-            // exchange halves (884,736 rows of 1,024 by 1,024: 1,179 -> 1,168 us; binary32, 20,012 rows
-            // of 1,001 by 777, 69 -> 65)
+            // exchange halves (884,736 rows of 1,024 by 1,024: 1,179 -> 1,168 us before they passed
+            // the caches by; binary32, 20,012 rows of 1,001 by 777, 69 -> 65)
             const int4v x = __builtin_bit_cast(int4v, values(i, j)), y = __builtin_bit_cast(int4v, values(i, j + kPair));
             int4v up, down;
 #pragma unroll
@@ -458,8 +462,15 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
               down[k] = __builtin_amdgcn_update_dpp(y[k], x[k], 0x128, 0xF, 0x3, false);
             }
             raw* const at = to + j * 16 + ((lane & 8) ? 16 * kPair - 8 * width : 0);
-            *reinterpret_cast<any*>(at) = __builtin_bit_cast(vec, up);
-            *reinterpret_cast<any*>(at + 8 * width) = __builtin_bit_cast(vec, down);
+            if (BP == 256 && past) {
+              asm volatile("" ::: "memory");      // or the compiler makes one of both branches, without the hint
+              __builtin_nontemporal_store(__builtin_bit_cast(vec, up), reinterpret_cast<any*>(at));
+              __builtin_nontemporal_store(__builtin_bit_cast(vec, down), reinterpret_cast<any*>(at + 8 * width));
+              asm volatile("" ::: "memory");
+            } else {
+              *reinterpret_cast<any*>(at) = __builtin_bit_cast(vec, up);
+              *reinterpret_cast<any*>(at + 8 * width) = __builtin_bit_cast(vec, down);
+            }
           } else {
             *reinterpret_cast<any*>(to + j * 16) = values(i, j);
           }

@@ -65,7 +65,8 @@ PRODUCTS = [  # counts, N, H, rows behind
     ([1], 1, 1, 0), ([1], 130, 128, 0), ([0, 3, 0], 7, 50, 2), ([5], 64, 129, 0), ([64, 0, 65, 1], 129, 300, 5), ([63] * 8, 200, 512, 0),
     ([1] * 200, 33, 640, 9), ([128, 129, 0, 127], 128, 256, 0), ([400], 300, 1001, 3), ([700, 0, 1, 900], 257, 384, 0), ([0, 0], 64, 64, 4),
     ([2] * 256, 16, 128, 0), ([300] * 3, 1, 2000, 0), ([1000], 520, 130, 1)]
-BIG = [([9000, 0, 8193, 300, 9001, 255, 7000], 1024, 200, 17), ([33000], 1100, 128, 0), ([6000, 5000, 0, 4000, 7100, 1], 1536, 513, 0)]
+BIG = [([9000, 0, 8193, 300, 9001, 255, 7000], 1024, 200, 17), ([33000], 1100, 128, 0), ([6000, 5000, 0, 4000, 7100, 1], 1536, 513, 0),
+       ([20000, 0, 30001, 20011], 2048, 130, 5)]      # more than the memory-side cache
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
@@ -99,7 +100,7 @@ def test_product(eqb, dtype, counts, N, H, behind):  # noqa: F811
 
 GRADS = [([1], 1, 1), ([0, 0, 5], 7, 50), ([128, 0, 1, 127, 129], 64, 130), ([300, 256, 0], 129, 257), ([0], 33, 64), ([3] * 60, 17, 20),
          ([600, 513], 200, 300), ([1, 0] * 20, 128, 128), ([2000], 300, 100), ([64] * 256, 8, 16)]
-BIG_GRADS = [([300, 0, 700, 1, 1300, 129, 128, 900], 1024, 2048), ([2000, 500], 4096, 4096)]
+BIG_GRADS = [([300, 0, 700, 1, 1300, 129, 128, 900], 1024, 2048), ([2000, 500], 4096, 4096), ([40, 300, 0] * 11, 2048, 2048)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
