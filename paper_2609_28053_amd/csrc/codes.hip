@@ -41,12 +41,25 @@ struct Eight {
   typedef vec any __attribute__((aligned(alignof(raw))));
 };
 
+// Calls that read or write more than the memory-side cache holds pass it by (kStream), where rows are whole
+// lines of 128 bytes: the others' lines are shared by neighbouring rows.  884,736 rows of 1,024 bf16 to their
+// experts 261 -> 241 us, 64 weights of 2,048 x 2,048 208 -> 191, 98,304 rows of 2,048 by columns 125
+// -> 119, gates and their gradients 496 -> 483; but 20,012 rows of 1,001 by columns 20.3 -> 23.8.
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
+template <bool kStream, class V>
+__device__ __forceinline__ V load_at(const V* at) { return kStream ? __builtin_nontemporal_load(at) : *at; }
+template <bool kStream, class V>
+__device__ __forceinline__ void store_at(V* at, V v) {
+  if constexpr (kStream) __builtin_nontemporal_store(v, at);
+  else *at = v;
+}
+
 // Elements c .. c + 7 of a row of H, zeros behind its end.
-template <int kDtype>
+template <int kDtype, bool kStream>
 __device__ __forceinline__ void load8(const typename Elem<kDtype>::raw* row, int c, int H, float (&v)[kPer]) {
   typedef Elem<kDtype> D;
   if (c + kPer <= H) {
-    const typename Eight<kDtype>::vec x = *reinterpret_cast<const typename Eight<kDtype>::any*>(row + c);
+    const typename Eight<kDtype>::vec x = load_at<kStream>(reinterpret_cast<const typename Eight<kDtype>::any*>(row + c));
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = D::to_f(x[i]);
   } else {
@@ -55,14 +68,14 @@ __device__ __forceinline__ void load8(const typename Elem<kDtype>::raw* row, int
   }
 }
 
-template <int kDtype>
+template <int kDtype, bool kStream>
 __device__ __forceinline__ void store8(typename Elem<kDtype>::raw* row, int c, int H, const float (&v)[kPer]) {
   typedef Elem<kDtype> D;
   typename Eight<kDtype>::vec x;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) x[i] = D::from_f(v[i]);
   if (c + kPer <= H) {
-    *reinterpret_cast<typename Eight<kDtype>::any*>(row + c) = x;
+    store_at<kStream>(reinterpret_cast<typename Eight<kDtype>::any*>(row + c), (typename Eight<kDtype>::any)x);
   } else {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
@@ -111,9 +124,9 @@ template <int kDtype>
 struct PlainRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = false;
-  template <bool kExact>
+  template <bool kExact, bool kStream>
   static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
-    load8<kDtype>(static_cast<const raw*>(a.x) + t * a.H, c, a.H, v);
+    load8<kDtype, kStream>(static_cast<const raw*>(a.x) + t * a.H, c, a.H, v);
     return false;
   }
 };
@@ -146,12 +159,12 @@ struct GatedRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = true;        // its values are not exact
   // whether a gate is so low that its sigmoid has fewer than 24 bits in binary32
-  template <bool kExact>
+  template <bool kExact, bool kStream>
   static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
     float g[kPer], u[kPer];
-    load8<kDtype>(row, c, a.H, g);
-    load8<kDtype>(row + a.H, c, a.H, u);
+    load8<kDtype, kStream>(row, c, a.H, g);
+    load8<kDtype, kStream>(row + a.H, c, a.H, u);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if constexpr (kExact) {
@@ -177,7 +190,7 @@ __device__ __forceinline__ int64_t rows_in_use(const CodeArgs& a) {
 
 // Sixteen lanes hold a block; a wave holds four.  With slots, a token's codes go to all of
 // its rows.
-template <class Row>
+template <class Row, bool kStream>
 __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeArgs a, int segments) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = rows_in_use(a), width = code_width(a.H), scales = scale_width(a.H);
@@ -198,14 +211,14 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
         byte = scale_byte(top);
         code = codes(scale_inverse(byte));
       };
-      const bool low = Row::template load<false>(a, t, c, v);
+      const bool low = Row::template load<false, kStream>(a, t, c, v);
       encode();
       if constexpr (Row::kOpen) {
         constexpr float kLess = 1.0f - 0x1p-19f, kMore = 1.0f + 0x1p-19f;
         const uint2 less = codes(scale_inverse(byte) * kLess), more = codes(scale_inverse(byte) * kMore);
         const bool open = low || less.x != more.x || less.y != more.y || scale_byte(top * kLess) != scale_byte(top * kMore);
         if (__ballot(open)) {
-          Row::template load<true>(a, t, c, v);
+          Row::template load<true, kStream>(a, t, c, v);
           encode();
         }
       }
@@ -215,7 +228,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
       for (int k = 0; k < a.K; ++k) {
         const int64_t r = a.slot ? a.slot[t * a.K + k] : t;
         if (r < 0 || r >= a.rows) continue;
-        if (c < width) *reinterpret_cast<uint2*>(a.codes + r * width + c) = code;
+        if (c < width) store_at<kStream>(reinterpret_cast<uint64_t*>(a.codes + r * width + c), __builtin_bit_cast(uint64_t, code));
         if (lane == 0) *reinterpret_cast<uint32_t*>(a.scales + r * scales + seg * 4) = word;
       }
     }
@@ -223,7 +236,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
 }
 
 // ---------------------------------------------------------- the gate --
-template <int kDtype, bool kBackward>
+template <int kDtype, bool kBackward, bool kStream>
 __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, int segments) {
   typedef typename Elem<kDtype>::raw raw;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -235,21 +248,21 @@ __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, i
       const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
       if constexpr (!kBackward) {
         float g[kPer], u[kPer];
-        load8<kDtype>(row, c, a.H, g);
-        load8<kDtype>(row + a.H, c, a.H, u);
+        load8<kDtype, kStream>(row, c, a.H, g);
+        load8<kDtype, kStream>(row + a.H, c, a.H, u);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           float s, rest;
           sigmoid_both(g[i], s, rest);
           g[i] = g[i] * s * u[i];
         }
-        store8<kDtype>(static_cast<raw*>(a.out) + t * a.H, c, a.H, g);
+        store8<kDtype, kStream>(static_cast<raw*>(a.out) + t * a.H, c, a.H, g);
       } else {
         raw* to = static_cast<raw*>(a.out) + t * 2 * a.H;
         float g[kPer], u[kPer], h[kPer];
-        load8<kDtype>(row, c, a.H, g);
-        load8<kDtype>(row + a.H, c, a.H, u);
-        load8<kDtype>(static_cast<const raw*>(a.grad) + t * a.H, c, a.H, h);
+        load8<kDtype, kStream>(row, c, a.H, g);
+        load8<kDtype, kStream>(row + a.H, c, a.H, u);
+        load8<kDtype, kStream>(static_cast<const raw*>(a.grad) + t * a.H, c, a.H, h);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           float s, rest;
@@ -259,8 +272,8 @@ __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, i
           g[i] = hs * u[i] * __builtin_fmaf(g[i], rest, 1.0f);
           u[i] = gu;
         }
-        store8<kDtype>(to, c, a.H, g);
-        store8<kDtype>(to + a.H, c, a.H, u);
+        store8<kDtype, kStream>(to, c, a.H, g);
+        store8<kDtype, kStream>(to + a.H, c, a.H, u);
       }
     }
   }
@@ -270,6 +283,7 @@ __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, i
 // A tile of 128 rows and kCols columns: a thread holds kRows neighbouring rows of 8 neighbouring columns,
 // and the transposed codes go through LDS.  kWeights: one scale for the tile (of 128 x 128), and the
 // codes in the rows' order too.
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
 constexpr int kTileStride = kCodeBlock + 4;        // bytes of a column in LDS: 33 words, so that columns 8 apart differ by 8 banks
 
 // The expert whose blocks of columns hold block b, the last one whose first block is at most b, and its rows
@@ -293,7 +307,7 @@ __device__ __forceinline__ void expert_of_block(const int32_t* offsets, int E, i
   end = end > rows ? rows : end;
 }
 
-template <int kDtype, bool kWeights, int kRows, int kCols>
+template <int kDtype, bool kWeights, bool kStream, int kRows, int kCols>
 __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const CodeArgs a) {
   constexpr int kGroups = kCols / kPer;         // of columns
   static_assert(kCodeBlock / kRows * kGroups == kCodeThreads && (!kWeights || kCols == kCodeBlock), "a thread for each");
@@ -331,7 +345,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
   for (int i = 0; i < kRows; ++i) {
     const int r = rg * kRows + i;
     if (r < nr && c < a.H) {
-      load8<kDtype>(static_cast<const raw*>(a.x) + (base + first + r) * a.H, c, a.H, v[i]);
+      load8<kDtype, kStream>(static_cast<const raw*>(a.x) + (base + first + r) * a.H, c, a.H, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) v[i][j] = 0.0f;
@@ -377,7 +391,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
       uint2 code;
       code.x = codes4(v[i][0], v[i][1], v[i][2], v[i][3]);
       code.y = codes4(v[i][4], v[i][5], v[i][6], v[i][7]);
-      *reinterpret_cast<uint2*>(a.codes + (base + first + r) * width + c) = code;
+      store_at<kStream>(reinterpret_cast<uint64_t*>(a.codes + (base + first + r) * width + c), __builtin_bit_cast(uint64_t, code));
     }
     // with the last block of a row, the zeros behind its scales
     const int64_t scales = scale_width(a.H);
@@ -400,7 +414,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
     const int at = tid + i * kCodeThreads, col = at >> 3, piece = at & 7;
     const uint32_t* from = reinterpret_cast<const uint32_t*>(sh_code + col * kTileStride + piece * 16);
     if (c0 + col < a.H)
-      *reinterpret_cast<uint4*>(to + (lead + c0 + col) * width + (int64_t)by * kCodeBlock + piece * 16) = make_uint4(from[0], from[1], from[2], from[3]);
+      store_at<kStream>(reinterpret_cast<word4*>(to + (lead + c0 + col) * width + (int64_t)by * kCodeBlock + piece * 16), word4{from[0], from[1], from[2], from[3]});
   }
   const int64_t scales = scale_width(width);
   if (kWeights) {
@@ -423,53 +437,74 @@ dim3 row_grid(const CodeArgs& a, int64_t width, int* segments) {
   return dim3((uint32_t)(*segments < 1024 ? *segments : 1024), (uint32_t)y);
 }
 
-template <template <int> class Row>
-eqb_status launch_rows_of(const CodeArgs& a, hipStream_t s) {
+int64_t bytes_of(int32_t dtype) { return dtype == EQB_DTYPE_F32 ? 4 : 2; }
+
+template <class Row>
+void launch_rows_in(const CodeArgs& a, bool stream, hipStream_t s) {
   int segments;
   const dim3 grid = row_grid(a, code_width(a.H), &segments);
-  if (a.dtype == EQB_DTYPE_BF16) quantize_rows_kernel<Row<EQB_DTYPE_BF16>><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else if (a.dtype == EQB_DTYPE_F16) quantize_rows_kernel<Row<EQB_DTYPE_F16>><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else quantize_rows_kernel<Row<EQB_DTYPE_F32>><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  if (stream) quantize_rows_kernel<Row, true><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else quantize_rows_kernel<Row, false><<<grid, kCodeThreads, 0, s>>>(a, segments);
+}
+template <template <int> class Row>
+eqb_status launch_rows_of(const CodeArgs& a, int per_value, hipStream_t s) {
+  const int64_t row = a.H * per_value * bytes_of(a.dtype), codes = a.T * a.K * code_width(a.H);
+  const bool stream = row % 128 == 0 && (a.T * row >= kStreamBytes || codes >= kStreamBytes);
+  if (a.dtype == EQB_DTYPE_BF16) launch_rows_in<Row<EQB_DTYPE_BF16>>(a, stream, s);
+  else if (a.dtype == EQB_DTYPE_F16) launch_rows_in<Row<EQB_DTYPE_F16>>(a, stream, s);
+  else launch_rows_in<Row<EQB_DTYPE_F32>>(a, stream, s);
   return launch_status();
 }
 
-template <bool kBackward>
-eqb_status launch_gate(const CodeArgs& a, hipStream_t s) {
+template <int kDtype, bool kBackward>
+void launch_gate_in(const CodeArgs& a, bool stream, hipStream_t s) {
   int segments;
   const dim3 grid = row_grid(a, a.H, &segments);
-  if (a.dtype == EQB_DTYPE_BF16) gated_kernel<EQB_DTYPE_BF16, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else if (a.dtype == EQB_DTYPE_F16) gated_kernel<EQB_DTYPE_F16, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else gated_kernel<EQB_DTYPE_F32, kBackward><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  if (stream) gated_kernel<kDtype, kBackward, true><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else gated_kernel<kDtype, kBackward, false><<<grid, kCodeThreads, 0, s>>>(a, segments);
+}
+template <bool kBackward>
+eqb_status launch_gate(const CodeArgs& a, hipStream_t s) {
+  const int64_t row = a.H * bytes_of(a.dtype);
+  const bool stream = row % 128 == 0 && a.T * row * 2 >= kStreamBytes;
+  if (a.dtype == EQB_DTYPE_BF16) launch_gate_in<EQB_DTYPE_BF16, kBackward>(a, stream, s);
+  else if (a.dtype == EQB_DTYPE_F16) launch_gate_in<EQB_DTYPE_F16, kBackward>(a, stream, s);
+  else launch_gate_in<EQB_DTYPE_F32, kBackward>(a, stream, s);
   return launch_status();
 }
 
 // Columns: 19,000 rows of 1,024 bf16 over 32 experts 16.9 us with 64 columns a tile, 17.7 with 128; 88,000 of
-// 2,048 90 and 98 (4.2 TB/s).  Weights, 64 of 2,048 x 2,048 bf16, both ways: 207 us (5.2 TB/s).
+// 2,048 90 and 98 (4.2 TB/s).  Weights, 64 of 2,048 x 2,048 bf16, both ways: 191 us (5.6 TB/s).
 constexpr int kColumnRows = 4, kColumnCols = 64;
-template <bool kWeights>
+template <bool kWeights, bool kStream>
 eqb_status launch_tiles(const CodeArgs& a, int64_t tiles, hipStream_t s) {
   if (tiles > INT32_MAX) return EQB_ERR_UNSUPPORTED;
   const uint32_t grid = (uint32_t)tiles;
   constexpr int R = kWeights ? 8 : kColumnRows, C = kWeights ? kCodeBlock : kColumnCols;
-  if (a.dtype == EQB_DTYPE_BF16) quantize_tiles_kernel<EQB_DTYPE_BF16, kWeights, R, C><<<grid, kCodeThreads, 0, s>>>(a);
-  else if (a.dtype == EQB_DTYPE_F16) quantize_tiles_kernel<EQB_DTYPE_F16, kWeights, R, C><<<grid, kCodeThreads, 0, s>>>(a);
-  else quantize_tiles_kernel<EQB_DTYPE_F32, kWeights, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  if (a.dtype == EQB_DTYPE_BF16) quantize_tiles_kernel<EQB_DTYPE_BF16, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  else if (a.dtype == EQB_DTYPE_F16) quantize_tiles_kernel<EQB_DTYPE_F16, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  else quantize_tiles_kernel<EQB_DTYPE_F32, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
   return launch_status();
 }
 
 }  // namespace
 
-eqb_status launch_quantize_rows(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, s); }
-eqb_status launch_dispatch_quantized(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, s); }
-eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s) { return launch_rows_of<GatedRow>(a, s); }
+eqb_status launch_quantize_rows(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, 1, s); }
+eqb_status launch_dispatch_quantized(const CodeArgs& a, hipStream_t s) { return launch_rows_of<PlainRow>(a, 1, s); }
+eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s) { return launch_rows_of<GatedRow>(a, 2, s); }
 eqb_status launch_gated(const CodeArgs& a, hipStream_t s) { return launch_gate<false>(a, s); }
 eqb_status launch_gated_backward(const CodeArgs& a, hipStream_t s) { return launch_gate<true>(a, s); }
 
 eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s) {
-  return launch_tiles<false>(a, ((int64_t)a.H + kColumnCols - 1) / kColumnCols * (column_width(a.rows, a.E) / kCodeBlock), s);
+  const int64_t tiles = ((int64_t)a.H + kColumnCols - 1) / kColumnCols * (column_width(a.rows, a.E) / kCodeBlock);
+  const int64_t row = a.H * bytes_of(a.dtype);
+  if (row % 128 == 0 && a.rows * row >= kStreamBytes) return launch_tiles<false, true>(a, tiles, s);
+  return launch_tiles<false, false>(a, tiles, s);
 }
 eqb_status launch_quantize_weights(const CodeArgs& a, hipStream_t s) {
-  return launch_tiles<true>(a, code_width(a.H) / kCodeBlock * (code_width(a.N) / kCodeBlock) * a.E, s);
+  const int64_t tiles = code_width(a.H) / kCodeBlock * (code_width(a.N) / kCodeBlock) * a.E, row = a.H * bytes_of(a.dtype);
+  if (row % 128 == 0 && (int64_t)a.E * a.N * row >= kStreamBytes) return launch_tiles<true, true>(a, tiles, s);
+  return launch_tiles<true, false>(a, tiles, s);
 }
 
 }  // namespace eqb

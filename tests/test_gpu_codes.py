@@ -281,3 +281,64 @@ def test_columns_of_descending_offsets(eqb):  # noqa: F811
         # the fill, zeros, and 1 = 256 2^-8
         assert np.isin(raw(codes), [0xA5, 0, 0x78]).all() and np.isin(raw(scales), [0xA5, 119]).all()
         assert (raw(codes)[-1] == 0xA5).all() and (raw(scales)[-1] == 0xA5).all()
+
+
+def test_more_than_the_cache_holds(eqb):  # noqa: F811
+    """Calls over more than 256 MiB, which pass the caches by: the bits of the same rows in calls of a quarter (and of
+    columns the transposed rows')."""
+    say("codes of large tensors")
+    rng = torch.Generator(device="cuda")
+    rng.manual_seed(3)
+    R, H = 66048, 2048
+    x = torch.randn((R, H), generator=rng, device="cuda", dtype=torch.bfloat16)
+    quarters = [slice(i * R // 4, (i + 1) * R // 4) for i in range(4)]
+    same = lambda a, b: torch.equal(a.view(torch.uint8), b.view(torch.uint8))  # noqa: E731
+
+    say("rows and dispatch")
+    c, s = buffers(eqb, (R,), H)
+    eqb.eqb_quantize_rows(x, c, s)
+    for q in quarters:
+        qc, qs = buffers(eqb, (R // 4,), H)
+        eqb.eqb_quantize_rows(x[q], qc, qs)
+        assert same(c[q], qc) and same(s[q], qs)
+    slot = torch.randperm(2 * R, generator=rng, device="cuda").to(torch.int32).view(R, 2)
+    dc, ds = buffers(eqb, (2 * R,), H)
+    eqb.eqb_dispatch_quantized(x, slot, dc, ds)
+    token = torch.empty(2 * R, dtype=torch.int64, device="cuda")
+    token[slot.view(-1).long()] = torch.arange(R, device="cuda").repeat_interleave(2)
+    assert torch.equal(dc.view(torch.uint8), c.view(torch.uint8)[token]) and torch.equal(ds.view(torch.uint8), s.view(torch.uint8)[token])
+    del dc, ds, token
+
+    say("columns")
+    W = eqb.eqb_column_width(R, 1)
+    cc, cs = buffers(eqb, (H,), W)
+    eqb.eqb_quantize_columns(x, torch.tensor([0, R], dtype=torch.int32, device="cuda"), cc, cs)
+    tc, ts = buffers(eqb, (H,), R)
+    eqb.eqb_quantize_rows(x.t().contiguous(), tc, ts)
+    assert same(cc[:, :R].contiguous(), tc) and torch.equal(cs.view(torch.uint8)[:, :R // 128], ts.view(torch.uint8)[:, :R // 128])
+
+    say("weights")
+    E = 36
+    w = torch.randn((E, 2048, 2048), generator=rng, device="cuda", dtype=torch.bfloat16)
+    whole = [*buffers(eqb, (E, 2048), 2048), *buffers(eqb, (E, 2048), 2048)]
+    whole[1::2] = [buffers(eqb, (E, 16), 2048)[1] for _ in range(2)]
+    eqb.eqb_quantize_weights(w, *whole)
+    for e in range(0, E, 9):
+        part = [t[e:e + 9].clone().view(torch.uint8).fill_(1).view(t.dtype) for t in whole]
+        eqb.eqb_quantize_weights(w[e:e + 9], *part)
+        assert all(same(a[e:e + 9], b) for a, b in zip(whole, part))
+    del w, whole, part
+
+    say("gates")
+    g = torch.randn((R, 2 * H), generator=rng, device="cuda", dtype=torch.bfloat16)
+    h, gx = torch.empty_like(x), torch.empty_like(g)
+    c, s = buffers(eqb, (R,), H)
+    eqb.eqb_gated(g, h)
+    eqb.eqb_gated_backward(x, g, gx)
+    eqb.eqb_gated_quantize(g, c, s)
+    for q in quarters:
+        qh, qg, (qc, qs) = torch.empty_like(x[q]), torch.empty_like(g[q]), buffers(eqb, (R // 4,), H)
+        eqb.eqb_gated(g[q], qh)
+        eqb.eqb_gated_backward(x[q], g[q], qg)
+        eqb.eqb_gated_quantize(g[q], qc, qs)
+        assert same(h[q], qh) and same(gx[q], qg) and same(c[q], qc) and same(s[q], qs)
