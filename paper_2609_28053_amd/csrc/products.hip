@@ -45,6 +45,7 @@ struct OutType<EQB_DTYPE_F16> {
 struct Experts {
   int2 rows[kMostExperts];        // first row, and how many
   int before[kMostExperts / 4], total;
+  uint8_t largest[kMostExperts];  // the experts by their rows, most first
 
   // By every wave of the block; lane l takes the experts 4l .. 4l + 3.
   __device__ __forceinline__ void fill(const int32_t* offsets, int E, int64_t most, int BP) {
@@ -67,6 +68,15 @@ struct Experts {
     }
     before[lane] = incl - sum;
     if (lane == 63) total = incl;
+  }
+  // By all threads, behind a barrier.
+  __device__ __forceinline__ void sort(int E) {
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+      const int n = rows[e].y;
+      int rank = 0;
+      for (int i = 0; i < E; ++i) rank += rows[i].y > n || (rows[i].y == n && i < e) ? 1 : 0;
+      largest[rank] = (uint8_t)e;
+    }
   }
   __device__ __forceinline__ int2 of(int e) const {
     const int2 r = rows[e];
@@ -159,6 +169,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
   __shared__ __attribute__((aligned(16))) Experts experts;
   experts.fill(a.offsets, a.E, a.rows, BP);
   __syncthreads();
+  if (kGrad) {
+    experts.sort(a.E);
+    __syncthreads();
+  }
   const uint32_t tiles = (uint32_t)((kGrad ? a.E * p_tiles : __builtin_amdgcn_readfirstlane(experts.total)) * q_tiles);
 
   auto tile_of = [&](uint32_t id) {
@@ -166,7 +180,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
     const uint32_t pt = id / (uint32_t)q_tiles;
     t.col = (int)(id - pt * q_tiles) * BQ;
     if (kGrad) {
-      const int e = (int)(pt / (uint32_t)p_tiles), p0 = ((int)pt - e * p_tiles) * BP;
+      const int n = (int)(pt / (uint32_t)p_tiles), p0 = ((int)pt - n * p_tiles) * BP;
+      const int e = __builtin_amdgcn_readfirstlane(experts.largest[n]);
       t.row = (int64_t)e * a.N + p0;
       t.np = a.N - p0;
       t.nq = a.H - t.col;
@@ -200,6 +215,11 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
   // ---- the loads: a sequence of steps over this block's tiles
   const uint32_t eighth = gridDim.x / 8;
   const uint32_t first_id = blockIdx.x < eighth * 8 ? (blockIdx.x % 8) * eighth + blockIdx.x / 8 : blockIdx.x;
+  // The gradients' tiles are as long as their experts are large: the largest come first, and the blocks
+  // take every other round of tiles in the other direction.
+  auto id_after = [&](uint32_t id) {
+    return kGrad ? 2 * gridDim.x * (id / gridDim.x + 1) - 1 - id : id + gridDim.x;
+  };
   // A load takes 8 rows (64 of scales).  A lane's place in each load is found once a tile, as an
   // offset from the tile's first row: its row, and the 16 bytes that its place in LDS is for.  The
   // pieces of a row are permuted by half the row's number, so that lanes that read the same piece
@@ -214,7 +234,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
   auto aim = [&]() {
     while (from_block == from_end && load_id < tiles) {
       const Tile t = tile_of(load_id);
-      load_id += gridDim.x;
+      load_id = id_after(load_id);
       from_block = t.block;
       from_end = t.end;
       if (t.block == t.end) continue;
@@ -339,7 +359,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void product_kernel(const ProductA
     for (int i = 0; i < TP; ++i)
 #pragma unroll
       for (int j = 0; j < TQ; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-    const uint32_t next_id = id + gridDim.x;
+    const uint32_t next_id = id_after(id);
     if (t.block < t.end && !ready) {
       next_step(t.block);
       read_first();
