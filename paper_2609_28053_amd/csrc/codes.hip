@@ -188,15 +188,20 @@ __device__ __forceinline__ int64_t rows_in_use(const CodeArgs& a) {
   return n < a.T ? n : a.T;
 }
 
-// Sixteen lanes hold a block; a wave holds four.  With slots, a token's codes go to all of
-// its rows.
-template <class Row, bool kStream>
+// Sixteen lanes hold a block; a wave holds four, of as many rows where rows are of one or two blocks
+// (kBlocks; 355,390 rows of 47 to their experts: 35 -> 15 us, 600,000 gated ones of 36
+// 375 -> 120).  With slots, a token's codes go to all
+// of its rows.
+template <class Row, bool kStream, int kBlocks>
 __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeArgs a, int segments) {
+  constexpr int kLanes = 16 * kBlocks, kRows = 4 / kBlocks;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = rows_in_use(a), width = code_width(a.H), scales = scale_width(a.H);
   for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
-    const int c = (int)seg * kWaveCols + lane * kPer;
-    for (int64_t t = (int64_t)blockIdx.y * kCodeWaves + wave; t < rows; t += (int64_t)gridDim.y * kCodeWaves) {
+    const int c = (int)seg * kWaveCols + lane % kLanes * kPer;
+    for (int64_t t0 = ((int64_t)blockIdx.y * kCodeWaves + wave) * kRows; t0 < rows; t0 += (int64_t)gridDim.y * kCodeWaves * kRows) {
+      const bool live = kRows == 1 || t0 + lane / kLanes < rows;
+      const int64_t t = kRows == 1 ? t0 : live ? t0 + lane / kLanes : rows - 1;
       float v[kPer], top;
       int byte;
       uint2 code;
@@ -223,28 +228,34 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
         }
       }
       const int mine = c < width ? byte : 0;
-      const uint32_t word = (uint32_t)__builtin_amdgcn_readlane(mine, 0) | (uint32_t)__builtin_amdgcn_readlane(mine, 16) << 8 |
-                            (uint32_t)__builtin_amdgcn_readlane(mine, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(mine, 48) << 24;
+      uint32_t word = (uint32_t)mine;
+      if constexpr (kBlocks == 2) word |= (uint32_t)__shfl_down(mine, 16) << 8;
+      if constexpr (kBlocks == 4)
+        word = (uint32_t)__builtin_amdgcn_readlane(mine, 0) | (uint32_t)__builtin_amdgcn_readlane(mine, 16) << 8 |
+               (uint32_t)__builtin_amdgcn_readlane(mine, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(mine, 48) << 24;
+      if (!live) continue;
       for (int k = 0; k < a.K; ++k) {
         const int64_t r = a.slot ? a.slot[t * a.K + k] : t;
         if (r < 0 || r >= a.rows) continue;
         if (c < width) store_at<kStream>(reinterpret_cast<uint64_t*>(a.codes + r * width + c), __builtin_bit_cast(uint64_t, code));
-        if (lane == 0) *reinterpret_cast<uint32_t*>(a.scales + r * scales + seg * 4) = word;
+        if (lane % kLanes == 0) *reinterpret_cast<uint32_t*>(a.scales + r * scales + seg * 4) = word;
       }
     }
   }
 }
 
 // ---------------------------------------------------------- the gate --
-template <int kDtype, bool kBackward, bool kStream>
+// kLanes of a row: 64, or as many as its elements need (16 or 32).
+template <int kDtype, bool kBackward, bool kStream, int kLanes>
 __global__ __launch_bounds__(kCodeThreads) void gated_kernel(const CodeArgs a, int segments) {
   typedef typename Elem<kDtype>::raw raw;
+  constexpr int kRows = 64 / kLanes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = rows_in_use(a);
   for (int64_t seg = blockIdx.x; seg < segments; seg += gridDim.x) {
-    const int c = (int)seg * kWaveCols + lane * kPer;
+    const int c = (int)seg * kWaveCols + lane % kLanes * kPer;
     if (c >= a.H) continue;
-    for (int64_t t = (int64_t)blockIdx.y * kCodeWaves + wave; t < rows; t += (int64_t)gridDim.y * kCodeWaves) {
+    for (int64_t t = ((int64_t)blockIdx.y * kCodeWaves + wave) * kRows + lane / kLanes; t < rows; t += (int64_t)gridDim.y * kCodeWaves * kRows) {
       const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
       if constexpr (!kBackward) {
         float g[kPer], u[kPer];
@@ -428,9 +439,10 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
   }
 }
 
-dim3 row_grid(const CodeArgs& a, int64_t width, int* segments) {
+// rows: of a wave at a time
+dim3 row_grid(const CodeArgs& a, int64_t width, int rows, int* segments) {
   *segments = (int)((width + kWaveCols - 1) / kWaveCols);
-  int64_t y = (a.T + kCodeWaves - 1) / kCodeWaves, most = 65535;
+  int64_t y = (a.T + kCodeWaves * rows - 1) / (kCodeWaves * rows), most = 65535;
   const int cap = max_blocks_cap();
   if (cap > 0 && cap < most) most = cap;
   if (y > most) y = most;
@@ -439,29 +451,42 @@ dim3 row_grid(const CodeArgs& a, int64_t width, int* segments) {
 
 int64_t bytes_of(int32_t dtype) { return dtype == EQB_DTYPE_F32 ? 4 : 2; }
 
-template <class Row>
+template <class Row, int kBlocks>
 void launch_rows_in(const CodeArgs& a, bool stream, hipStream_t s) {
   int segments;
-  const dim3 grid = row_grid(a, code_width(a.H), &segments);
-  if (stream) quantize_rows_kernel<Row, true><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else quantize_rows_kernel<Row, false><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  const dim3 grid = row_grid(a, code_width(a.H), 4 / kBlocks, &segments);
+  if (stream) quantize_rows_kernel<Row, true, kBlocks><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else quantize_rows_kernel<Row, false, kBlocks><<<grid, kCodeThreads, 0, s>>>(a, segments);
+}
+template <class Row>
+void launch_rows_by(const CodeArgs& a, bool stream, hipStream_t s) {
+  const int64_t width = code_width(a.H);
+  if (width <= kCodeBlock) launch_rows_in<Row, 1>(a, stream, s);
+  else if (width <= 2 * kCodeBlock) launch_rows_in<Row, 2>(a, stream, s);
+  else launch_rows_in<Row, 4>(a, stream, s);
 }
 template <template <int> class Row>
 eqb_status launch_rows_of(const CodeArgs& a, int per_value, hipStream_t s) {
   const int64_t row = a.H * per_value * bytes_of(a.dtype), codes = a.T * a.K * code_width(a.H);
   const bool stream = row % 128 == 0 && (a.T * row >= kStreamBytes || codes >= kStreamBytes);
-  if (a.dtype == EQB_DTYPE_BF16) launch_rows_in<Row<EQB_DTYPE_BF16>>(a, stream, s);
-  else if (a.dtype == EQB_DTYPE_F16) launch_rows_in<Row<EQB_DTYPE_F16>>(a, stream, s);
-  else launch_rows_in<Row<EQB_DTYPE_F32>>(a, stream, s);
+  if (a.dtype == EQB_DTYPE_BF16) launch_rows_by<Row<EQB_DTYPE_BF16>>(a, stream, s);
+  else if (a.dtype == EQB_DTYPE_F16) launch_rows_by<Row<EQB_DTYPE_F16>>(a, stream, s);
+  else launch_rows_by<Row<EQB_DTYPE_F32>>(a, stream, s);
   return launch_status();
 }
 
+template <int kDtype, bool kBackward, int kLanes>
+void launch_gate_lanes(const CodeArgs& a, bool stream, hipStream_t s) {
+  int segments;
+  const dim3 grid = row_grid(a, a.H, 64 / kLanes, &segments);
+  if (stream) gated_kernel<kDtype, kBackward, true, kLanes><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  else gated_kernel<kDtype, kBackward, false, kLanes><<<grid, kCodeThreads, 0, s>>>(a, segments);
+}
 template <int kDtype, bool kBackward>
 void launch_gate_in(const CodeArgs& a, bool stream, hipStream_t s) {
-  int segments;
-  const dim3 grid = row_grid(a, a.H, &segments);
-  if (stream) gated_kernel<kDtype, kBackward, true><<<grid, kCodeThreads, 0, s>>>(a, segments);
-  else gated_kernel<kDtype, kBackward, false><<<grid, kCodeThreads, 0, s>>>(a, segments);
+  if (a.H <= 16 * kPer) launch_gate_lanes<kDtype, kBackward, 16>(a, stream, s);
+  else if (a.H <= 32 * kPer) launch_gate_lanes<kDtype, kBackward, 32>(a, stream, s);
+  else launch_gate_lanes<kDtype, kBackward, 64>(a, stream, s);
 }
 template <bool kBackward>
 eqb_status launch_gate(const CodeArgs& a, hipStream_t s) {

@@ -550,7 +550,10 @@ eqb_status launch_form(const ProductArgs& a, int per_cu, hipStream_t s) {
 //   few rows an expert, up to 64 on average: 64 rows of 2,048 to 2,048 columns, E = 256, 38.5 with 64,
 //   39.6 with 128, 54 with 256; one row 9.9, 13.0, 25; 4,096 rows of 1,024, E = 64, 21.7, 24.1, 23.8;
 //   but 4,096 rows of 1,024, E = 8, 16.7, 14.7, 20.8.
-//   weight gradients of few tiles: 16 of 512 x 256, 15.2, 18.4, 40; but 8 of 1,024 x 1,024, 20.2, 17.0, 23.4.
+//   weight gradients of up to two tiles of 128 a compute unit: 16 of 512 x 256, 15.2, 18.4, 40; and the more
+//   where experts are uneven, since a large one's tiles are as many more steps: with the largest of 6 times the
+//   mean 128 of 128 x 140 over 256,879 rows 77, 124, 262 (binary32), with 4.7 times 64 of 256 x 512 over 100,362
+//   84, 104, 170; but 8 even ones of 1,024 x 1,024 20.2, 17.0, 23.4, 16 with 2.3 times 212, 168, 240.
 //   256 once two of its tiles come on a compute unit and what they reach over the edges costs no more
 //   than an eighth: 98,304 rows of 2,048 to 2,048, E = 64, 454 against 561 with 128; 196,608 of 1,024
 //   to 1,024, E = 256, 304, 352; 24,576 rows of 2,048 160 both; but 80,000 of 500 to 300, E = 32,
@@ -564,7 +567,7 @@ eqb_status launch_product(const ProductArgs& a, hipStream_t s) {
   auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to; };
   // an expert's rows end in the middle of a tile
   auto tiles = [&](int64_t side) { return (kGrad ? E * up(p, side) : p / side + most / 2) * up(q, side); };
-  const bool small = kGrad ? tiles(128) < cus : a.rows <= 64 * E;
+  const bool small = kGrad ? tiles(128) <= 2 * cus : a.rows <= 64 * E;
   const bool large = tiles(256) >= 2 * cus && 4 * tiles(256) * 8 <= tiles(128) * 9;
   if (a.dtype == EQB_DTYPE_F32) {
     if (small) return launch_form<64, 64, 2, 2, kGrad, true>(a, 4, s);
