@@ -504,8 +504,8 @@ eqb_status eqb_adamw_step_counted(const eqb_adamw_tensor* tensors, int32_t n, in
  *     any); only the experts of the top_groups groups of the largest scores take part.
  *   The K largest q are chosen, in that order.  Where masks leave fewer, the last entries are
  *     expert -1 of weight 0: dropped pairs to eqb_dispatch_plan.
- *   weight_k = scale s_k / (sum of the chosen s) (normalize; 0 where that sum is 0) or scale s_k,
- *     in binary32.  Scores below 2^-126 may count as 0 there.
+ *   weight_k = scale s_k / (sum of the chosen s) (normalize; also where binary32 holds none of those s) or
+ *     scale s_k, in binary32.  Scores below 2^-126, normalized weights below 2^-100 scale, may count as 0 there.
  * Ties go to the lower expert and to the lower group.  Which of two scores is larger is decided as
  * in binary64 (without a bias: by the logits), so that the choice does not depend on a rounding of
  * binary32.

@@ -29,6 +29,20 @@ def scores(z, softmax):
     return np.divide(e, d, out=np.zeros_like(e), where=d > 0)
 
 
+def shares(z, s, softmax):
+    """What the chosen scores s of the logits z are of their sum: from their logarithms, so that scores that binary64
+    does not hold have a share too (0 of masked ones and of none)."""
+    on = z > -np.inf
+    if not on.any():
+        return np.zeros_like(s)
+    x = z[on]
+    log = x if softmax else x - np.logaddexp(0.0, x)
+    r = np.exp(log - log.max())
+    out = np.zeros_like(s)
+    out[on] = r / r.sum()
+    return out
+
+
 def route(z, bias, K, softmax=False, groups=1, top_groups=1, group_top=1, normalize=True, scale=1.0):
     """idx [T,K] and weight [T,K]."""
     T, E = z.shape
@@ -48,10 +62,7 @@ def route(z, bias, K, softmax=False, groups=1, top_groups=1, group_top=1, normal
         # without a bias the scores' order is the logits', also where the scores are no longer told apart
         best = sorted(q, key=lambda e: (-z[t, e] if bias is None else -q[e], e))[:K]
         idx[t, :len(best)] = best
-        weight[t, :len(best)] = s[t, best]
-    if normalize:
-        S = weight.sum(1, keepdims=True)
-        weight = np.divide(weight, S, out=np.zeros_like(weight), where=S > 0)
+        weight[t, :len(best)] = shares(z[t, best], s[t, best], softmax) if normalize else s[t, best]
     return idx, scale * weight
 
 
@@ -64,12 +75,14 @@ def route_backward(z, idx, g, softmax=False, normalize=True, scale=1.0):
         on = [k for k in range(idx.shape[1]) if 0 <= idx[t, k] < E]
         sk = s[t, idx[t, on]]
         gk = g[t, on]
-        a, m = gk.copy(), np.abs(gk)
         if normalize:
-            S = sk.sum()
-            a = (gk - (gk @ sk) / S) / S if S > 0 else np.zeros_like(gk)
-            m = (np.abs(gk) + (np.abs(gk) @ sk) / S) / S if S > 0 else np.zeros_like(gk)
-        a, m = scale * a, abs(scale) * m
+            r = shares(z[t, idx[t, on]], sk, softmax)
+            x = z[t, idx[t, on]]
+            rest = 1.0 if softmax else np.exp(-np.logaddexp(0.0, x))
+            np.add.at(grad[t], idx[t, on], scale * (gk - gk @ r) * r * rest)
+            np.add.at(size[t], idx[t, on], abs(scale) * (np.abs(gk) + np.abs(gk) @ r) * r * rest)
+            continue
+        a, m = scale * gk, abs(scale) * np.abs(gk)
         at, mt = np.zeros(E), np.zeros(E)
         np.add.at(at, idx[t, on], a)
         np.add.at(mt, idx[t, on], m)

@@ -59,6 +59,16 @@ __device__ __forceinline__ float sigmoid_of(float z) {
 }
 __device__ __forceinline__ double sigmoid_of(double z) { return 1.0 / (1.0 + exp(-z)); }
 
+// Normalized weights are ratios of scores.  Where the chosen ones of a row sum to less than this, as after a
+// bias has chosen logits far below the largest, some may have few bits or none in binary32: they are formed
+// again over a power of e, that of the largest chosen logit.  Left is what lies below 2^-106 of the weights' sum.
+constexpr float kLowSum = 0x1p-20f;
+__device__ __forceinline__ float raised_score(float z, float most, bool softmax) {
+  float s, rest = 1.0f;
+  if (!softmax) sigmoid_pair(z, s, rest);           // s = e^z (1 - s)
+  return exp_neg(most - z) * rest;
+}
+
 template <class F>
 __device__ __forceinline__ F lowest_of() { return -(F)__builtin_inf(); }
 
@@ -309,10 +319,21 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_kernel(const Scor
       for (int k = l; k < a.K; k += L) sum += chosen[k] >= 0 ? score(chosen[k]) : 0.0f;
       sum = row_sum<L>(sum);
     }
+    const bool low = a.normalize && sum < kLowSum;
+    float most = -__builtin_inff();
+    auto raised = [&](int e) { return raised_score(clean(Logit<kDtype>::to_f(row[e])), most, a.softmax); };
+    if (__ballot(low && chosen[0] >= 0)) {
+      float again = 0.0f;
+      for (int k = l; k < a.K; k += L) most = fmaxf(most, chosen[k] >= 0 ? clean(Logit<kDtype>::to_f(row[chosen[k]])) : most);
+      most = row_max<L>(most);
+      for (int k = l; k < a.K; k += L) again += chosen[k] >= 0 ? raised(chosen[k]) : 0.0f;
+      again = row_sum<L>(again);
+      sum = low ? again : sum;
+    }
     if (live) {
       for (int k = l; k < a.K; k += L) {
         const int e = chosen[k];
-        float w = e >= 0 ? score(e) : 0.0f;
+        float w = e < 0 ? 0.0f : low ? raised(e) : score(e);
         if (a.normalize) w = sum > 0.0f ? w / sum : 0.0f;
         a.idx[t * a.K + k] = e;
         a.weight[t * a.K + k] = a.scale * w;
@@ -635,7 +656,26 @@ __global__ __launch_bounds__(kScoredThreads, N == 8 ? 4 : 3) void route_scored_b
       }
       sum += s[h];
     }
-    const float by = a.normalize ? row_sum<L>(sum) : total;
+    float by = a.normalize ? row_sum<L>(sum) : total;
+    const bool low = a.normalize && by < kLowSum;
+    if (__ballot(low && e[0] >= 0)) {
+      float x[kEach], most = none;
+#pragma unroll
+      for (int h = 0; h < kEach; ++h) {
+        x[h] = e[h] >= 0 ? clean(Logit<kDtype>::to_f(row[e[h]])) : none;
+        most = fmaxf(most, x[h]);
+      }
+      most = row_max<L>(most);
+      sum = 0.0f;
+#pragma unroll
+      for (int h = 0; h < kEach; ++h) {
+        const float again = e[h] >= 0 ? raised_score(x[h], most, kSoftmax) : 0.0f;
+        s[h] = low ? again : s[h];
+        sum += s[h];
+      }
+      sum = row_sum<L>(sum);
+      by = low ? sum : by;
+    }
     const uint64_t doubts = __ballot(doubt && live);
     const bool again = (doubts >> (lane / L * L) & (L == 64 ? ~0ull : (1ull << (L & 63)) - 1)) != 0;
     if (live && !again) {
@@ -662,12 +702,17 @@ __global__ __launch_bounds__(kScoredThreads, N == 8 ? 4 : 3) void route_scored_b
       if (kSoftmax) softmax_of<kSlow, kDtype>(zs, top_s, total_s);
       const raw* at = static_cast<const raw*>(a.z) + tr * E;
       const int es = lane < a.K ? sh_chosen[wave][lane & (N - 1)] : -1;
-      float ss = 0.0f;
+      float ss = 0.0f, x = none;
       if (es >= 0) {
-        const float x = clean(Logit<kDtype>::to_f(at[es]));
+        x = clean(Logit<kDtype>::to_f(at[es]));
         ss = kSoftmax ? exp_neg(top_s - x) : sigmoid_of(x);
       }
-      const float by_s = a.normalize ? row_sum<N>(ss) : total_s;      // lanes 0 .. N - 1 hold them
+      float by_s = a.normalize ? row_sum<N>(ss) : total_s;      // lanes 0 .. N - 1 hold them
+      if (__ballot(a.normalize && es >= 0 && by_s < kLowSum)) {
+        const float most = row_max<N>(x);
+        ss = es >= 0 ? raised_score(x, most, kSoftmax) : 0.0f;
+        by_s = row_sum<N>(ss);
+      }
       if (lane < a.K) {
         a.idx[tr * a.K + lane] = es;
         a.weight[tr * a.K + lane] = by_s > 0.0f ? a.scale * (ss / by_s) : 0.0f;
@@ -725,9 +770,14 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(c
       top = row_max<L>(top);
       if (top == -__builtin_inff()) top = 0.0f;
     }
+    float most = 0.0f;
+    bool low = false;                     // a sigmoid's scores are over e^most
     auto score = [&](int e, float& s, float& rest) {
       const float x = clean(Logit<kDtype>::to_f(row[e]));
-      if (a.softmax) {
+      if (low) {
+        sigmoid_pair(x, s, rest);
+        s = exp_neg(most - x) * rest;
+      } else if (a.softmax) {
         s = total > 0.0f ? exp_neg(top - x) / total : 0.0f;
         rest = 1.0f;
       } else {
@@ -735,17 +785,31 @@ __global__ __launch_bounds__(kScoredThreads) void route_scored_backward_kernel(c
       }
     };
     // S = sum of the chosen scores and the sum of g s
-    float S = 0.0f, gs = 0.0f;
-    for (int k = l; k < a.K; k += L) {
-      const int e = idx[k];
-      if (e < 0 || e >= E) continue;
-      float s, rest;
-      score(e, s, rest);
-      S += s;
-      gs += gw[k] * s;
+    float S, gs;
+    auto sums = [&]() {
+      S = gs = 0.0f;
+      for (int k = l; k < a.K; k += L) {
+        const int e = idx[k];
+        if (e < 0 || e >= E) continue;
+        float s, rest;
+        score(e, s, rest);
+        S += s;
+        gs += gw[k] * s;
+      }
+      S = row_sum<L>(S);
+      gs = row_sum<L>(gs);
+    };
+    sums();
+    if (a.normalize && !a.softmax && __ballot(S < kLowSum)) {
+      most = -__builtin_inff();
+      for (int k = l; k < a.K; k += L) {
+        const int e = idx[k];
+        if (e >= 0 && e < E) most = fmaxf(most, clean(Logit<kDtype>::to_f(row[e])));
+      }
+      most = row_max<L>(most);
+      low = S < kLowSum && most > -__builtin_inff();
+      sums();
     }
-    S = row_sum<L>(S);
-    gs = row_sum<L>(gs);
     const float inv = a.normalize ? (S > 0.0f ? 1.0f / S : 0.0f) : 1.0f, mean = a.normalize ? gs * inv : 0.0f;
     lds_wave_sync();
     // entry by entry, so that an expert that a row names twice gets both in their order
