@@ -593,7 +593,9 @@ eqb_status eqb_experts_grad_weight(const uint8_t* grad_codes, const uint8_t* gra
  * The gated activation between an expert's two products: x [rows, 2 hidden] holds a row's gate g and
  * then its u, h = g sigmoid(g) u.  Computed in binary32, rounded once.
  *   eqb_gated: h [rows, hidden] of x's type.  eqb_gated_quantize: h as eqb_quantize_rows leaves it,
- *   without a rounding in between.
+ *   without a rounding in between.  eqb_gated_quantize_columns: h of x's type as eqb_quantize_columns
+ *   leaves it, for the gradient of the second product's weights; what the type does not hold (above
+ *   65504 in F16) is taken in binary32, as the second product had it.
  *   eqb_gated_backward: grad_x [rows, 2 hidden] from grad_h [rows, hidden]:
  *     grad_g = grad_h u s (1 + g (1 - s)), grad_u = grad_h g s, s = sigmoid(g).
  * count as in eqb_quantize_rows.
@@ -602,6 +604,8 @@ eqb_status eqb_gated(const void* x, const int32_t* count, int64_t rows, int32_t 
                      void* stream);
 eqb_status eqb_gated_quantize(const void* x, const int32_t* count, int64_t rows, int32_t hidden, int32_t dtype,
                               uint8_t* codes, uint8_t* scales, void* stream);
+eqb_status eqb_gated_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
+                                      int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream);
 eqb_status eqb_gated_backward(const void* grad_h, const void* x, const int32_t* count, int64_t rows, int32_t hidden,
                               int32_t dtype, void* grad_x, void* stream);
 

@@ -182,6 +182,27 @@ struct GatedRow {
   }
 };
 
+// The gated value as eqb_gated stores it, in binary32 where the type does not hold it (F16 ends at 65,504).
+template <int kDtype>
+struct StoredGate {
+  typedef typename Elem<kDtype>::raw raw;
+  template <bool kExact, bool kStream>
+  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+    const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
+    float g[kPer], u[kPer];
+    load8<kDtype, kStream>(row, c, a.H, g);
+    load8<kDtype, kStream>(row + a.H, c, a.H, u);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      float s, rest;
+      sigmoid_both(g[i], s, rest);
+      const float h = g[i] * s * u[i], stored = Elem<kDtype>::to_f(Elem<kDtype>::from_f(h));
+      v[i] = fabsf(stored) < __builtin_inff() ? stored : h;
+    }
+    return false;
+  }
+};
+
 __device__ __forceinline__ int64_t rows_in_use(const CodeArgs& a) {
   if (!a.count) return a.T;
   const int64_t n = *a.count;
@@ -318,11 +339,10 @@ __device__ __forceinline__ void expert_of_block(const int32_t* offsets, int E, i
   end = end > rows ? rows : end;
 }
 
-template <int kDtype, bool kWeights, bool kStream, int kRows, int kCols>
+template <class Row, bool kWeights, bool kStream, int kRows, int kCols>
 __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const CodeArgs a) {
   constexpr int kGroups = kCols / kPer;         // of columns
   static_assert(kCodeBlock / kRows * kGroups == kCodeThreads && (!kWeights || kCols == kCodeBlock), "a thread for each");
-  typedef typename Elem<kDtype>::raw raw;
   __shared__ __attribute__((aligned(16))) uint8_t sh_code[kCols * kTileStride];
   __shared__ float sh_top[kCodeWaves][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -356,7 +376,7 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_tiles_kernel(const Code
   for (int i = 0; i < kRows; ++i) {
     const int r = rg * kRows + i;
     if (r < nr && c < a.H) {
-      load8<kDtype, kStream>(static_cast<const raw*>(a.x) + (base + first + r) * a.H, c, a.H, v[i]);
+      Row::template load<false, kStream>(a, base + first + r, c, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) v[i][j] = 0.0f;
@@ -501,14 +521,14 @@ eqb_status launch_gate(const CodeArgs& a, hipStream_t s) {
 // Columns: 19,000 rows of 1,024 bf16 over 32 experts 16.9 us with 64 columns a tile, 17.7 with 128; 88,000 of
 // 2,048 90 and 98 (4.2 TB/s).  Weights, 64 of 2,048 x 2,048 bf16, both ways: 191 us (5.6 TB/s).
 constexpr int kColumnRows = 4, kColumnCols = 64;
-template <bool kWeights, bool kStream>
+template <template <int> class Row, bool kWeights, bool kStream>
 eqb_status launch_tiles(const CodeArgs& a, int64_t tiles, hipStream_t s) {
   if (tiles > INT32_MAX) return EQB_ERR_UNSUPPORTED;
   const uint32_t grid = (uint32_t)tiles;
   constexpr int R = kWeights ? 8 : kColumnRows, C = kWeights ? kCodeBlock : kColumnCols;
-  if (a.dtype == EQB_DTYPE_BF16) quantize_tiles_kernel<EQB_DTYPE_BF16, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
-  else if (a.dtype == EQB_DTYPE_F16) quantize_tiles_kernel<EQB_DTYPE_F16, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
-  else quantize_tiles_kernel<EQB_DTYPE_F32, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  if (a.dtype == EQB_DTYPE_BF16) quantize_tiles_kernel<Row<EQB_DTYPE_BF16>, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  else if (a.dtype == EQB_DTYPE_F16) quantize_tiles_kernel<Row<EQB_DTYPE_F16>, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
+  else quantize_tiles_kernel<Row<EQB_DTYPE_F32>, kWeights, kStream, R, C><<<grid, kCodeThreads, 0, s>>>(a);
   return launch_status();
 }
 
@@ -520,16 +540,19 @@ eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s) { return laun
 eqb_status launch_gated(const CodeArgs& a, hipStream_t s) { return launch_gate<false>(a, s); }
 eqb_status launch_gated_backward(const CodeArgs& a, hipStream_t s) { return launch_gate<true>(a, s); }
 
-eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s) {
+template <template <int> class Row>
+static eqb_status launch_columns_of(const CodeArgs& a, int per_value, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.H + kColumnCols - 1) / kColumnCols * (column_width(a.rows, a.E) / kCodeBlock);
   const int64_t row = a.H * bytes_of(a.dtype);
-  if (row % 128 == 0 && a.rows * row >= kStreamBytes) return launch_tiles<false, true>(a, tiles, s);
-  return launch_tiles<false, false>(a, tiles, s);
+  if (row % 128 == 0 && a.rows * row * per_value >= kStreamBytes) return launch_tiles<Row, false, true>(a, tiles, s);
+  return launch_tiles<Row, false, false>(a, tiles, s);
 }
+eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s) { return launch_columns_of<PlainRow>(a, 1, s); }
+eqb_status launch_gated_quantize_columns(const CodeArgs& a, hipStream_t s) { return launch_columns_of<StoredGate>(a, 2, s); }
 eqb_status launch_quantize_weights(const CodeArgs& a, hipStream_t s) {
   const int64_t tiles = code_width(a.H) / kCodeBlock * (code_width(a.N) / kCodeBlock) * a.E, row = a.H * bytes_of(a.dtype);
-  if (row % 128 == 0 && (int64_t)a.E * a.N * row >= kStreamBytes) return launch_tiles<true, true>(a, tiles, s);
-  return launch_tiles<true, false>(a, tiles, s);
+  if (row % 128 == 0 && (int64_t)a.E * a.N * row >= kStreamBytes) return launch_tiles<PlainRow, true, true>(a, tiles, s);
+  return launch_tiles<PlainRow, true, false>(a, tiles, s);
 }
 
 }  // namespace eqb

@@ -630,8 +630,9 @@ eqb_status eqb_dispatch_quantized(const void* x, const int32_t* slot, int64_t T,
   return launch_dispatch_quantized(a, static_cast<hipStream_t>(stream));
 }
 
-eqb_status eqb_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
-                                int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream) {
+static eqb_status columns_call(eqb_status (*launch)(const CodeArgs&, hipStream_t), const void* x, const int32_t* offsets,
+                               int64_t rows, int32_t E, int32_t hidden, int32_t dtype, uint8_t* codes, uint8_t* scales,
+                               void* stream) {
   if (!code_shape(rows, hidden, dtype) || E < 1) return EQB_ERR_INVALID_ARG;
   if (E > kMostExperts) return EQB_ERR_UNSUPPORTED;
   if (rows == 0) return EQB_OK;
@@ -646,7 +647,17 @@ eqb_status eqb_quantize_columns(const void* x, const int32_t* offsets, int64_t r
   a.dtype = dtype;
   a.codes = codes;
   a.scales = scales;
-  return launch_quantize_columns(a, static_cast<hipStream_t>(stream));
+  return launch(a, static_cast<hipStream_t>(stream));
+}
+
+eqb_status eqb_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
+                                int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream) {
+  return columns_call(launch_quantize_columns, x, offsets, rows, E, hidden, dtype, codes, scales, stream);
+}
+
+eqb_status eqb_gated_quantize_columns(const void* x, const int32_t* offsets, int64_t rows, int32_t E, int32_t hidden,
+                                      int32_t dtype, uint8_t* codes, uint8_t* scales, void* stream) {
+  return columns_call(launch_gated_quantize_columns, x, offsets, rows, E, hidden, dtype, codes, scales, stream);
 }
 
 eqb_status eqb_quantize_weights(const void* w, int32_t E, int32_t N, int32_t hidden, int32_t dtype, uint8_t* codes,

@@ -233,6 +233,7 @@ eqb_status launch_quantize_columns(const CodeArgs& a, hipStream_t s);
 eqb_status launch_quantize_weights(const CodeArgs& a, hipStream_t s);
 eqb_status launch_gated(const CodeArgs& a, hipStream_t s);
 eqb_status launch_gated_quantize(const CodeArgs& a, hipStream_t s);
+eqb_status launch_gated_quantize_columns(const CodeArgs& a, hipStream_t s);
 eqb_status launch_gated_backward(const CodeArgs& a, hipStream_t s);
 
 struct ProductArgs {

@@ -84,6 +84,7 @@ EXPORTS = (
     "eqb_experts_grad_weight",
     "eqb_gated",
     "eqb_gated_quantize",
+    "eqb_gated_quantize_columns",
     "eqb_gated_backward",
     "eqb_set_max_blocks",
     "eqb_get_max_blocks",
@@ -143,6 +144,7 @@ def _load():
         "eqb_experts_grad_weight": [P, P, P, P, P, i64, i32, i32, i32, i32, P, P],
         "eqb_gated": [P, P, i64, i32, i32, P, P],
         "eqb_gated_quantize": [P, P, i64, i32, i32, P, P, P],
+        "eqb_gated_quantize_columns": [P, P, i64, i32, i32, i32, P, P, P],
         "eqb_gated_backward": [P, P, P, i64, i32, i32, P, P],
         "eqb_set_max_blocks": [i32],
         "eqb_get_max_blocks": [],
@@ -793,6 +795,17 @@ def eqb_gated_quantize(x, codes, scales, count=None, stream=None):
     _check("eqb_gated_quantize", lib.eqb_gated_quantize(
         _ptr(x, name="x"), _ptr(count, torch.int32, 1, "count"), R, H, _row_type(x, "x"),
         *_coded(codes, scales, (R,), H, ""), _stream(stream)))
+
+
+def eqb_gated_quantize_columns(x, offsets, codes, scales, stream=None):
+    """eqb_quantize_columns of what eqb_gated makes of x [R,2H], also where its type would not hold it: what the gradient
+    of the second product's weights takes."""
+    R, H, E = x.shape[0], x.shape[1] // 2, offsets.numel() - 1
+    if x.shape[1] % 2:
+        raise ValueError("x holds gate and u in rows of an even number of elements")
+    _check("eqb_gated_quantize_columns", lib.eqb_gated_quantize_columns(
+        _ptr(x, name="x"), _ptr(offsets, torch.int32, E + 1, "offsets"), R, E, H, _row_type(x, "x"),
+        *_coded(codes, scales, (H,), eqb_column_width(R, E), ""), _stream(stream)))
 
 
 def eqb_gated_backward(grad_h, x, grad_x, count=None, stream=None):

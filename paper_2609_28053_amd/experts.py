@@ -108,9 +108,9 @@ class GatedExperts(_Handle):
         eqb.eqb_experts_product(*codes, *(weights.all()[2:] if transposed else weights.all()[:2]), offsets, out)
         return out
 
-    def _columns(self, x, offsets):
-        codes = self._codes(x.shape[1], eqb.eqb_column_width(x.shape[0], self.E), x.device)
-        eqb.eqb_quantize_columns(x, offsets, *codes)
+    def _columns(self, x, offsets, gated=False):
+        codes = self._codes(self.F if gated else x.shape[1], eqb.eqb_column_width(x.shape[0], self.E), x.device)
+        (eqb.eqb_gated_quantize_columns if gated else eqb.eqb_quantize_columns)(x, offsets, *codes)
         return codes
 
     def forward(self, x, rows: ExpertRows, stream=None, train=True, plan=None):
@@ -131,7 +131,8 @@ class GatedExperts(_Handle):
 
     def backward(self, grad_out, saved, stream=None):
         """Gradients with respect to the dispatched rows [T*K,H] (ExpertRows.combine without weights gives the tokens'),
-        to up and to down (binary32); grad_out [T*K,H] is the combine's gradient of what forward returned."""
+        to up and to down (binary32); grad_out [T*K,H] is the combine's gradient of what forward returned.  In between, the
+        gradients of the hidden rows and of the gate are of x's type."""
         x, gate, offsets, slot = saved
         with self._on(stream, grad_out, x, gate, offsets, slot):
             R, count = grad_out.shape[0], offsets[self.E:]
@@ -139,10 +140,8 @@ class GatedExperts(_Handle):
             codes = self._codes(R, self.H, x.device)
             eqb.eqb_quantize_rows(grad_out, *codes, count)
             grad_hidden = self._product(codes, self.down, True, offsets, self.F, x.dtype)
-            hidden = torch.empty_like(grad_hidden)
-            eqb.eqb_gated(gate, hidden, count)
             grad_down = new(self.E, self.H, self.F)
-            eqb.eqb_experts_grad_weight(*self._columns(grad_out, offsets), *self._columns(hidden, offsets), offsets, grad_down)
+            eqb.eqb_experts_grad_weight(*self._columns(grad_out, offsets), *self._columns(gate, offsets, gated=True), offsets, grad_down)
             grad_gate = torch.empty_like(gate)
             eqb.eqb_gated_backward(grad_hidden, gate, grad_gate, count)
             codes = self._codes(R, 2 * self.F, x.device)
