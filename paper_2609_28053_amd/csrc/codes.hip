@@ -125,9 +125,9 @@ struct PlainRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = false;
   template <bool kExact, bool kStream>
-  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+  static __device__ __forceinline__ float load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     load8<kDtype, kStream>(static_cast<const raw*>(a.x) + t * a.H, c, a.H, v);
-    return false;
+    return 0.0f;
   }
 };
 // A gated value that is to become a code is computed in binary32, within 11 2^-24 for gates above -80 (a
@@ -158,9 +158,10 @@ template <int kDtype>
 struct GatedRow {
   typedef typename Elem<kDtype>::raw raw;
   static constexpr bool kOpen = true;        // its values are not exact
-  // whether a gate is so low that its sigmoid has fewer than 24 bits in binary32
+  // Infinity if a gate is so low that its sigmoid has fewer than 24 bits in binary32; else what multiplies the
+  // 2^-150 that g sigmoid(g) is off by where it is subnormal, the largest |u| (F16's gates begin at 2^-24).
   template <bool kExact, bool kStream>
-  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+  static __device__ __forceinline__ float load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
     float g[kPer], u[kPer];
     load8<kDtype, kStream>(row, c, a.H, g);
@@ -178,7 +179,13 @@ struct GatedRow {
     float least = g[0];
 #pragma unroll
     for (int i = 1; i < kPer; ++i) least = fminf(least, g[i]);
-    return least < -80.0f;
+    if (least < -80.0f) return __builtin_inff();
+    float most = 0.0f;
+    if constexpr (kDtype != EQB_DTYPE_F16) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) most = fmaxf(most, fabsf(u[i]));
+    }
+    return most;
   }
 };
 
@@ -187,7 +194,7 @@ template <int kDtype>
 struct StoredGate {
   typedef typename Elem<kDtype>::raw raw;
   template <bool kExact, bool kStream>
-  static __device__ __forceinline__ bool load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
+  static __device__ __forceinline__ void load(const CodeArgs& a, int64_t t, int c, float (&v)[kPer]) {
     const raw* row = static_cast<const raw*>(a.x) + t * 2 * a.H;
     float g[kPer], u[kPer];
     load8<kDtype, kStream>(row, c, a.H, g);
@@ -199,7 +206,6 @@ struct StoredGate {
       const float h = g[i] * s * u[i], stored = Elem<kDtype>::to_f(Elem<kDtype>::from_f(h));
       v[i] = fabsf(stored) < __builtin_inff() ? stored : h;
     }
-    return false;
   }
 };
 
@@ -237,12 +243,14 @@ __global__ __launch_bounds__(kCodeThreads) void quantize_rows_kernel(const CodeA
         byte = scale_byte(top);
         code = codes(scale_inverse(byte));
       };
-      const bool low = Row::template load<false, kStream>(a, t, c, v);
+      const float reach = Row::template load<false, kStream>(a, t, c, v);
       encode();
       if constexpr (Row::kOpen) {
         constexpr float kLess = 1.0f - 0x1p-19f, kMore = 1.0f + 0x1p-19f;
         const uint2 less = codes(scale_inverse(byte) * kLess), more = codes(scale_inverse(byte) * kMore);
-        const bool open = low || less.x != more.x || less.y != more.y || scale_byte(top * kLess) != scale_byte(top * kMore);
+        // the least middle between two codes is 2^(byte - 137), and 2^-20 of it is left beside the other roundings
+        const float most = __uint_as_float((uint32_t)(byte < 134 ? byte + 120 : 254) << 23);
+        const bool open = reach > most || less.x != more.x || less.y != more.y || scale_byte(top * kLess) != scale_byte(top * kMore);
         if (__ballot(open)) {
           Row::template load<true, kStream>(a, t, c, v);
           encode();
