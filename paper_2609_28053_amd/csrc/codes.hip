@@ -132,20 +132,30 @@ struct PlainRow {
 };
 // A gated value that is to become a code is computed in binary32, within 11 2^-24 for gates above -80 (a
 // sigmoid 8, three roundings).  Where that leaves open which of two codes it is, some six in a hundred
-// thousand, and for lower gates, it is computed once more to 37 bits and rounded to the odd neighbour in
+// thousand, and for lower gates, it is computed once more to some 50 bits and rounded to the odd neighbour in
 // binary32, so that the code's rounding is as if it were the only one.  The exponential is then its series to
-// y^9 for |y| <= ln 2 / 2 (off by 7e-12).  98,304 rows of 2,048 bf16: 291 us; all of them to 37 bits 385.
+// y^12 for |y| <= ln 2 / 2 (off by 2e-16), e^-a of a from 1,200 on 0.
 __device__ __forceinline__ double sigmoid_wide(double x) {
-  const double a = fmin(fabs(x), 200.0), n = __builtin_rint(a * 1.4426950408889634);
-  const double y = __builtin_fma(n, 0.6931471805599453, -a);
-  double e = 1.0 / 362880;
-  constexpr double c[9] = {1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0};
+  const double a = fmin(fabs(x), 1200.0), n = __builtin_rint(a * 1.4426950408889634);
+  const double y = __builtin_fma(n, 2.3190468138462996e-17, __builtin_fma(n, 0.6931471805599453, -a));      // n ln 2 in two parts
+  double e = 1.0 / 479001600;
+  constexpr double c[12] = {1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720,
+                            1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0};
 #pragma unroll
-  for (int i = 0; i < 9; ++i) e = __builtin_fma(e, y, c[i]);
+  for (int i = 0; i < 12; ++i) e = __builtin_fma(e, y, c[i]);
   e = __builtin_amdgcn_ldexp(e, -(int)n);
-  const double d = 1.0 + e, r0 = __builtin_amdgcn_rcp(d);      // within 2^-23, squared by the step
-  const double r = __builtin_fma(__builtin_fma(-d, r0, 1.0), r0, r0);
+  const double d = 1.0 + e, r0 = __builtin_amdgcn_rcp(d);      // within 2^-23, squared by each step
+  const double r1 = __builtin_fma(__builtin_fma(-d, r0, 1.0), r0, r0), r = __builtin_fma(__builtin_fma(-d, r1, 1.0), r1, r1);
   return x >= 0.0 ? r : e * r;
+}
+// g sigmoid(g) u.  Of a small gate it is p (1 + g / 2), p = g u / 2 (the next term is below 2^-64 of p): p has at most 48
+// bits and may be the middle between two codes, so that the side on which the rest lies is kept however small it is.
+__device__ __forceinline__ double gated_wide(double g, double u) {
+  if (fabs(g) >= 0x1p-30) return g * sigmoid_wide(g) * u;
+  const double p = 0.5 * g * u, h = __builtin_fma(p, 0.5 * g, p);
+  if (p == 0.0) return p;                     // with its sign
+  if (h != p) return h;
+  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + (g > 0.0 ? 1 : -1));
 }
 __device__ __forceinline__ float round_odd(double h) {
   const float r = (float)h;
@@ -169,7 +179,7 @@ struct GatedRow {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if constexpr (kExact) {
-        v[i] = round_odd((double)g[i] * sigmoid_wide(g[i]) * (double)u[i]);
+        v[i] = round_odd(gated_wide(g[i], u[i]));
       } else {
         float s, rest;
         sigmoid_both(g[i], s, rest);
