@@ -47,8 +47,6 @@ struct Eight {
 // -> 119, gates and their gradients 496 -> 483; but 20,012 rows of 1,001 by columns 20.3 -> 23.8.
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 template <bool kStream, class V>
-__device__ __forceinline__ V load_at(const V* at) { return kStream ? __builtin_nontemporal_load(at) : *at; }
-template <bool kStream, class V>
 __device__ __forceinline__ void store_at(V* at, V v) {
   if constexpr (kStream) __builtin_nontemporal_store(v, at);
   else *at = v;
@@ -59,7 +57,9 @@ template <int kDtype, bool kStream>
 __device__ __forceinline__ void load8(const typename Elem<kDtype>::raw* row, int c, int H, float (&v)[kPer]) {
   typedef Elem<kDtype> D;
   if (c + kPer <= H) {
-    const typename Eight<kDtype>::vec x = load_at<kStream>(reinterpret_cast<const typename Eight<kDtype>::any*>(row + c));
+    // not through a template over the type, which would drop its alignment
+    const auto* const at = reinterpret_cast<const typename Eight<kDtype>::any*>(row + c);
+    const typename Eight<kDtype>::vec x = kStream ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = D::to_f(x[i]);
   } else {
@@ -75,7 +75,9 @@ __device__ __forceinline__ void store8(typename Elem<kDtype>::raw* row, int c, i
 #pragma unroll
   for (int i = 0; i < kPer; ++i) x[i] = D::from_f(v[i]);
   if (c + kPer <= H) {
-    store_at<kStream>(reinterpret_cast<typename Eight<kDtype>::any*>(row + c), (typename Eight<kDtype>::any)x);
+    auto* const at = reinterpret_cast<typename Eight<kDtype>::any*>(row + c);
+    if constexpr (kStream) __builtin_nontemporal_store(x, at);
+    else *at = x;
   } else {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
