@@ -261,7 +261,7 @@ __device__ __forceinline__ bool choose(const ScoredArgs& a, const float (&z)[kPe
 template <int E, int kDtype>
 __device__ __forceinline__ void load_row(const void* z, int64_t t, int l, float (&v)[kPer]) {
   typedef typename Logit<kDtype>::raw raw;
-  typedef raw vec __attribute__((ext_vector_type(kPer)));
+  typedef raw vec __attribute__((ext_vector_type(kPer), aligned(16)));       // what a caller promises
   const vec x = *reinterpret_cast<const vec*>(static_cast<const raw*>(z) + t * E + l * kPer);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) v[i] = clean(Logit<kDtype>::to_f(x[i]));
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(kScoredThreads, N == 8 ? 4 : 3) void route_scored_b
   constexpr int kLists = V > N ? V / N : 1, kListPieces = kPieces / kLists;       // a lane's lists of N
   constexpr int kSlow = E / kPer;               // lanes of a row that is looked at once more
   typedef typename Logit<kDtype>::raw raw;
-  typedef raw vec __attribute__((ext_vector_type(kPer)));
+  typedef raw vec __attribute__((ext_vector_type(kPer), aligned(16)));       // what a caller promises
   __shared__ __attribute__((aligned(16))) float sh_bias[E];
   __shared__ int16_t sh_chosen[kScoredWaves][N];
   const int lane = threadIdx.x & 63, l = lane % L;

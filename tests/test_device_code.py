@@ -32,8 +32,8 @@ def ir(tmp_path_factory):
         with open(to) as f:
             return f.read()
 
-    names = ("codes", "products")
-    with concurrent.futures.ThreadPoolExecutor(2) as pool:
+    names = ("codes", "scored", "products")
+    with concurrent.futures.ThreadPoolExecutor(3) as pool:
         return dict(zip(names, pool.map(compiled, names)))
 
 
@@ -43,7 +43,7 @@ def accesses(text):
     return [(t, int(a)) for t, a in found]
 
 
-@pytest.mark.parametrize("name", ["codes", "products"])
+@pytest.mark.parametrize("name", ["codes", "scored", "products"])
 def test_no_access_claims_more_than_sixteen_bytes(ir, name):
     found = accesses(ir[name])
     assert len(found) > 100
