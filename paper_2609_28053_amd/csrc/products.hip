@@ -116,14 +116,18 @@ __device__ __forceinline__ void step_barrier() { asm volatile("s_waitcnt vmcnt(0
 
 // Memory to LDS: 16 (4) bytes a lane from base + off to to + 16 (4) lane.  Written out, since
 // the compiler would wait for all of them before any LDS read: step_barrier waits for them.
+// They change m0, which the compiler reserves: it says that it will not keep what was there, and need not.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy16(uint8_t* to, const uint8_t* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(lds_word*)to), "v"(off), "s"(base)
-               : "memory");
+               : "m0", "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t* to, const uint8_t* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"((uint32_t)(uintptr_t)(lds_word*)to), "v"(off), "s"(base)
-               : "memory");
+               : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 // What a tile of out is computed from.
 struct Tile {

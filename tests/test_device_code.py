@@ -1,5 +1,5 @@
 """The GPU code that the compiler is given (CPU only: LLVM IR of code built here): the alignment that each access of global
-memory is taken to have.
+memory is taken to have, and what inline assembly says that it changes.
 
 The header promises 16 bytes for logits, codes and scales and an element's size for rows; an access that claims more is
 undefined for what the header allows."""
@@ -57,3 +57,9 @@ def test_rows_may_begin_at_any_element(ir, name):
     rows = [(t, a) for t, a in accesses(ir[name]) if re.fullmatch(r"<8 x (i16|half|bfloat|float)>", t)]
     assert len(rows) > 50
     assert not [(t, a) for t, a in rows if a > size[t[5:-1]]]
+
+
+def test_assembly_that_writes_m0_says_so(ir):
+    calls = re.findall(r'asm sideeffect "([^"]*)", "([^"]*)"', ir["products"])
+    written = [c for c in calls if re.search(r"s_mov_b32 m0", c[0])]
+    assert len(written) > 50 and all("~{m0}" in c[1] for c in written)
