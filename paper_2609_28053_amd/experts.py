@@ -68,9 +68,12 @@ class _Weights:
         self.scales = new(eqb._SCALES, E, up(N), eqb.eqb_scale_width(H))
         self.scales_t = new(eqb._SCALES, E, up(H), eqb.eqb_scale_width(N))
 
-    def take(self, w):
+    def check(self, w):
         if tuple(w.shape) != self.shape:
             raise ValueError(f"weights have shape {tuple(w.shape)}, expected {self.shape}")
+        eqb._ptr(w, tuple(eqb._ROW_TYPES), name="weights")
+
+    def take(self, w):
         eqb.eqb_quantize_weights(w, self.codes, self.scales, self.codes_t, self.scales_t)
 
     def all(self):
@@ -94,7 +97,9 @@ class GatedExperts(_Handle):
         return (*self.up.all(), *self.down.all())
 
     def refresh(self, up, down, stream=None):
-        """Takes over new weights."""
+        """Takes over new weights; ones that do not fit change nothing."""
+        self.up.check(up)
+        self.down.check(down)
         with self._on(stream, up, down):
             self.up.take(up)
             self.down.take(down)
