@@ -104,6 +104,10 @@ class GatedExperts(_Handle):
             self.up.take(up)
             self.down.take(down)
 
+    def _width(self, x, name):
+        if x.shape[1] != self.H:              # other rows may have as many codes
+            raise ValueError(f"{name} has rows of {x.shape[1]} elements, the experts take {self.H}")
+
     def _codes(self, rows, hidden, device):
         return (torch.empty((rows, eqb.eqb_code_width(hidden)), dtype=torch.uint8, device=device).view(eqb._CODES),
                 torch.empty((rows, eqb.eqb_scale_width(hidden)), dtype=torch.uint8, device=device).view(eqb._SCALES))
@@ -124,6 +128,7 @@ class GatedExperts(_Handle):
         offsets, slot = (rows.offsets, rows.slot) if plan is None else plan
         if offsets is None:
             raise ValueError("no plan has been made")
+        self._width(x, "x")
         with self._on(stream, x, offsets, slot):
             R, count = slot.numel(), offsets[self.E:]
             codes = self._codes(R, self.H, x.device)
@@ -139,6 +144,7 @@ class GatedExperts(_Handle):
         to up and to down (binary32); grad_out [T*K,H] is the combine's gradient of what forward returned.  In between, the
         gradients of the hidden rows and of the gate are of x's type."""
         x, gate, offsets, slot = saved
+        self._width(grad_out, "grad_out")
         with self._on(stream, grad_out, x, gate, offsets, slot):
             R, count = grad_out.shape[0], offsets[self.E:]
             new = lambda *s: torch.empty(s, dtype=torch.float32, device=x.device)  # noqa: E731

@@ -33,3 +33,17 @@ def test_refresh_takes_both_weights_or_none():
     experts.refresh(other, down)
     got, _ = experts.forward(x, rows)
     assert not torch.equal(got, want)
+
+
+def test_rows_of_another_width_are_refused():
+    """Rows of 72 and of 80 elements have codes of the same width, 128."""
+    say("rows of another width")
+    up, down, x, rows, experts = made()
+    wide = torch.zeros((50, 80), dtype=torch.bfloat16, **D)
+    for train in (False, True):
+        with pytest.raises(ValueError, match="80"):
+            experts.forward(wide, rows, train=train)
+    out, saved = experts.forward(x, rows)
+    with pytest.raises(ValueError, match="80"):
+        experts.backward(torch.zeros((100, 80), dtype=torch.bfloat16, **D), saved)
+    experts.backward(torch.zeros_like(out), saved)
