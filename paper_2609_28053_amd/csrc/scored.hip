@@ -131,6 +131,11 @@ __device__ __forceinline__ void merge2(F& a1, F& a2, F b1, F b2) {
   a2 = fmax(lo, fmax(a2, b2));
 }
 
+// A group's score of its two best.  In binary32 a sum that it does not hold counts as its largest or lowest number, so that
+// groups of such sums are no masked ones (-inf) and meet, which near() sends to binary64.
+__device__ __forceinline__ float sum_of_two(float a, float b) { return fminf(fmaxf(a + b, -kLargest), kLargest); }
+__device__ __forceinline__ double sum_of_two(double a, double b) { return a + b; }
+
 // Every expert's group score.
 template <int L, class F>
 __device__ __forceinline__ void group_scores(const F (&q)[kPer], int each, int group_top, F (&g)[kPer]) {
@@ -168,7 +173,7 @@ __device__ __forceinline__ void group_scores(const F (&q)[kPer], int each, int g
     }
   }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) g[i] = group_top == 2 && t2[i] > lowest_of<F>() ? t1[i] + t2[i] : t1[i];
+  for (int i = 0; i < kPer; ++i) g[i] = group_top == 2 && t2[i] > lowest_of<F>() ? sum_of_two(t1[i], t2[i]) : t1[i];
 }
 
 // The largest of a row's values and the lowest place that has it (kNone: all -inf).
@@ -195,7 +200,8 @@ __device__ __forceinline__ int largest(const F (&q)[kPer], int l, F& top) {
 //   d = 39, less than 2^-56 behind that), and its sum of 256, a tree of 32 and 3 levels or of 8 and 5, by 35
 //   2^-24, the same way for a row: 2^-16 (|q| + bias) + 2^-54.
 __device__ __forceinline__ bool near(float a, float b, float most_bias, bool softmax) {
-  return a - b <= (softmax ? 0x1p-16f : 0x1.8p-20f) * (fabsf(a) + most_bias) + (softmax ? 0x1p-54f : 0x1p-28f);
+  // two infinities are near
+  return !(a - b > (softmax ? 0x1p-16f : 0x1.8p-20f) * (fabsf(a) + most_bias) + (softmax ? 0x1p-54f : 0x1p-28f));
 }
 __device__ __forceinline__ bool near(double, double, float, bool) { return false; }
 
@@ -474,7 +480,7 @@ __device__ __forceinline__ bool group_kept(const ScoredArgs& a, float t1, float 
     if (share >= 4) join(from_lane<2>(t1), from_lane<2>(t2));
   }
   const float none = -__builtin_inff();
-  const float g = a.group_top == 2 && t2 > none ? t1 + t2 : t1;
+  const float g = a.group_top == 2 && t2 > none ? sum_of_two(t1, t2) : t1;
   const int mine = l / share;
   int better = 0;
   auto look = [&](auto x) {
