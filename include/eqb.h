@@ -579,8 +579,9 @@ eqb_status eqb_quantize_weights(const void* w, int32_t E, int32_t N, int32_t hid
  *     columns' codes of grad [rows, N] and of x [rows, hidden]; zeros for an expert without rows.  Columns
  *     of up to 2^24.
  * Results of 16 bits come from 8-bit matrix instructions, whose sum over a block of 128 cuts off what
- * lies 16 bits below the block's largest product; results in binary32 from BF16 ones, which sum in
- * full (and take a code times its scale below 2^-133 as 0, from 2^128 on as infinite).
+ * lies 16 bits below the block's largest product: at most 2^-9 of that product a block, which may be
+ * more than a sum whose terms cancel; results in binary32 from BF16 ones, which sum in full (and take
+ * a code times its scale below 2^-133 as 0, from 2^128 on as infinite).
  */
 eqb_status eqb_experts_product(const uint8_t* codes, const uint8_t* scales, const uint8_t* w_codes,
                                const uint8_t* w_scales, const int32_t* offsets, int64_t rows, int32_t E, int32_t N,

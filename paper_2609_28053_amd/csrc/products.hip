@@ -7,10 +7,11 @@
 // contracted over an expert's rows.  One matrix instruction contracts over a whole block
 // of 128 and takes both scales, which are powers of two, so that a block costs no
 // operation beside it.  But it adds a block's 128 products with what lies some 16 bits
-// below the largest of them cut off: on codes of 11 binades a sum is off by 5e-5 of itself,
-// a quarter of what rounding to f16 costs.  That serves results of 16 bits; for results in
-// binary32 the codes become BF16 with their scale (exact down to 2^-133) on the way from LDS,
-// and the instruction for those sums in full (6e-8), at half the rate.
+// below the largest of them cut off: at most 2^-9 of the largest, however small the sum is; on
+// random codes of 11 binades 5e-5 of the sum, a quarter of what rounding to f16 costs.  That
+// serves results of 16 bits, which are rounded by up to 2^-8 (bf16) or 2^-11 of themselves; for
+// results in binary32 the codes become BF16 with their scale (exact down to 2^-133) on the way
+// from LDS, and the instruction for those sums in full (6e-8), at half the rate.
 #include "eqb_internal.hpp"
 
 namespace eqb {

@@ -373,7 +373,10 @@ __device__ __forceinline__ void softmax_of(const float (&z)[V], float& top, floa
 // SIMD: 55 us (1.4 TB/s; the bytes alone take 15), K = 8 60, without groups 47, without a bias as well 35,
 // a softmax 77; K = 12 77 and K = 16 82 at three waves, 80 and 84 at four, 89 and 94 at two.  Where a wider
 // bound of doubt sent more rows to binary64: K = 6 at four waves 68, five 70, six 79, two waves with all
-// 32 keys of a lane in registers 151.  With K rounds of a maximum over 32 lanes, as above, K = 6 215, K = 12 280.
+// 32 keys of a lane in registers 151.  All of that is with biases of which no two are equal: two experts of equal
+// logits and biases are in doubt as well, and with a bias of zeros, or of steps of 0.001, K = 6 takes 212 and 74 us,
+// K = 8 288 and 87, without groups 224 and 74; the bound grows with the largest bias, and one of -1e9 sends every row
+// to binary64 (485 us).  With K rounds of a maximum over 32 lanes, as above, K = 6 215, K = 12 280.
 __device__ __forceinline__ double key_max(double a, double b) {
   double r;
   asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
